@@ -218,6 +218,118 @@ int loract_prenorm_backward(const void* A_dev, int64_t m, int64_t n, int64_t lda
                             int64_t ldda, void* dX_dev, int64_t lddx, void* stream);
 
 /*
+ * The sub-layer around a compressed activation (Section 3.3: Z = F(Norm(X)) + X): the linear maps with what
+ * follows them, their backward pass, dropout, and the norm and rotation of queries and keys.
+ */
+
+/* Activations of loract_linear: none, max(z, 0), z Phi(z) (by erf), z / (1 + exp(-z)). */
+typedef enum { LORACT_ACT_NONE = 0, LORACT_ACT_RELU = 1, LORACT_ACT_GELU = 2, LORACT_ACT_SILU = 3 } loract_act;
+/* Layouts of loract_linear's weights. */
+typedef enum { LORACT_W_OUT_IN = 0, LORACT_W_IN_OUT = 1 } loract_w_layout;
+#define LORACT_MAX_LORA_RANK 64
+#define LORACT_MAX_HEAD 1024     /* largest head size of loract_qknorm_rope_* */
+
+/*
+ * Dropout from a counter.  Element (i, j) of an m x n matrix is kept where the 16-bit field
+ *   bits 16 (j mod 4) .. 16 (j mod 4) + 15  of  splitmix64 output number  i ceil(n/4) + floor(j/4) + 1  of `seed`
+ * is at least thr = floor(65536 p + 1/2) (65535 at most), and then multiplied by 65536 / (65536 - thr); all others
+ * become 0 whatever they hold.  The mask is a function of seed, i and j alone: it is never stored, and the gradient
+ * is the same call on the output's gradient.
+ *   Y = D(X) + R
+ * X_dev, R_dev (optional), Y_dev: m x n of dtype (leading dimensions ldx, ldr, ldy); Y may be X or R.  0 <= p < 1.
+ */
+int loract_dropout(const void* X_dev, int64_t ldx, const void* R_dev, int64_t ldr, int64_t m, int64_t n, int32_t dtype,
+                   double p, uint64_t seed, void* Y_dev, int64_t ldy, void* stream);
+
+typedef struct {
+  int64_t m;             /* tokens */
+  int64_t n_in, n_out;   /* sizes of the map */
+  int64_t ldx;           /* leading dimensions in elements: X (backward: unused) */
+  int64_t ldw;           /* W (backward: unused) */
+  int64_t ldr;           /* residual (backward: unused) */
+  int64_t ldy;           /* Y (backward: dY) */
+  int64_t ldz;           /* Z */
+  int64_t ldp;           /* backward: dP (forward: unused) */
+  int32_t dtype;         /* loract_dtype of X, W, T, B_lora, R, Z (backward: of dY, Z, T, dP) */
+  int32_t out_dtype;     /* loract_dtype of Y; float32 inputs require float32 (backward: unused) */
+  int32_t w_layout;      /* loract_w_layout */
+  int32_t act;           /* loract_act */
+  int32_t r_lora;        /* columns of T, 0 = no low-rank term, at most LORACT_MAX_LORA_RANK */
+  float lora_scale;
+  double p_drop;         /* 0 <= p_drop < 1 */
+  uint64_t seed;         /* of the dropout mask */
+} loract_linear_params;
+
+/*
+ * Linear map of a sub-layer with everything that follows it:
+ *   P = X W^T + lora_scale T B_lora + bias,   Y = R + D(act(P))
+ * X_dev     m x n_in.   W_dev  n_out x n_in (LORACT_W_OUT_IN) or n_in x n_out (LORACT_W_IN_OUT): with the other layout's name
+ *           the same weights give the input gradient dP W of the backward pass.
+ * bias_dev  n_out floats, or NULL.   T_dev m x r_lora and Blora_dev r_lora x n_out, contiguous: the low-rank update with
+ *           T = X A (itself a call with W = A), as B_lora of loract_lora_grad; not read if r_lora is 0.
+ * R_dev     m x n_out, or NULL.   Y_dev out, m x n_out of out_dtype; Y may be R where their types and ld are the same.
+ * Z_dev     out, m x n_out of dtype, or NULL: P rounded to dtype, what the backward pass reads.
+ * Sums are float32.  Workspace: loract_linear_workspace_bytes.  NaN and infinities of X and W reach the outputs they belong to.
+ */
+int loract_linear_workspace_bytes(const loract_linear_params* p, size_t* bytes);
+int loract_linear(const void* X_dev, const void* W_dev, const float* bias_dev, const void* T_dev, const void* Blora_dev,
+                  const void* R_dev, const loract_linear_params* p, void* Y_dev, void* Z_dev, void* ws_dev,
+                  size_t ws_bytes, void* stream);
+
+/*
+ * Backward of loract_linear up to the products, one pass over dY and Z:
+ *   dP = act'(Z) D(dY),   dbias_j = sum_i dP_ij,   dB_lora = lora_scale T^T dP
+ * Z_dev     what the forward call kept; not read (may be NULL) without an activation.
+ * dP_dev    out, m x n_out of dtype.   dbias_dev out, n_out floats, or NULL.   dB_dev out, r_lora x n_out floats, or NULL
+ *           (then T_dev is not read).  The sums are of the unrounded float32 dP.
+ * The rest of the backward pass are calls on dP: dT = lora_scale dP B_lora^T and dX = dP W + dT A^T by loract_linear,
+ * dA by loract_lora_grad.  Workspace: loract_linear_backward_workspace_bytes.
+ */
+int loract_linear_backward_workspace_bytes(const loract_linear_params* p, size_t* bytes);
+int loract_linear_backward(const void* dY_dev, const void* Z_dev, const void* T_dev, const loract_linear_params* p,
+                           void* dP_dev, float* dbias_dev, float* dB_dev, void* ws_dev, size_t ws_bytes, void* stream);
+
+/* table_dev (n_pos x rot floats): for position first + p the rot / 2 cosines, then the rot / 2 sines, of
+ * (first + p) theta^(-2 i / rot); the angle is formed in float64.  rot even, theta > 0. */
+int loract_rope_table(float* table_dev, int64_t n_pos, int32_t rot, double theta, int64_t first, void* stream);
+
+typedef struct {
+  int64_t m;             /* tokens */
+  int32_t heads_q, heads_k;      /* heads_k may be 0 */
+  int32_t d;             /* head size, at most LORACT_MAX_HEAD */
+  int32_t rot;           /* leading elements of a head that are rotated: even, 0 <= rot <= d */
+  int32_t interleaved;   /* pairs are (i, i + rot/2), or (2i, 2i + 1) if nonzero */
+  int32_t dtype;         /* loract_dtype of queries, keys and their gradients */
+  int64_t n_pos;         /* rows of the table */
+  float eps;             /* >= 0 */
+  /* strides in elements, token then head, the elements of a head are contiguous: inputs, outputs (backward: dq, dk),
+   * and the gradients of the forward's outputs (backward only) */
+  int64_t q_token, q_head, k_token, k_head;
+  int64_t qo_token, qo_head, ko_token, ko_head;
+  int64_t dq_token, dq_head, dk_token, dk_head;
+} loract_qk_params;
+
+/*
+ * RMS norm of every head of the queries and keys and the rotation by position in one pass:
+ *   y = Rot_pos(x / sqrt(mean_d x_d^2 + eps) * gamma)
+ * gamma_q_dev, gamma_k_dev: d floats, or NULL (ones).  table_dev: n_pos x rot floats of loract_rope_table (unread if rot is 0).
+ * pos_dev: m int32 positions, or NULL: token t stands at t.  A token with a negative position is padding: its outputs (and
+ * gradients) are zero and it adds nothing to gamma's gradients; a position of n_pos or more gives NaN.
+ * forward   q_out may be q, k_out may be k (with the same strides).
+ * backward  from the inputs and the gradients of the outputs: dq, dk and, where not NULL, dgamma_q, dgamma_k (d floats).
+ *           dq may be dq_out or q, dk dk_out or k (with the same strides).
+ * No workspace in the forward direction; loract_qknorm_rope_workspace_bytes in the backward one.
+ */
+int loract_qknorm_rope_workspace_bytes(const loract_qk_params* p, size_t* bytes);
+int loract_qknorm_rope_forward(const void* q_dev, const void* k_dev, const loract_qk_params* p, const float* gamma_q_dev,
+                               const float* gamma_k_dev, const float* table_dev, const int32_t* pos_dev, void* q_out_dev,
+                               void* k_out_dev, void* stream);
+int loract_qknorm_rope_backward(const void* q_dev, const void* k_dev, const loract_qk_params* p, const float* gamma_q_dev,
+                                const float* gamma_k_dev, const float* table_dev, const int32_t* pos_dev,
+                                const void* dq_out_dev, const void* dk_out_dev, void* dq_dev, void* dk_dev,
+                                float* dgamma_q_dev, float* dgamma_k_dev, void* ws_dev, size_t ws_bytes, void* stream);
+
+/*
  * Per-kernel timing with HIP events on the stream the kernels are launched on.
  * begin: start bracketing every kernel launch of this library with event records.
  * end:   stop, wait for the recorded events, and aggregate by kernel name.

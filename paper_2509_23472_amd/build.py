@@ -39,15 +39,27 @@ def source_hash() -> str:
 
 
 def build_library(verbose: bool = True) -> str:
-    """Compile every HIP source into paper_2509_23472_amd/libloract.so and return its path."""
+    """Compile every HIP source, each in a process of its own, link them into
+    paper_2509_23472_amd/libloract.so and return its path."""
+    import tempfile
     sources = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".hip"))
-    cmd = [hipcc_path()] + HIPCC_FLAGS + sources + ["-o", LIB_PATH + ".tmp"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(line for line in proc.stdout.splitlines()
-                    if "packed-fp32-ops" not in line)
-    if proc.returncode != 0:
+    with tempfile.TemporaryDirectory() as tmp:
+        objects, running = [], []
+        for src in sources:
+            obj = os.path.join(tmp, os.path.basename(src) + ".o")
+            cmd = [hipcc_path()] + [f for f in HIPCC_FLAGS if f != "-shared"] + ["-c", src, "-o", obj]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            objects.append(obj)
+            running.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+        results = [(proc.communicate()[0], proc.returncode) for proc in running]
+        link = subprocess.run([hipcc_path(), "--offload-arch=gfx950", "-fPIC", "-shared"] + objects + ["-o", LIB_PATH + ".tmp"],
+                              stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) \
+            if all(code == 0 for _, code in results) else None
+    if link is not None:
+        results.append((link.stdout, link.returncode))
+    out = "\n".join(line for text, _ in results for line in text.splitlines() if "packed-fp32-ops" not in line)
+    if any(code != 0 for _, code in results):
         raise RuntimeError("hipcc failed:\n" + out)
     if verbose and out.strip():
         print(out)

@@ -30,6 +30,15 @@ __device__ inline void store_f64(void* p, int64_t i, int ek, double v) {
   else ((bf16_t*)p)[i] = (bf16_t)(float)v;
 }
 
+// splitmix64: state += golden; output = mix(state).
+__host__ __device__ inline uint64_t splitmix64_mix(uint64_t z) {
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  return z ^ (z >> 31);
+}
+#define SPLITMIX_GOLDEN 0x9E3779B97F4A7C15ull
+
+static inline bool dtype_ok(int d) { return d == LORACT_F32 || d == LORACT_BF16; }
 static inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -39,7 +48,7 @@ static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; 
 struct LoractHostState {
   std::string last_hip_error;
 };
-static thread_local LoractHostState g_host;
+inline thread_local LoractHostState g_host;
 
 static inline int hip_fail(hipError_t e, const char* what) {
   g_host.last_hip_error = std::string(what) + ": " + hipGetErrorString(e);
@@ -60,7 +69,7 @@ struct ProfState {
   std::map<std::string, std::pair<double, int64_t>> agg;
   std::vector<std::string> order;
 };
-static ProfState g_prof;
+inline ProfState g_prof;                      // (one for all of the library's source files)
 
 static inline hipEvent_t prof_event() {   // caller holds g_prof.mu
   hipEvent_t e;

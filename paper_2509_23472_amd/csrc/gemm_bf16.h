@@ -280,7 +280,7 @@ __global__ __launch_bounds__(256) void gemm_bf16_kernel(GemmBf16Args g) {
 
 // out[row][col] = sum over splits (ascending, eight loads in flight) of part[s][row][col], converted to
 // out_kind; columns N .. n_pad-1 are written as zero.
-__global__ __launch_bounds__(256) void reduce_partials_f32(const float* part, int splits, int64_t M, int64_t N,
+static __global__ __launch_bounds__(256) void reduce_partials_f32(const float* part, int splits, int64_t M, int64_t N,
                                                            int64_t n_pad, void* out, int64_t ldc, int out_kind) {
   const int64_t total = M * N, width = N > n_pad ? N : n_pad;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < M * width; i += (int64_t)gridDim.x * blockDim.x) {

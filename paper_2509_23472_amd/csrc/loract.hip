@@ -28,14 +28,6 @@ __global__ void store_indices_kernel(IdxPack pack, int count, int32_t* dst, int3
   if (t == 0 && status) *status = 0;
 }
 
-// splitmix64: state += golden; output = mix(state).
-__host__ __device__ inline uint64_t splitmix64_mix(uint64_t z) {
-  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-  return z ^ (z >> 31);
-}
-#define SPLITMIX_GOLDEN 0x9E3779B97F4A7C15ull
-
 __global__ __launch_bounds__(256) void gaussian_kernel(void* dst, int ek, int64_t count,
                                                        uint64_t seed) {
   for (int64_t e = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; e < count;
@@ -50,8 +42,6 @@ __global__ __launch_bounds__(256) void gaussian_kernel(void* dst, int ek, int64_
 
 // ---------------------------------------------------------------------------------------------
 // Host helpers.
-
-static bool dtype_ok(int d) { return d == LORACT_F32 || d == LORACT_BF16; }
 
 static int sample_indices_host(int64_t m, int32_t l, uint64_t seed, int32_t* out) {
   if (!out || l < 0 || m < 0 || l > m || m > 0x7fffffffLL) return LORACT_ERR_INVALID_ARG;
