@@ -3,6 +3,7 @@
 #include "common.h"
 #include "dropout.h"
 #include "linear_backward.h"
+#include "linear_large.h"
 #include "linear_tile.h"
 #include "qknorm.h"
 
@@ -50,7 +51,10 @@ int loract_dropout(const void* X_dev, int64_t ldx, const void* R_dev, int64_t ld
 int loract_linear_workspace_bytes(const loract_linear_params* p, size_t* bytes) {
   if (!bytes) return LORACT_ERR_INVALID_ARG;
   LORACT_TRY(check_linear_forward(p));
-  *bytes = align_up(linear_tile_part_bytes(p->m, p->n_out, p->n_in, p->dtype == LORACT_BF16), 256);
+  const bool bf16 = p->dtype == LORACT_BF16;
+  *bytes = align_up(linear_tile_part_bytes(p->m, p->n_out, p->n_in, bf16), 256);
+  if (bf16 && linear_large_pays(p->m, p->n_out, p->n_in))            // whichever the call's alignment allows
+    *bytes = std::max(*bytes, linear_large_ws_bytes(p->m, p->n_out, p->r_lora));
   return LORACT_OK;
 }
 
@@ -77,6 +81,7 @@ int loract_linear(const void* X_dev, const void* W_dev, const float* bias_dev, c
   const size_t quad = bf16 ? 8 : 16;
   e.vec = p->n_out % 4 == 0 && aligned_rows(R_dev, p->ldr, 4, quad) && aligned_rows(Z_dev, p->ldz, 4, quad) &&
           aligned_rows(Y_dev, p->ldy, 4, e.y_f32 ? 16 : 8);
+  if (bf16 && linear_large_pays(g.m, g.n, g.k) && linear_large_fits(g, w_kc)) return launch_linear_large((hipStream_t)stream, g, w_kc);
   return bf16 ? launch_linear_tile<bf16_t>((hipStream_t)stream, g, w_kc) : launch_linear_tile<float>((hipStream_t)stream, g, w_kc);
 }
 
