@@ -90,7 +90,7 @@ __global__ __launch_bounds__(64 * LB_WAVES) void linear_backward_kernel(LinBackA
         for (int e = 4 * q; e < 4 * q + 4; ++e) {
           float v = (float)y[u][e];
           if (g.d.thr) v = drop_one(g.d, word, e & 3, v);
-          if (g.Z) v *= lin_act_slope(g.act, (float)z[u][e]);
+          if (g.Z) v *= lin_act_slope<sizeof(T) == 2>(g.act, (float)z[u][e]);
           p[e] = v;
           o[e] = (T)v;
           sum[e] += v;

@@ -4,22 +4,55 @@
 #pragma once
 #include "dropout.h"
 
-// The activations and their slopes.  erff and expf are the device library's.
+// The activations and their slopes.  FAST (bf16 inputs): exp and the reciprocal by the hardware's instructions, and Phi from
+//   erfc(x) = q(t) exp(-x^2),  t = 1 / (1 + 0.4 x),  x >= 0,
+// q a polynomial fitted here to the least relative error (1.4e-7, 4e-7 evaluated in float32): relative errors below 2^-20
+// wherever the result matters to 8 bits, at a fifth of the instructions of erff, expf and a division -- an epilogue of a large tile is
+// vector instructions that nothing hides (8192 x 11008 with SiLU, 4096 in: 986 -> 706 us).  Float32 inputs take the device library's functions.
+__device__ inline float lin_exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+__device__ inline float lin_sigmoid_fast(float z) { return __builtin_amdgcn_rcpf(1.0f + lin_exp_fast(-z)); }
+// Phi(z); *density: exp(-z^2 / 2)
+__device__ inline float lin_phi_fast(float z, float* density) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.4f * 0.70710678118654752f, 1.0f));
+  float q = 0.05026593804359436f;
+  q = fmaf(q, t, -0.182917058467865f);
+  q = fmaf(q, t, 0.16911154985427856f);
+  q = fmaf(q, t, -0.005630594678223133f);
+  q = fmaf(q, t, 0.1414429396390915f);
+  q = fmaf(q, t, 0.16853874921798706f);
+  q = fmaf(q, t, 0.20784316956996918f);
+  q = fmaf(q, t, 0.22566956281661987f);
+  q = fmaf(q, t, 0.22567586600780487f);
+  *density = lin_exp_fast(-0.5f * z * z);
+  const float half = 0.5f * q * t * *density;
+  return z < 0.0f ? half : 1.0f - half;
+}
+template <bool FAST>
 __device__ inline float lin_act(int act, float z) {
   switch (act) {
     case LORACT_ACT_RELU: return z < 0.0f ? 0.0f : z;                       // (a NaN stays one)
-    case LORACT_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    case LORACT_ACT_SILU: return z / (1.0f + expf(-z));
+    case LORACT_ACT_GELU: {
+      float density;
+      return FAST ? z * lin_phi_fast(z, &density) : 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    }
+    case LORACT_ACT_SILU: return FAST ? z * lin_sigmoid_fast(z) : z / (1.0f + expf(-z));
     default: return z;
   }
 }
+template <bool FAST>
 __device__ inline float lin_act_slope(int act, float z) {
   switch (act) {
     case LORACT_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-    case LORACT_ACT_GELU:
+    case LORACT_ACT_GELU: {
+      if (FAST) {
+        float density;
+        const float phi = lin_phi_fast(z, &density);
+        return phi + z * (density * 0.39894228040143268f);
+      }
       return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * (expf(-0.5f * z * z) * 0.39894228040143268f);
+    }
     case LORACT_ACT_SILU: {
-      const float s = 1.0f / (1.0f + expf(-z));
+      const float s = FAST ? lin_sigmoid_fast(z) : 1.0f / (1.0f + expf(-z));
       return s * (1.0f + z * (1.0f - s));
     }
     default: return 1.0f;
@@ -72,7 +105,7 @@ __device__ inline void lin_store4(const LinEpilogue& e, int64_t row, int64_t col
   for (int u = 0; u < 4; ++u) {
     const float z = v[u] + b[u];
     zq[u] = (T)z;
-    float a = lin_act(e.act, z);
+    float a = lin_act<sizeof(T) == 2>(e.act, z);
     if (e.d.thr) a = drop_one(e.d, word, u, a);
     y[u] = e.R ? a + r[u] : a;
   }

@@ -1,20 +1,19 @@
 // P = X W^T + s T B for large bf16 maps: tiles of 256 x 256 on v_mfma_f32_16x16x32_bf16.
 //
-// Slabs of 32 of K go from memory straight into a ring of four LDS stages (asynchronous copies, three slabs ahead); a
-// stage holds 256 rows of X as [row][32] and either the same of W or, for W stored n_in x n_out, 32 rows of it as they lie ([k][256],
-// read with the transposing LDS read).  The 16-byte chunks of a row are permuted so that eight neighbouring lanes of a fragment read
-// hit eight different groups of banks.  A wave reads the fragments of the next 16 of K while it multiplies the present ones;
-// there is one barrier per slab, in the middle of its products.
+// Slabs of 64 of K -- whole 128-byte lines of X and of W -- go from memory straight into LDS (asynchronous copies): three stages for
+// X, fetched up to three slabs ahead, and two for W, 160 KB in all.  A stage holds 256 rows as [row][64] or, for W stored
+// n_in x n_out, 64 rows of it as they lie ([k][256], read with the transposing LDS read).  A wave reads the fragments of the next 32 of K
+// while it multiplies the present ones; there is one barrier per slab, behind the first products of its second half.
 #pragma once
 #include "linear_tile.h"
 
 #include <type_traits>
 
-#define LL_BK 32
-#define LL_STAGES 4
+#define LL_BK 64
 #define LL_WAVES 8
-#define LL_OP (256 * LL_BK * 2)       // bytes of one operand's slab
-#define LL_STAGE (2 * LL_OP)
+#define LL_STAGE (256 * LL_BK * 2)    // bytes of one operand's slab
+#define LL_X_STAGES 3
+#define LL_W_STAGES 2
 
 // XCD b % 8 takes a run of consecutive tiles; within it tiles go in bands of LL_BAND tile rows, so that the tiles that are in
 // flight on one XCD share rows of X and of W in its L2.
@@ -37,14 +36,15 @@ __device__ inline bf16x8 ll_read_tr(const unsigned char* lds, int off) {
 }
 // Where the 16-byte chunks of a row lie: chunk c of row r (along K) at c ^ ll_turn(r), chunk c of row k of W as it lies at
 // c ^ ll_turn_k(k).  The 16 lanes that LDS serves at a time (256 bytes) then read from 16 different groups of banks, whether these are 16
-// neighbours or the four runs of four that the hardware is said to take (counted: no conflicts).
-__device__ inline int ll_turn(int r) { return ((r >> 1) & 2) ^ ((r & 8) ? 3 : 0); }
+// neighbours or four runs of four (counted: no conflicts).
+__device__ inline int ll_turn(int r) { return (r >> 1) & 7; }
 __device__ inline int ll_turn_k(int k) { return 4 * (k & 3) + ((k >> 2) & 2); }
 
 template <bool WKC>
 __global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearArgs g, int tiles_m, int tiles_n) {
-  constexpr int MT = 8, NT = 4, C = 16 / LL_WAVES;       // a wave: 8 x 4 products of 16 x 16; copies per operand and slab
-  __shared__ __attribute__((aligned(16))) unsigned char smem[LL_STAGES * LL_STAGE];
+  constexpr int MT = 8, NT = 4, C = 32 / LL_WAVES;       // a wave: 8 x 4 products of 16 x 16; copies per operand and slab
+  __shared__ __attribute__((aligned(16))) unsigned char smem[(LL_X_STAGES + LL_W_STAGES) * LL_STAGE];
+  unsigned char* const smem_w = smem + LL_X_STAGES * LL_STAGE;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave >> 2, wn = wave & 3;
   int tm, tn;
@@ -55,159 +55,181 @@ __global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearAr
   const char* const xb = (const char*)((const bf16_t*)g.X + row0 * g.ldx);
   const char* const wb = (const char*)((const bf16_t*)g.W + (WKC ? col0 * g.ldw : col0));
   const int64_t w_step = WKC ? 2 * LL_BK : 2 * LL_BK * g.ldw;
+  // copy c of a wave: 8 rows of 128 bytes along K, or two rows of 512 bytes of W as it lies
+  const int copy_row = 8 * wave * C + (lane >> 3), copy_k = 2 * wave * C + (lane >> 5);
+  auto chunk_of = [&](int c) { return (lane & 7) ^ ll_turn(copy_row + 8 * c); };
+  auto col_of = [&](int c) {
+    const int64_t col = ((lane & 31) ^ ll_turn_k(copy_k + 2 * c)) * 8;
+    return col0 + col < g.n ? col : g.n - 8 - col0;                         // columns past the end are never stored
+  };
   unsigned xo[C], wo[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int p = wave * C + c, row = 16 * p + (lane >> 2), chunk = (lane & 3) ^ ll_turn(row);
-    const int64_t xr = row0 + row < g.m ? row : g.m - 1 - row0;            // rows past the end are never stored
-    xo[c] = (unsigned)(xr * g.ldx * 2) + chunk * 16;
+    const int row = copy_row + 8 * c;
+    const int64_t xr = row0 + row < g.m ? row : g.m - 1 - row0;            // (nor rows)
+    xo[c] = (unsigned)(xr * g.ldx * 2) + chunk_of(c) * 16;
     if (WKC) {
       const int64_t wr = col0 + row < g.n ? row : g.n - 1 - col0;
-      wo[c] = (unsigned)(wr * g.ldw * 2) + chunk * 16;
+      wo[c] = (unsigned)(wr * g.ldw * 2) + chunk_of(c) * 16;
     } else {
-      const int kr = 2 * p + (lane >> 5), col = ((lane & 31) ^ ll_turn_k(kr)) * 8;
-      wo[c] = (unsigned)(kr * g.ldw * 2) + (unsigned)(col0 + col < g.n ? col : g.n - 8 - col0) * 2;
+      wo[c] = (unsigned)((copy_k + 2 * c) * g.ldw * 2) + (unsigned)col_of(c) * 2;
     }
   }
-  // Slabs are numbered through: nlr of T and B, then those of X and W.
-  const int r = g.T ? (int)g.r : 0, nlr = (r + LL_BK - 1) / LL_BK, slabs = nlr + nslab;
-  auto copy = [&](int v) {
+  // Slabs are numbered through: the one of T and B, if there is a low-rank term, then those of X and W.
+  const int r = g.T ? (int)g.r : 0, nlr = r ? 1 : 0, slabs = nlr + nslab;
+  auto x_stage = [&](int v) { return smem + v % LL_X_STAGES * LL_STAGE; };
+  auto w_stage = [&](int v) { return smem_w + v % LL_W_STAGES * LL_STAGE; };
+  auto copy_x = [&](int v) {
+    unsigned char* const st = x_stage(v) + wave * (C * 1024);
     if (v >= slabs) v = slabs - 1;                                         // (never multiplied)
-    unsigned char* const st = smem + (v & 3) * LL_STAGE + wave * (C * 1024);
-    if (v < nlr) {
-      const int left = r - v * LL_BK;
+    const int left = v < nlr ? r : k_len - (v - nlr) * LL_BK;              // of K in this slab
+    const char* const xs = xb + (int64_t)(v - nlr) * (2 * LL_BK);
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int p = wave * C + c, row = 16 * p + (lane >> 2), chunk = (lane & 3) ^ ll_turn(row);
-        const int64_t tr = row0 + row < g.m ? row0 + row : g.m - 1;
-        sb_async16((const bf16_t*)g.T + tr * r + v * LL_BK + (chunk * 8 < left ? chunk * 8 : 0), st + c * 1024);
-        const int kr = 2 * p + (lane >> 5), col = ((lane & 31) ^ ll_turn_k(kr)) * 8;
-        sb_async16((const bf16_t*)g.B + (int64_t)(v * LL_BK + (kr < left ? kr : left - 1)) * g.n + (col0 + col < g.n ? col0 + col : g.n - 8),
-                   st + LL_OP + c * 1024);
-      }
-      return;
-    }
-    const int s = v - nlr;
-    const char* const xs = xb + (int64_t)s * (2 * LL_BK);
-    const char* const ws = wb + s * w_step;
-    const int left = k_len - s * LL_BK;                                    // of K in this slab
-    if (left >= LL_BK) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        sb_async16_at(xs, xo[c], st + c * 1024);
-        sb_async16_at(ws, wo[c], st + LL_OP + c * 1024);
-      }
-    } else {                                                               // past the end of K: something that is there
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int p = wave * C + c, row = 16 * p + (lane >> 2), chunk = (lane & 3) ^ ll_turn(row), kr = 2 * p + (lane >> 5);
-        const unsigned back = chunk * 8 < left ? 0u : chunk * 16u;
+    for (int c = 0; c < C; ++c) {
+      const int chunk = chunk_of(c);
+      const int back = chunk * 8 < left ? 0 : chunk * 16;                  // past the end of K: something that is there
+      if (v < nlr) {
+        const int64_t row = row0 + copy_row + 8 * c;
+        sb_async16((const char*)g.T + (row < g.m ? row : g.m - 1) * r * 2 + chunk * 16 - back, st + c * 1024);
+      } else {
         sb_async16_at(xs, xo[c] - back, st + c * 1024);
-        sb_async16_at(ws, wo[c] - (WKC ? back : (unsigned)((kr < left ? 0 : kr - left + 1) * g.ldw * 2)), st + LL_OP + c * 1024);
       }
     }
   };
+  auto copy_w = [&](int v) {
+    unsigned char* const st = w_stage(v) + wave * (C * 1024);
+    if (v >= slabs) v = slabs - 1;
+    const int left = v < nlr ? r : k_len - (v - nlr) * LL_BK;
+    const char* const ws = wb + (v - nlr) * w_step;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int kr = copy_k + 2 * c, chunk = chunk_of(c);
+      if (v < nlr)
+        sb_async16((const bf16_t*)g.B + (int64_t)(kr < left ? kr : left - 1) * g.n + col0 + col_of(c), st + c * 1024);
+      else if (WKC)
+        sb_async16_at(ws, wo[c] - (chunk * 8 < left ? 0 : chunk * 16), st + c * 1024);
+      else
+        sb_async16_at(ws, wo[c] - (unsigned)((kr < left ? 0 : kr - left + 1) * g.ldw * 2), st + c * 1024);
+    }
+  };
 
-  // fragments: 16 rows (columns), lane l holds row l % 16 and the eight k from 8 (l / 16) on
-  const int k_off = ((lane >> 4) ^ ll_turn(lane & 15)) << 4;
-  const int xr_off = (wm * 128 + (lane & 15)) * 64 + k_off;
-  const int wr_off = LL_OP + (wn * 64 + (lane & 15)) * 64 + k_off;
+  // fragments: 16 rows (columns), lane l holds row l % 16 and the eight k from 8 (l / 16) on of a half slab
+  const int k_off[2] = {((lane >> 4) ^ ll_turn(lane & 15)) << 4, ((4 + (lane >> 4)) ^ ll_turn(lane & 15)) << 4};
+  const int xr_off = (wm * 128 + (lane & 15)) * 128, wr_off = (wn * 64 + (lane & 15)) * 128;
   int tr_off[NT];
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     const int s16 = lane & 15, kr = 8 * (lane >> 4) + (s16 >> 2), c = wn * 64 + 16 * j + 4 * (s16 & 3);
-    tr_off[j] = LL_OP + kr * 512 + (((c >> 3) ^ ll_turn_k(kr)) << 4) + (c & 7) * 2;
+    tr_off[j] = kr * 512 + (((c >> 3) ^ ll_turn_k(kr)) << 4) + (c & 7) * 2;
   }
   bf16x8 x[2][MT], w[2][NT];
-  auto read_one = [&](int v, int set, bool w_kc, int f) {                   // fragment f of slab v: those of W, then those of X
-    const unsigned char* const st = smem + (v & 3) * LL_STAGE;
-    if (f < NT) w[set][f] = w_kc ? *(const bf16x8*)(st + wr_off + f * 1024) : ll_read_tr(st, tr_off[f]);
-    else x[set][f - NT] = *(const bf16x8*)(st + xr_off + (f - NT) * 1024);
+  // fragment f of half h of a slab: those of W, then those of X
+  auto read_one = [&](const unsigned char* xs, const unsigned char* ws, int h, bool w_kc, int f) {
+    if (f < NT) w[h][f] = w_kc ? *(const bf16x8*)(ws + wr_off + k_off[h] + f * 2048) : ll_read_tr(ws, tr_off[f] + h * (32 * 512));
+    else x[h][f - NT] = *(const bf16x8*)(xs + xr_off + k_off[h] + (f - NT) * 2048);
   };
-  auto read = [&](int v, int set, bool w_kc) {
+  auto read = [&](int v, int h, bool w_kc) {
 #pragma unroll
-    for (int f = 0; f < MT + NT; ++f) read_one(v, set, w_kc, f);
+    for (int f = 0; f < MT + NT; ++f) read_one(x_stage(v), w_stage(v), h, w_kc, f);
   };
   f32x4 acc[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
-  auto multiply = [&](int set) {
+  auto multiply = [&](int h) {
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[set][j], x[set][i], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[h][j], x[h][i], acc[i][j], 0, 0, 0);
   };
-  auto mask = [&](int set, int left) {                                      // zero past the end of K, in both operands
-    const bool keep = 8 * (lane >> 4) < left;
+  auto mask = [&](int h, int left) {                                        // zero past the end of K, in both operands
+    const bool keep = 32 * h + 8 * (lane >> 4) < left;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) x[set][i] = keep ? x[set][i] : (bf16x8){};
+    for (int i = 0; i < MT; ++i) x[h][i] = keep ? x[h][i] : (bf16x8){};
 #pragma unroll
-    for (int j = 0; j < NT; ++j) w[set][j] = keep ? w[set][j] : (bf16x8){};
+    for (int j = 0; j < NT; ++j) w[h][j] = keep ? w[h][j] : (bf16x8){};
   };
 
-  copy(0);
-  copy(1);
-  copy(2);
-  copy(3);
+  copy_x(0);
+  copy_w(0);
+  copy_x(1);
+  copy_w(1);
+  copy_x(2);
+  SB_WAIT_VMCNT(3 * C);                // slab 0 has landed
+  sb_barrier_lds();
   if (r) {
-    for (int v = 0; v < nlr; ++v) {
-      SB_WAIT_VMCNT(6 * C);            // slab v has landed
-      sb_barrier_lds();
-      read(v, 0, false);
-      mask(0, r - v * LL_BK);
-      multiply(0);
-      sb_barrier_lds();                // (its stage is free)
-      copy(v + 4);
+    read(0, 0, false);
+    mask(0, r);
+    multiply(0);
+    if (r > 32) {
+      read(0, 1, false);
+      mask(1, r);
+      multiply(1);
     }
+    sb_barrier_lds();                  // (its stages are free)
+    copy_w(2);
+    copy_x(3);
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j) acc[i][j] *= g.lora_scale;
+    SB_WAIT_VMCNT(3 * C);
+    sb_barrier_lds();
   }
-  SB_WAIT_VMCNT(6 * C);
-  sb_barrier_lds();
   read(nlr, 0, WKC);
   int v = nlr;
-  // A slab's products, with its fragments in set SET.  One instruction of another kind after a product at most: whatever keeps a
-  // wave from issuing the next product leaves its matrix unit idle.
-  auto step = [&](auto set) {
-    constexpr int SET = decltype(set)::value;
-    const char* const xs = xb + (int64_t)(v + 4 - nlr) * (2 * LL_BK);
-    const char* const ws = wb + (v + 4 - nlr) * w_step;
-    unsigned char* const st = smem + (v & 3) * LL_STAGE + wave * (C * 1024);
+  // One instruction of another kind after a product at most: whatever keeps a wave from issuing the next product leaves its
+  // matrix unit idle.
+  for (; v + 3 < nlr + full; ++v) {
+    const unsigned char *xs = x_stage(v), *ws = w_stage(v);
 #pragma unroll
     for (int u = 0; u < MT * NT; ++u) {
-      acc[u / NT][u % NT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[SET][u % NT], x[SET][u / NT], acc[u / NT][u % NT], 0, 0, 0);
+      acc[u / NT][u % NT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[0][u % NT], x[0][u / NT], acc[u / NT][u % NT], 0, 0, 0);
+      if (u < 2 * (MT + NT) && u % 2 == 0) read_one(xs, ws, 1, WKC, u / 2);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    xs = x_stage(v + 1);
+    ws = w_stage(v + 1);
+    const char* const x_src = xb + (int64_t)(v + 3 - nlr) * (2 * LL_BK);
+    const char* const w_src = wb + (v + 2 - nlr) * w_step;
+    unsigned char* const x_dst = x_stage(v) + wave * (C * 1024);
+    unsigned char* const w_dst = w_stage(v) + wave * (C * 1024);
+#pragma unroll
+    for (int u = 0; u < MT * NT; ++u) {
+      acc[u / NT][u % NT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[1][u % NT], x[1][u / NT], acc[u / NT][u % NT], 0, 0, 0);
       if (u == 3) {
-        SB_WAIT_VMCNT(4 * C);          // slab v + 1 has landed (behind it: v + 2, v + 3); everyone has read slab v
+        SB_WAIT_VMCNT(C);              // slab v + 1 has landed (behind it: X of slab v + 2); everyone has read slab v
         sb_barrier_lds();
       }
-      if (u >= 4 && u < 4 + 2 * (MT + NT) && u % 2 == 0) read_one(v + 1, SET ^ 1, WKC, (u - 4) / 2);
-      if (u >= 4 && u % 8 == 5) {
-        const int c = u / 8;
-        if (c < C) sb_async16_at(xs, xo[c % C], st + (c % C) * 1024);
-        else sb_async16_at(ws, wo[c % C], st + LL_OP + (c % C) * 1024);
+      if (u >= 4 && u < 4 + 2 * (MT + NT) && u % 2 == 0) read_one(xs, ws, 0, WKC, (u - 4) / 2);
+      if (u >= 4 && u < 4 + 3 * 2 * C && u % 3 == 1) {
+        const int c = (u - 4) / 3;
+        if (c < C) sb_async16_at(w_src, wo[c % C], w_dst + (c % C) * 1024);
+        else sb_async16_at(x_src, xo[c % C], x_dst + (c % C) * 1024);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    ++v;
-  };
-  while (v + 5 < nlr + full) {
-    step(std::integral_constant<int, 0>());
-    step(std::integral_constant<int, 1>());
   }
   for (; v < nlr + full; ++v) {
+    read(v, 1, WKC);
     multiply(0);
-    SB_WAIT_VMCNT(4 * C);
+    SB_WAIT_VMCNT(C);
     sb_barrier_lds();
-    copy(v + 4);
+    copy_w(v + 2);
+    copy_x(v + 3);
     read(v + 1, 0, WKC);               // (past the last slab: not multiplied)
+    multiply(1);
   }
   if (full < nslab) {
-    mask(0, k_len - full * LL_BK);
+    const int left = k_len - full * LL_BK;
+    mask(0, left);
     multiply(0);
+    if (left > 32) {
+      read(v, 1, WKC);
+      mask(1, left);
+      multiply(1);
+    }
   }
   SB_WAIT_VMCNT(0);
   sb_barrier_lds();
@@ -263,7 +285,7 @@ __global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearAr
 #pragma unroll
       for (int q = 0; q < N8; ++q)
 #pragma unroll
-        for (int u = 0; u < 8; ++u) y[q][u] = lin_act(e.act, y[q][u]);
+        for (int u = 0; u < 8; ++u) y[q][u] = lin_act<true>(e.act, y[q][u]);
     }
     if (e.d.thr) {
 #pragma unroll

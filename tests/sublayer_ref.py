@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import math
 
+import numpy as np
 import torch
 
 U = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}      # unit roundoff: half a step of 8 and of 24 significant bits
@@ -24,16 +25,20 @@ def splitmix64(seed, number):
 
 def drop_factors(m, n, p, seed, rows=None):
     """What dropout multiplies every element with (the rows `rows` of an m x n matrix, or all of them)."""
-    rows = range(m) if rows is None else rows
+    rows = np.arange(m) if rows is None else np.asarray(rows)
     if p == 0.0:
         return torch.ones(len(rows), n, dtype=torch.float64)
     thr = min(65535, math.floor(65536 * p + 0.5))
     per = -(-n // 4)
-    keep = []
-    for i in rows:
-        words = [splitmix64(seed, i * per + g + 1) for g in range(per)]
-        keep.append([((words[j // 4] >> (16 * (j % 4))) & 0xFFFF) >= thr for j in range(n)])
-    return torch.tensor(keep, dtype=torch.float64).view(len(rows), n) * (65536.0 / (65536 - thr))
+    number = rows.astype(np.uint64)[:, None] * np.uint64(per) + np.arange(1, per + 1, dtype=np.uint64)[None, :]
+    z = np.uint64(seed & ALL) + number * np.uint64(GOLDEN)
+    z = (z ^ (z >> np.uint64(30))) * np.uint64(C1)
+    z = (z ^ (z >> np.uint64(27))) * np.uint64(C2)
+    z ^= z >> np.uint64(31)
+    assert int(z[-1, -1]) == splitmix64(seed, int(number[-1, -1]))
+    fields = (z[..., None] >> np.array([0, 16, 32, 48], dtype=np.uint64)) & np.uint64(0xFFFF)
+    keep = torch.from_numpy((fields.reshape(len(rows), per * 4)[:, :n] >= thr).astype(np.float64))
+    return keep * (65536.0 / (65536 - thr))
 
 
 def act(name, z):

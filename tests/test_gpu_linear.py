@@ -67,6 +67,29 @@ def test_product(m, n_in, n_out, layout, dtype):
     _case(m, n_in, n_out, dtype=dtype, layout=layout)
 
 
+# large enough for the tiles of 256 x 256 (128 of them): K of one slab and of several, whole and ragged, edges in both directions
+@pytest.mark.parametrize("layout", ["nt", "nn"])
+@pytest.mark.parametrize("m,n_in,n_out,parts", [
+    (2816, 128, 3080, dict()), (2817, 136, 2824, dict(keep=True)), (4000, 200, 2048, dict(r=16, act="silu", bias=True, keep=True)),
+    (2900, 264, 2816, dict(r=33, p=0.1, residual=True)), (8, 64, 64, dict()), (3000, 168, 3000, dict(r=64, act="gelu", out_dtype="f32")),
+    (2818, 520, 2832, dict(r=8, act="relu", bias=True, p=0.2, residual=True, keep=True)), (33000, 192, 256, dict(r=5)),
+    (260, 448, 33000, dict(r=40, residual=True)), (3001, 1000, 2808, dict(p=0.3)), (2816, 384, 2816, dict(pad=8, shift=8, r=16, residual=True)),
+    (2816, 152, 2816, dict(pad=24, shift=16, r=12, act="gelu", bias=True, p=0.1))])
+def test_large_tiles(m, n_in, n_out, parts, layout):
+    _case(m, n_in, n_out, layout=layout, **parts)
+
+
+def test_large_tiles_keep_nan_and_infinity_where_they_belong():
+    for layout in ("nt", "nn"):
+        def poison(x, w):
+            x[17, 199] = float("nan")
+            w[2815, 0] = float("inf")
+            x[:, 0] = x[:, 0].abs() + 0.5
+        got = _case(2816, 200, 2816, layout=layout, poison=poison).float().cpu()
+        bad = ~torch.isfinite(got)
+        assert bad[17].all() and bad[:, 2815].all() and int(bad.sum()) == 2816 * 2 - 1
+
+
 @pytest.mark.parametrize("layout", ["nt", "nn"])
 @pytest.mark.parametrize("dtype,out_dtype", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
 @pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
