@@ -24,14 +24,14 @@ class LoractParams(ctypes.Structure):
 
 
 class LoractLinearParams(ctypes.Structure):
-    """Mirror of `loract_linear_params` in include/loract.h."""
+    """Mirror of `loract_linear_params` in include/loract.h (api.py packs the same bytes)."""
     _fields_ = [(f, ctypes.c_int64) for f in ("m", "n_in", "n_out", "ldx", "ldw", "ldr", "ldy", "ldz", "ldp")] + \
                [(f, ctypes.c_int32) for f in ("dtype", "out_dtype", "w_layout", "act", "r_lora")] + \
                [("lora_scale", ctypes.c_float), ("p_drop", ctypes.c_double), ("seed", ctypes.c_uint64)]
 
 
 class LoractQkParams(ctypes.Structure):
-    """Mirror of `loract_qk_params` in include/loract.h."""
+    """Mirror of `loract_qk_params` in include/loract.h (api.py packs the same bytes)."""
     _fields_ = [("m", ctypes.c_int64)] + \
                [(f, ctypes.c_int32) for f in ("heads_q", "heads_k", "d", "rot", "interleaved", "dtype")] + \
                [("n_pos", ctypes.c_int64), ("eps", ctypes.c_float)] + \
@@ -66,14 +66,14 @@ SIGNATURES = {
     "loract_prenorm_backward": (ctypes.c_int, [_vp, _i64, _i64, _i64, _i32, _vp, _vp, _vp, _i64, _vp,
                                                _i64, _vp]),
     "loract_dropout": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i64, _i64, _i32, ctypes.c_double, _u64, _vp, _i64, _vp]),
-    "loract_linear_workspace_bytes": (ctypes.c_int, [_P(LoractLinearParams), _P(_sz)]),
-    "loract_linear": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _P(LoractLinearParams), _vp, _vp, _vp, _sz, _vp]),
-    "loract_linear_backward_workspace_bytes": (ctypes.c_int, [_P(LoractLinearParams), _P(_sz)]),
-    "loract_linear_backward": (ctypes.c_int, [_vp, _vp, _vp, _P(LoractLinearParams), _vp, _vp, _vp, _vp, _sz, _vp]),
+    "loract_linear_workspace_bytes": (ctypes.c_int, [_vp, _P(_sz)]),
+    "loract_linear": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "loract_linear_backward_workspace_bytes": (ctypes.c_int, [_vp, _P(_sz)]),
+    "loract_linear_backward": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "loract_rope_table": (ctypes.c_int, [_vp, _i64, _i32, ctypes.c_double, _i64, _vp]),
-    "loract_qknorm_rope_workspace_bytes": (ctypes.c_int, [_P(LoractQkParams), _P(_sz)]),
-    "loract_qknorm_rope_forward": (ctypes.c_int, [_vp, _vp, _P(LoractQkParams), _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
-    "loract_qknorm_rope_backward": (ctypes.c_int, [_vp, _vp, _P(LoractQkParams), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+    "loract_qknorm_rope_workspace_bytes": (ctypes.c_int, [_vp, _P(_sz)]),
+    "loract_qknorm_rope_forward": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "loract_qknorm_rope_backward": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                                    _vp, _vp, _vp, _sz, _vp]),
     "loract_profile_begin": (ctypes.c_int, []),
     "loract_profile_end": (ctypes.c_int, []),

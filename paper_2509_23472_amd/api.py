@@ -7,12 +7,13 @@ library.  Names match the C entry points.  No step of the method runs in Python.
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Dict, Optional, Sequence, Tuple
 
 import torch
 
 from . import _lib
-from ._lib import LoractLinearParams, LoractParams, LoractQkParams
+from ._lib import LoractParams
 
 F32, BF16 = 0, 1
 MAX_RANK = 320
@@ -50,7 +51,7 @@ def _torch_dtype(code: int) -> torch.dtype:
 
 
 def _stream_ptr() -> int:
-    return int(torch.cuda.current_stream().cuda_stream)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _require_cuda(*tensors: torch.Tensor) -> None:
@@ -320,19 +321,31 @@ def loract_prenorm_backward(a: torch.Tensor, rms: torch.Tensor, gamma: torch.Ten
     return dx
 
 
-def _rows(t: torch.Tensor, shape: Tuple[int, int], dtype: torch.dtype, what: str) -> int:
+# The parameter structures of the sub-layer's entry points as bytes (loract_linear_params, loract_qk_params): a call in
+# serving is a few microseconds, and packing is a tenth of filling a ctypes structure.
+_LINEAR_PARAMS = struct.Struct("9q5ifdQ")
+_QK_PARAMS = struct.Struct("q6iqf4x12q")
+_SEED = 2 ** 64 - 1
+
+
+def _rows(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str) -> int:
     """Leading dimension of a GPU matrix of that shape and type with unit column stride."""
-    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_cuda or (shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s must be a %d x %d GPU tensor of %s with unit column stride" % ((what,) + shape + (dtype,)))
-    if shape[0] > 1 and t.stride(0) < shape[1]:
+    if t.shape != (rows, cols) or t.dtype is not dtype or not t.is_cuda:
+        raise ValueError("%s must be a %d x %d GPU tensor of %s" % (what, rows, cols, dtype))
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError("%s must have unit column stride" % what)
+    if rows < 2:
+        return cols
+    if ld < cols:
         raise ValueError("the rows of %s must not overlap" % what)
-    return t.stride(0) if shape[0] > 1 else shape[1]
+    return ld
 
 
 def _floats(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
     if t is None:
         return None
-    if t.shape != (n,) or t.dtype != torch.float32 or not t.is_contiguous() or not t.is_cuda:
+    if t.shape != (n,) or t.dtype is not torch.float32 or not t.is_contiguous() or not t.is_cuda:
         raise ValueError("%s must be a contiguous float32 GPU tensor of length %d" % (what, n))
     return t.data_ptr()
 
@@ -341,29 +354,47 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _scratch(query, where: str, params: bytes, t: torch.Tensor, stream: int) -> Tuple[Optional[int], int]:
+    """Workspace (pointer, bytes) for a call with these parameters on the stream."""
+    nbytes = ctypes.c_size_t()
+    code = query(params, ctypes.byref(nbytes))
+    if code:
+        raise LoractError(code, where)
+    if not nbytes.value:
+        return None, 0
+    ws = _workspaces.get((t.get_device(), stream))
+    if ws is None or ws.numel() < nbytes.value:
+        ws = _workspace(nbytes.value, t.device)
+    return ws.data_ptr(), ws.numel()
+
+
 def _act_code(act: str) -> int:
-    if act not in ACTIVATIONS:
+    code = ACTIVATIONS.get(act)
+    if code is None:
         raise ValueError("act must be one of %s" % ", ".join(ACTIVATIONS))
-    return ACTIVATIONS[act]
+    return code
 
 
 def loract_dropout(x: torch.Tensor, p_drop: float, seed: int, residual: Optional[torch.Tensor] = None,
                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """D(x) + residual, the mask a function of (seed, row, column) that is never stored; the gradient of D is the same
     call on the gradient.  `out` may be x or residual."""
-    _require_cuda(x)
     if x.dim() != 2:
         raise ValueError("x must be a matrix")
     m, n = x.shape
-    ldx = _rows(x, (m, n), x.dtype, "x")
-    ldr = 0 if residual is None else _rows(residual, (m, n), x.dtype, "residual")
+    dt = x.dtype
+    ldx = _rows(x, m, n, dt, "x")
+    ldr = 0 if residual is None else _rows(residual, m, n, dt, "residual")
     if out is None:
-        out = torch.empty((m, n), dtype=x.dtype, device=x.device)
-    ldy = _rows(out, (m, n), x.dtype, "out")
+        out, ldy = x.new_empty((m, n)), n
+    else:
+        ldy = _rows(out, m, n, dt, "out")
     if m == 0 or n == 0:
         return out
-    _check(_lib.load().loract_dropout(x.data_ptr(), ldx, _ptr(residual), ldr, m, n, _dtype_code(x.dtype), float(p_drop),
-                                      seed & (2 ** 64 - 1), out.data_ptr(), ldy, _stream_ptr()), "loract_dropout")
+    code = _lib.load().loract_dropout(x.data_ptr(), ldx, _ptr(residual), ldr, m, n, _dtype_code(dt), p_drop, seed & _SEED,
+                                      out.data_ptr(), ldy, _stream_ptr())
+    if code:
+        raise LoractError(code, "loract_dropout")
     return out
 
 
@@ -376,45 +407,38 @@ def loract_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor]
     x m x n_in; w n_out x n_in, or n_in x n_out with `w_transposed` (the forward's weights, for the input gradient);
     bias n_out floats; lora_t m x r and lora_b r x n_out; act none, relu, gelu or silu.  Returns Y, or (Y, Z) with
     `save_preact`: Z = P rounded to x's type, for loract_linear_backward."""
-    _require_cuda(x, w)
     if x.dim() != 2 or w.dim() != 2:
         raise ValueError("x and w must be matrices")
     m, n_in = x.shape
-    n_out = w.shape[1] if w_transposed else w.shape[0]
-    odt = x.dtype if out_dtype is None else out_dtype
-    p = LoractLinearParams(m=m, n_in=n_in, n_out=n_out, ldx=_rows(x, (m, n_in), x.dtype, "x"),
-                           ldw=_rows(w, (n_in, n_out) if w_transposed else (n_out, n_in), x.dtype, "w"),
-                           dtype=_dtype_code(x.dtype), out_dtype=_dtype_code(odt),
-                           w_layout=W_IN_OUT if w_transposed else W_OUT_IN, act=_act_code(act), lora_scale=float(lora_scale),
-                           p_drop=float(p_drop), seed=seed & (2 ** 64 - 1))
-    if (lora_t is None) != (lora_b is None):
-        raise ValueError("lora_t and lora_b go together")
-    if lora_t is not None:
+    n_out = w.shape[1 if w_transposed else 0]
+    dt = x.dtype
+    odt = dt if out_dtype is None else out_dtype
+    ldx = _rows(x, m, n_in, dt, "x")
+    ldw = _rows(w, n_in, n_out, dt, "w") if w_transposed else _rows(w, n_out, n_in, dt, "w")
+    r, t_ptr, b_ptr = 0, None, None
+    if lora_t is not None or lora_b is not None:
+        if lora_t is None or lora_b is None:
+            raise ValueError("lora_t and lora_b go together")
         r = lora_b.shape[0]
-        _rows(lora_t, (m, r), x.dtype, "lora_t")
-        _rows(lora_b, (r, n_out), x.dtype, "lora_b")
-        if not lora_t.is_contiguous() or not lora_b.is_contiguous():
+        if _rows(lora_t, m, r, dt, "lora_t") != r or _rows(lora_b, r, n_out, dt, "lora_b") != n_out:
             raise ValueError("lora_t and lora_b must be contiguous")
-        p.r_lora = r
-    if residual is not None:
-        p.ldr = _rows(residual, (m, n_out), x.dtype, "residual")
-    bias_ptr = _floats(bias, n_out, "bias")
+        t_ptr, b_ptr = lora_t.data_ptr(), lora_b.data_ptr()
+    ldr, r_ptr = (0, None) if residual is None else (_rows(residual, m, n_out, dt, "residual"), residual.data_ptr())
+    bias_ptr = None if bias is None else _floats(bias, n_out, "bias")
     if out is None:
-        out = torch.empty((m, n_out), dtype=odt, device=x.device)
-    p.ldy = _rows(out, (m, n_out), odt, "out")
-    z = None
-    if save_preact:
-        z = torch.empty((m, n_out), dtype=x.dtype, device=x.device)
-        p.ldz = n_out
-    if m == 0:
-        return (out, z) if save_preact else out
-    lib = _lib.load()
-    nbytes = ctypes.c_size_t(0)
-    _check(lib.loract_linear_workspace_bytes(ctypes.byref(p), ctypes.byref(nbytes)), "loract_linear_workspace_bytes")
-    ws = _workspace(int(nbytes.value), x.device)
-    _check(lib.loract_linear(x.data_ptr(), w.data_ptr(), bias_ptr, _ptr(lora_t), _ptr(lora_b), _ptr(residual),
-                             ctypes.byref(p), out.data_ptr(), _ptr(z), ws.data_ptr(), ws.numel(), _stream_ptr()),
-           "loract_linear")
+        out, ldy = x.new_empty((m, n_out), dtype=odt), n_out
+    else:
+        ldy = _rows(out, m, n_out, odt, "out")
+    z = x.new_empty((m, n_out)) if save_preact else None
+    if m:
+        params = _LINEAR_PARAMS.pack(m, n_in, n_out, ldx, ldw, ldr, ldy, n_out, 0, _dtype_code(dt), _dtype_code(odt),
+                                     W_IN_OUT if w_transposed else W_OUT_IN, _act_code(act), r, lora_scale, p_drop, seed & _SEED)
+        lib, stream = _lib.load(), _stream_ptr()
+        ws, size = _scratch(lib.loract_linear_workspace_bytes, "loract_linear_workspace_bytes", params, x, stream)
+        code = lib.loract_linear(x.data_ptr(), w.data_ptr(), bias_ptr, t_ptr, b_ptr, r_ptr, params, out.data_ptr(), _ptr(z), ws,
+                                 size, stream)
+        if code:
+            raise LoractError(code, "loract_linear")
     return (out, z) if save_preact else out
 
 
@@ -425,39 +449,37 @@ def loract_linear_backward(dy: torch.Tensor, z: Optional[torch.Tensor] = None, *
     """dP = act'(z) D(dy), the bias gradient (n_out floats; None without `bias_grad`) and lora_scale lora_t^T dP
     (r x n_out floats; None without `lora_t`), in one pass.  z is what loract_linear kept with `save_preact`; it may
     be None without an activation.  `out` (dP) may be dy."""
-    _require_cuda(dy)
     if dy.dim() != 2:
         raise ValueError("dy must be a matrix")
     m, n = dy.shape
-    p = LoractLinearParams(m=m, n_in=1, n_out=n, ldy=_rows(dy, (m, n), dy.dtype, "dy"), dtype=_dtype_code(dy.dtype),
-                           act=_act_code(act), lora_scale=float(lora_scale), p_drop=float(p_drop), seed=seed & (2 ** 64 - 1))
-    if p.act and z is None:
-        raise ValueError("the slope of an activation needs z")
-    if p.act:
-        p.ldz = _rows(z, (m, n), dy.dtype, "z")
+    dt = dy.dtype
+    ldy = _rows(dy, m, n, dt, "dy")
+    act_code, ldz, z_ptr = _act_code(act), 0, None
+    if act_code:
+        if z is None:
+            raise ValueError("the slope of an activation needs z")
+        ldz, z_ptr = _rows(z, m, n, dt, "z"), z.data_ptr()
     if out is None:
-        out = torch.empty((m, n), dtype=dy.dtype, device=dy.device)
-    p.ldp = _rows(out, (m, n), dy.dtype, "out")
-    db = torch.empty((n,), dtype=torch.float32, device=dy.device) if bias_grad else None
-    d_b = None
+        out, ldp = dy.new_empty((m, n)), n
+    else:
+        ldp = _rows(out, m, n, dt, "out")
+    db = dy.new_empty((n,), dtype=torch.float32) if bias_grad else None
+    r, t_ptr, d_b = 0, None, None
     if lora_t is not None:
-        p.r_lora = lora_t.shape[1] if lora_t.dim() == 2 else 0
-        _rows(lora_t, (m, p.r_lora), dy.dtype, "lora_t")
-        if not lora_t.is_contiguous():
+        r = lora_t.shape[1] if lora_t.dim() == 2 else 0
+        if _rows(lora_t, m, r, dt, "lora_t") != r:
             raise ValueError("lora_t must be contiguous")
-        d_b = torch.empty((p.r_lora, n), dtype=torch.float32, device=dy.device)
+        t_ptr, d_b = lora_t.data_ptr(), dy.new_empty((r, n), dtype=torch.float32)
     if m == 0:
         return out, db if db is None else db.zero_(), d_b if d_b is None else d_b.zero_()
-    lib = _lib.load()
-    ws = None
-    if bias_grad or lora_t is not None:
-        nbytes = ctypes.c_size_t(0)
-        _check(lib.loract_linear_backward_workspace_bytes(ctypes.byref(p), ctypes.byref(nbytes)),
-               "loract_linear_backward_workspace_bytes")
-        ws = _workspace(int(nbytes.value), dy.device)
-    _check(lib.loract_linear_backward(dy.data_ptr(), _ptr(z) if p.act else None, _ptr(lora_t), ctypes.byref(p), out.data_ptr(),
-                                      _ptr(db), _ptr(d_b), _ptr(ws), 0 if ws is None else ws.numel(), _stream_ptr()),
-           "loract_linear_backward")
+    params = _LINEAR_PARAMS.pack(m, 1, n, 0, 0, 0, ldy, ldz, ldp, _dtype_code(dt), 0, 0, act_code, r, lora_scale, p_drop, seed & _SEED)
+    lib, stream = _lib.load(), _stream_ptr()
+    ws, size = None, 0
+    if bias_grad or r:
+        ws, size = _scratch(lib.loract_linear_backward_workspace_bytes, "loract_linear_backward_workspace_bytes", params, dy, stream)
+    code = lib.loract_linear_backward(dy.data_ptr(), z_ptr, t_ptr, params, out.data_ptr(), _ptr(db), _ptr(d_b), ws, size, stream)
+    if code:
+        raise LoractError(code, "loract_linear_backward")
     return out, db, d_b
 
 
@@ -470,31 +492,39 @@ def loract_rope_table(n_pos: int, rot: int, theta: float = 10000.0, first: int =
     return table
 
 
-def _heads(t: torch.Tensor, m: int, d: int, dtype: torch.dtype, what: str) -> Tuple[int, int]:
+def _heads(t: torch.Tensor, m: int, heads: int, d: int, dtype: torch.dtype, what: str) -> Tuple[int, int]:
     """Token and head strides of a GPU tensor tokens x heads x d with contiguous heads."""
-    if t.dim() != 3 or t.shape[0] != m or t.shape[2] != d or t.dtype != dtype or not t.is_cuda or (d > 1 and t.stride(2) != 1):
-        raise ValueError("%s must be a GPU tensor of %d tokens x heads x %d of %s with contiguous heads" % (what, m, d, dtype))
-    return t.stride(0), t.stride(1)
+    if t.shape != (m, heads, d) or t.dtype is not dtype or not t.is_cuda:
+        raise ValueError("%s must be a GPU tensor of %d tokens x %d heads x %d of %s" % (what, m, heads, d, dtype))
+    token, head, step = t.stride()
+    if step != 1 and d > 1:
+        raise ValueError("the heads of %s must be contiguous" % what)
+    return token, head
 
 
-def _qk_params(q, k, table, positions, eps, interleaved) -> LoractQkParams:
-    _require_cuda(q)
-    if q.dim() != 3:
-        raise ValueError("q must be tokens x heads x head size")
-    m, heads, d = q.shape
-    if table is not None and (table.dim() != 3 or table.shape[1] != 2 or table.dtype != torch.float32 or
-                              not table.is_contiguous() or not table.is_cuda):
-        raise ValueError("table must come from loract_rope_table (positions x 2 x rot / 2, float32)")
-    if positions is not None and (positions.shape != (m,) or positions.dtype != torch.int32 or
+def _qk_call(q, k, gamma_q, gamma_k, table, positions, eps, interleaved, q_out, k_out, dq, dk):
+    """Parameters of a call (dq, dk: the gradients of the forward's outputs, or None)."""
+    if q.dim() != 3 or (k is not None and k.dim() != 3):
+        raise ValueError("q and k must be tokens x heads x head size")
+    m, hq, d = q.shape
+    dt = q.dtype
+    hk = 0 if k is None else k.shape[1]
+    n_pos, rot = 0, 0
+    if table is not None:
+        if table.dim() != 3 or table.shape[1] != 2 or table.dtype is not torch.float32 or not table.is_contiguous() or not table.is_cuda:
+            raise ValueError("table must come from loract_rope_table (positions x 2 x rot / 2, float32)")
+        n_pos, rot = table.shape[0], 2 * table.shape[2]
+    if positions is not None and (positions.shape != (m,) or positions.dtype is not torch.int32 or
                                   not positions.is_contiguous() or not positions.is_cuda):
         raise ValueError("positions must be a contiguous int32 GPU tensor with one entry per token")
-    p = LoractQkParams(m=m, heads_q=heads, heads_k=0 if k is None else k.shape[1], d=d, rot=0 if table is None else 2 * table.shape[2],
-                       interleaved=int(interleaved), dtype=_dtype_code(q.dtype), n_pos=0 if table is None else table.shape[0],
-                       eps=float(eps))
-    p.q_token, p.q_head = _heads(q, m, d, q.dtype, "q")
-    if k is not None:
-        p.k_token, p.k_head = _heads(k, m, d, q.dtype, "k")
-    return p
+    strides = _heads(q, m, hq, d, dt, "q")
+    strides += (0, 0) if k is None else _heads(k, m, hk, d, dt, "k")
+    strides += (hq * d, d) if q_out is None else _heads(q_out, m, hq, d, dt, "out")
+    strides += (hk * d, d) if k_out is None else _heads(k_out, m, hk, d, dt, "out")
+    strides += (0, 0) if dq is None else _heads(dq, m, hq, d, dt, "dq_out")
+    strides += (0, 0) if dk is None else _heads(dk, m, hk, d, dt, "dk_out")
+    params = _QK_PARAMS.pack(m, hq, hk, d, rot, 1 if interleaved else 0, _dtype_code(dt), n_pos, eps, *strides)
+    return params, _floats(gamma_q, d, "gamma_q"), None if k is None else _floats(gamma_k, d, "gamma_k")
 
 
 def loract_qknorm_rope_forward(q: torch.Tensor, k: Optional[torch.Tensor], gamma_q: Optional[torch.Tensor],
@@ -505,22 +535,17 @@ def loract_qknorm_rope_forward(q: torch.Tensor, k: Optional[torch.Tensor], gamma
     """Rot(x / rms(x) * gamma) of every head of q and k (tokens x heads x d, any token and head stride: slices of a packed
     projection will do).  table from loract_rope_table (None: no rotation); positions int32, negative for padding, None for
     the token's index.  out = (q, k) works in place."""
-    p = _qk_params(q, k, table, positions, eps, interleaved)
-    m, heads, d = q.shape
-    gq, gk = _floats(gamma_q, d, "gamma_q"), _floats(gamma_k, d, "gamma_k")
+    qo, ko = (None, None) if out is None else (out[0], None if k is None else out[1])
+    if out is not None and (qo is None or (k is not None and ko is None)):
+        raise ValueError("out must hold a tensor for q and one for k")
+    params, gq, gk = _qk_call(q, k, gamma_q, gamma_k, table, positions, eps, interleaved, qo, ko, None, None)
     if out is None:
-        qo = torch.empty((m, heads, d), dtype=q.dtype, device=q.device)
-        ko = None if k is None else torch.empty(tuple(k.shape), dtype=q.dtype, device=q.device)
-    else:
-        qo, ko = out if k is not None else (out[0], None)
-        if qo.shape != q.shape or (k is not None and (ko is None or ko.shape != k.shape)):
-            raise ValueError("out must have the shapes of q and k")
-    p.qo_token, p.qo_head = _heads(qo, m, d, q.dtype, "out")
-    if k is not None:
-        p.ko_token, p.ko_head = _heads(ko, m, d, q.dtype, "out")
-    if m:
-        _check(_lib.load().loract_qknorm_rope_forward(q.data_ptr(), _ptr(k), ctypes.byref(p), gq, gk, _ptr(table), _ptr(positions),
-                                                      qo.data_ptr(), _ptr(ko), _stream_ptr()), "loract_qknorm_rope_forward")
+        qo, ko = q.new_empty(q.shape), None if k is None else q.new_empty(k.shape)
+    if q.shape[0]:
+        code = _lib.load().loract_qknorm_rope_forward(q.data_ptr(), _ptr(k), params, gq, gk, _ptr(table), _ptr(positions),
+                                                      qo.data_ptr(), _ptr(ko), _stream_ptr())
+        if code:
+            raise LoractError(code, "loract_qknorm_rope_forward")
     return qo, ko
 
 
@@ -530,36 +555,26 @@ def loract_qknorm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], gamm
                                 interleaved: bool = False, out: Optional[Tuple[torch.Tensor, Optional[torch.Tensor]]] = None):
     """(dq, dk, dgamma_q, dgamma_k) from the forward's inputs and the gradients of its outputs; the gammas' gradients are
     float32, None where the gamma is.  out = (dq, dk) may be (dq_out, dk_out) or slices of a packed gradient."""
-    p = _qk_params(q, k, table, positions, eps, interleaved)
-    m, heads, d = q.shape
-    gq, gk = _floats(gamma_q, d, "gamma_q"), _floats(gamma_k, d, "gamma_k")
+    dq, dk = (None, None) if out is None else (out[0], None if k is None else out[1])
+    if dq_out is None or (k is not None and dk_out is None) or (out is not None and (dq is None or (k is not None and dk is None))):
+        raise ValueError("gradients must have the shapes of q and k")
+    dk_out = None if k is None else dk_out
+    params, gq, gk = _qk_call(q, k, gamma_q, gamma_k, table, positions, eps, interleaved, dq, dk, dq_out, dk_out)
     if out is None:
-        dq = torch.empty((m, heads, d), dtype=q.dtype, device=q.device)
-        dk = None if k is None else torch.empty(tuple(k.shape), dtype=q.dtype, device=q.device)
-    else:
-        dq, dk = out if k is not None else (out[0], None)
-    for grad, of in ((dq_out, q), (dq, q)) + (() if k is None else ((dk_out, k), (dk, k))):
-        if grad is None or grad.shape != of.shape:
-            raise ValueError("gradients must have the shapes of q and k")
-    p.qo_token, p.qo_head = _heads(dq, m, d, q.dtype, "out")
-    p.dq_token, p.dq_head = _heads(dq_out, m, d, q.dtype, "dq_out")
-    if k is not None:
-        p.ko_token, p.ko_head = _heads(dk, m, d, q.dtype, "out")
-        p.dk_token, p.dk_head = _heads(dk_out, m, d, q.dtype, "dk_out")
-    dgq = None if gamma_q is None else torch.empty((d,), dtype=torch.float32, device=q.device)
-    dgk = None if gamma_k is None or k is None else torch.empty((d,), dtype=torch.float32, device=q.device)
-    if m == 0:
+        dq, dk = q.new_empty(q.shape), None if k is None else q.new_empty(k.shape)
+    d = q.shape[2]
+    dgq = None if gq is None else q.new_empty((d,), dtype=torch.float32)
+    dgk = None if gk is None else q.new_empty((d,), dtype=torch.float32)
+    if q.shape[0] == 0:
         return dq, dk, dgq if dgq is None else dgq.zero_(), dgk if dgk is None else dgk.zero_()
-    lib = _lib.load()
-    ws = None
+    lib, stream = _lib.load(), _stream_ptr()
+    ws, size = None, 0
     if dgq is not None or dgk is not None:
-        nbytes = ctypes.c_size_t(0)
-        _check(lib.loract_qknorm_rope_workspace_bytes(ctypes.byref(p), ctypes.byref(nbytes)), "loract_qknorm_rope_workspace_bytes")
-        ws = _workspace(int(nbytes.value), q.device)
-    _check(lib.loract_qknorm_rope_backward(q.data_ptr(), _ptr(k), ctypes.byref(p), gq, gk, _ptr(table), _ptr(positions),
-                                           dq_out.data_ptr(), _ptr(dk_out) if k is not None else None, dq.data_ptr(), _ptr(dk),
-                                           _ptr(dgq), _ptr(dgk), _ptr(ws), 0 if ws is None else ws.numel(), _stream_ptr()),
-           "loract_qknorm_rope_backward")
+        ws, size = _scratch(lib.loract_qknorm_rope_workspace_bytes, "loract_qknorm_rope_workspace_bytes", params, q, stream)
+    code = lib.loract_qknorm_rope_backward(q.data_ptr(), _ptr(k), params, gq, gk, _ptr(table), _ptr(positions), dq_out.data_ptr(),
+                                           _ptr(dk_out), dq.data_ptr(), _ptr(dk), _ptr(dgq), _ptr(dgk), ws, size, stream)
+    if code:
+        raise LoractError(code, "loract_qknorm_rope_backward")
     return dq, dk, dgq, dgk
 
 

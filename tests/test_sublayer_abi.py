@@ -26,6 +26,14 @@ def test_parameter_structures_match_the_header(tmp_path):
     assert got == want
 
 
+def test_packed_parameters_are_the_structures():
+    from paper_2509_23472_amd import api
+    values = list(range(1, 15)) + [0.5, 0.25, 2 ** 64 - 3]
+    assert api._LINEAR_PARAMS.pack(*values) == bytes(LoractLinearParams(*values))
+    values = list(range(1, 9)) + [0.5] + list(range(20, 32))
+    assert api._QK_PARAMS.pack(*values) == bytes(LoractQkParams(*values))
+
+
 def _linear(**kw):
     base = dict(m=64, n_in=32, n_out=48, ldx=32, ldw=32, ldr=48, ldy=48, ldz=48, ldp=48, dtype=1, out_dtype=1, w_layout=0, act=0, r_lora=0,
                 lora_scale=1.0, p_drop=0.0, seed=0)
