@@ -23,24 +23,32 @@ struct LinBackArgs {
   int64_t m, n;
   int act;
   int64_t chunk;         // rows per workgroup
-  float* part;           // [chunk][1 + 16 RB][strips * 16 E]; null: no sums
+  float* part;           // [chunk][1 + 16 RB][columns of all strips]; null: no sums
   int64_t n_pad;
   DropArgs d;
 };
 
 #define LB_WAVES 4
 
-// VEC: rows allow 16-byte pieces.  RB: blocks of 16 columns of T (0: the bias gradient alone, or nothing).
+// Columns per lane: 16 bytes' worth; 8 for bf16 with more than 32 columns of T, whose accumulators would leave room for one wave
+// per SIMD.
+constexpr int lb_columns(int size, int rb) { return size == 2 && rb <= 2 ? 8 : 4; }
+
+// VEC: rows allow pieces of lb_columns elements.  RB: blocks of 16 columns of T (0: the bias gradient alone, or nothing).  The
+// i-th row of the products' block b stands for column RB i + b of T, so that a lane's RB values of T lie together.
 template <typename T, bool VEC, int RB>
 __global__ __launch_bounds__(64 * LB_WAVES) void linear_backward_kernel(LinBackArgs g) {
-  constexpr int E = 16 / sizeof(T), U = 2;
+  constexpr int E = lb_columns(sizeof(T), RB), U = E == 4 && sizeof(T) == 2 ? 4 : 2;
+  constexpr bool FAST = sizeof(T) == 2;
   typedef T piece __attribute__((ext_vector_type(E)));
+  typedef T t_piece __attribute__((ext_vector_type(RB ? RB : 1)));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = lane & 15, k = lane >> 4;
   const int64_t col = (int64_t)blockIdx.x * (16 * E) + c * E;
   const int64_t r_beg = (int64_t)blockIdx.y * g.chunk;
   const int64_t r_end = r_beg + g.chunk < g.m ? r_beg + g.chunk : g.m;
   const bool on = col < g.n;
+  const bool t_vec = g.r == 16 * RB && RB != 3 && (uintptr_t)g.T % (RB * sizeof(T) + (RB == 0)) == 0;
   float sum[E];
   f32x4 acc[RB ? RB : 1][E];
 #pragma unroll
@@ -51,7 +59,7 @@ __global__ __launch_bounds__(64 * LB_WAVES) void linear_backward_kernel(LinBackA
   }
   for (int64_t r0 = r_beg + wave * (4 * U); r0 < r_end; r0 += LB_WAVES * 4 * U) {
     T y[U][E], z[U][E];
-    float tv[U][RB ? RB : 1];
+    float tv[U][RB ? RB : 1], p[U][E];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t row = r0 + 4 * u + k;
@@ -73,30 +81,58 @@ __global__ __launch_bounds__(64 * LB_WAVES) void linear_backward_kernel(LinBackA
             }
         }
       }
+      if (RB) {
+        const T* tp = (const T*)g.T + row * g.r + RB * c;
 #pragma unroll
-      for (int b = 0; b < RB; ++b)
-        tv[u][b] = row < r_end && 16 * b + c < g.r ? (float)((const T*)g.T)[row * g.r + 16 * b + c] : 0.0f;
+        for (int b = 0; b < RB; ++b) tv[u][b] = 0.0f;
+        if (row < r_end) {
+          if (t_vec) {
+            const t_piece t = *(const t_piece*)tp;
+#pragma unroll
+            for (int b = 0; b < RB; ++b) tv[u][b] = (float)t[b];
+          } else {
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+              if (RB * c + b < g.r) tv[u][b] = (float)tp[b];
+          }
+        }
+      }
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < E; ++e) p[u][e] = (float)y[u][e];
+    if (g.d.thr) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < E / 4; ++q) {
+          const uint64_t word = drop_word(g.d, r0 + 4 * u + k, col / 4 + q);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[u][4 * q + e] = drop_one(g.d, word, e, p[u][4 * q + e]);
+        }
+    }
+    // (one choice for all of them)
+    auto slopes = [&](int act) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < E; ++e) p[u][e] *= lin_act_slope<FAST>(act, (float)z[u][e]);
+    };
+    if (g.act == LORACT_ACT_RELU) slopes(LORACT_ACT_RELU);
+    else if (g.act == LORACT_ACT_GELU) slopes(LORACT_ACT_GELU);
+    else if (g.act == LORACT_ACT_SILU) slopes(LORACT_ACT_SILU);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t row = r0 + 4 * u + k;
-      const bool live = on && row < r_end;
-      float p[E];
       T o[E];
 #pragma unroll
-      for (int q = 0; q < E / 4; ++q) {
-        const uint64_t word = g.d.thr ? drop_word(g.d, row, col / 4 + q) : 0;
-#pragma unroll
-        for (int e = 4 * q; e < 4 * q + 4; ++e) {
-          float v = (float)y[u][e];
-          if (g.d.thr) v = drop_one(g.d, word, e & 3, v);
-          if (g.Z) v *= lin_act_slope<sizeof(T) == 2>(g.act, (float)z[u][e]);
-          p[e] = v;
-          o[e] = (T)v;
-          sum[e] += v;
-        }
+      for (int e = 0; e < E; ++e) {
+        if (row >= r_end) p[u][e] = 0.0f;            // (the slope of a zero need not be finite times zero)
+        o[e] = (T)p[u][e];
+        sum[e] += p[u][e];
       }
-      if (live) {
+      if (on && row < r_end) {
         T* dp = (T*)g.dP + row * g.lddp + col;
         if (VEC) {
           *(piece*)dp = *(const piece*)o;
@@ -109,7 +145,7 @@ __global__ __launch_bounds__(64 * LB_WAVES) void linear_backward_kernel(LinBackA
 #pragma unroll
       for (int b = 0; b < RB; ++b)
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(tv[u][b], p[e], acc[b][e], 0, 0, 0);
+        for (int e = 0; e < E; ++e) acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(tv[u][b], p[u][e], acc[b][e], 0, 0, 0);
     }
   }
   if (!g.part) return;
@@ -129,7 +165,7 @@ __global__ __launch_bounds__(64 * LB_WAVES) void linear_backward_kernel(LinBackA
         for (int b = 0; b < RB; ++b)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            float* at = &red[1 + 16 * b + 4 * k + q][c * E + e];
+            float* at = &red[1 + RB * (4 * k + q) + b][c * E + e];
             *at = (w ? *at : 0.0f) + acc[b][e][q];
           }
       }
@@ -150,12 +186,12 @@ __global__ __launch_bounds__(256) void linear_backward_join_kernel(const float* 
   const float* src = part + row * n_pad + i;
   const int64_t step = rows * n_pad;
   float s = 0.0f;
-  for (int z = 0; z < chunks; z += 8) {
-    float v[8];
+  for (int z = 0; z < chunks; z += 16) {
+    float v[16];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = src[(z + u < chunks ? z + u : chunks - 1) * step];
+    for (int u = 0; u < 16; ++u) v[u] = src[(z + u < chunks ? z + u : chunks - 1) * step];
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
+    for (int u = 0; u < 16; ++u)
       if (z + u < chunks) s += v[u];
   }
   if (row == 0) { if (db) db[i] = s; }
@@ -167,14 +203,14 @@ struct LinBackPlan {
   int rb;
   size_t bytes;
 };
-// Rows are cut so that there are eight workgroups per CU, 64 rows each at least.
+// Rows are cut so that there are four workgroups per CU, 64 rows each at least.
 static LinBackPlan linear_backward_plan(int64_t m, int64_t n, int64_t r, bool bf16) {
   LinBackPlan p;
-  const int width = bf16 ? 128 : 64;
-  p.strips = ceil_div64(n, width);
   p.rb = (int)ceil_div64(r, 16);
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2048 / p.strips, ceil_div64(m, 64)));
-  p.chunk = ceil_div64(ceil_div64(m, want), 32) * 32;
+  const int width = 16 * lb_columns(bf16 ? 2 : 4, p.rb);
+  p.strips = ceil_div64(n, width);
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(1, 1024 / p.strips), ceil_div64(m, 64)));
+  p.chunk = ceil_div64(ceil_div64(m, want), 64) * 64;
   p.chunks = ceil_div64(m, p.chunk);
   p.n_pad = p.strips * width;
   p.bytes = (size_t)p.chunks * (1 + 16 * p.rb) * p.n_pad * 4;

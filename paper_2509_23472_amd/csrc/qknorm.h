@@ -282,8 +282,8 @@ __global__ __launch_bounds__(64 * QK_WAVES) void qknorm_rope_any_kernel(QkArgs g
   }
 }
 
-// dgamma of both streams (blockIdx.x) from the workgroups' partial sums: 16 threads share an element's partial sums, each takes every
-// 16th in order, and their sums are added in order.
+// dgamma of both streams (blockIdx.x) from the workgroups' partial sums.  Sixteen elements per workgroup, 64 threads to each of
+// them: a thread takes every 64th partial sum in order, sixteen of them in flight, then 64 sums are added pair by pair.
 struct QkJoin {
   const float* part[2];
   int blocks[2];
@@ -291,17 +291,26 @@ struct QkJoin {
   int d, d_pad;
 };
 __global__ __launch_bounds__(1024) void qknorm_join_kernel(QkJoin g) {
-  __shared__ float red[16][64];
-  const int which = blockIdx.x, i = blockIdx.y * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+  __shared__ float red[64][17];
+  const int which = blockIdx.x, c = threadIdx.x & 15, i = blockIdx.y * 16 + c, w = threadIdx.x >> 4;
   if (!g.out[which]) return;
+  const float* src = g.part[which] + i;              // (rows are padded past d)
+  const int blocks = g.blocks[which];
   float s = 0.0f;
-  if (i < g.d)
-    for (int b = w; b < g.blocks[which]; b += 16) s += g.part[which][(int64_t)b * g.d_pad + i];
-  red[w][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (w || i >= g.d) return;
-  for (int j = 1; j < 16; ++j) s += red[j][threadIdx.x];
-  g.out[which][i] = s;
+  for (int b0 = w; b0 < blocks; b0 += 1024) {
+    float v[16];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) v[u] = src[(int64_t)(b0 + 64 * u < blocks ? b0 + 64 * u : b0) * g.d_pad];
+#pragma unroll
+    for (int u = 0; u < 16; ++u)
+      if (b0 + 64 * u < blocks) s += v[u];
+  }
+  red[w][c] = s;
+  for (int h = 32; h > 0; h >>= 1) {
+    __syncthreads();
+    if (w < h) red[w][c] += red[w + h][c];
+  }
+  if (w == 0 && i < g.d) g.out[which][i] = red[0][c];
 }
 
 // cos and sin of position * theta^(-2 i / rot), the angle in float64.

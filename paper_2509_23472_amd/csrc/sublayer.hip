@@ -4,6 +4,7 @@
 #include "dropout.h"
 #include "linear_backward.h"
 #include "linear_large.h"
+#include "linear_thin.h"
 #include "linear_tile.h"
 #include "qknorm.h"
 
@@ -53,7 +54,9 @@ int loract_linear_workspace_bytes(const loract_linear_params* p, size_t* bytes) 
   LORACT_TRY(check_linear_forward(p));
   const bool bf16 = p->dtype == LORACT_BF16;
   *bytes = align_up(linear_tile_part_bytes(p->m, p->n_out, p->n_in, bf16), 256);
-  if (bf16 && linear_large_pays(p->m, p->n_out, p->n_in))            // whichever the call's alignment allows
+  // (whichever form the call's alignment allows)
+  if (bf16) *bytes = std::max(*bytes, align_up(linear_thin_part_bytes(p->m, p->n_out, p->n_in, p->w_layout == LORACT_W_OUT_IN), 256));
+  if (bf16 && linear_large_pays(p->m, p->n_out, p->n_in))
     *bytes = std::max(*bytes, linear_large_ws_bytes(p->m, p->n_out, p->r_lora));
   return LORACT_OK;
 }
@@ -81,6 +84,7 @@ int loract_linear(const void* X_dev, const void* W_dev, const float* bias_dev, c
   const size_t quad = bf16 ? 8 : 16;
   e.vec = p->n_out % 4 == 0 && aligned_rows(R_dev, p->ldr, 4, quad) && aligned_rows(Z_dev, p->ldz, 4, quad) &&
           aligned_rows(Y_dev, p->ldy, 4, e.y_f32 ? 16 : 8);
+  if (bf16 && linear_thin_form(g.m, g.n, g.k, w_kc) && linear_thin_fits(g)) return launch_linear_thin((hipStream_t)stream, g, w_kc);
   if (bf16 && linear_large_pays(g.m, g.n, g.k) && linear_large_fits(g, w_kc)) return launch_linear_large((hipStream_t)stream, g, w_kc);
   return bf16 ? launch_linear_tile<bf16_t>((hipStream_t)stream, g, w_kc) : launch_linear_tile<float>((hipStream_t)stream, g, w_kc);
 }
@@ -203,7 +207,7 @@ int loract_qknorm_rope_backward(const void* q_dev, const void* k_dev, const lora
   QkJoin j;
   j.part[0] = g.q.part; j.part[1] = g.k.part; j.blocks[0] = plan.q_blocks; j.blocks[1] = plan.k_blocks;
   j.out[0] = dgamma_q_dev; j.out[1] = dgamma_k_dev; j.d = p->d; j.d_pad = plan.d_pad;
-  LORACT_LAUNCH("qknorm_rope_join", (hipStream_t)stream, qknorm_join_kernel, dim3(2, (unsigned)(plan.d_pad / 64)), dim3(1024), 0, j);
+  LORACT_LAUNCH("qknorm_rope_join", (hipStream_t)stream, qknorm_join_kernel, dim3(2, (unsigned)(plan.d_pad / 16)), dim3(1024), 0, j);
   return LORACT_OK;
 }
 

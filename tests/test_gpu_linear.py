@@ -79,6 +79,19 @@ def test_large_tiles(m, n_in, n_out, parts, layout):
     _case(m, n_in, n_out, layout=layout, **parts)
 
 
+# few tokens, few outputs: K that fills no wave's share, one and two blocks of 16, several workgroups along K
+@pytest.mark.parametrize("layout", ["nt", "nn"])
+@pytest.mark.parametrize("m,n_in,n_out,parts", [
+    (1, 8, 8, dict()), (1, 40, 24, dict(r=3)), (1, 4104, 136, dict(r=64, act="silu", bias=True, keep=True)), (7, 2048, 264, dict(r=33, residual=True)),
+    (16, 264, 1000, dict(p=0.2, act="gelu")), (17, 1032, 520, dict(r=16, keep=True)), (32, 72, 4096, dict(r=8, residual=True, p=0.1)),
+    (32, 11008, 40, dict(out_dtype="f32", act="relu")), (5, 8200, 64, dict(residual=True, keep=True, r=40)), (2, 32, 5, dict()),
+    (300, 264, 16, dict(r=16)), (300, 8, 64, dict(residual=True)), (333, 2056, 8, dict(act="silu", bias=True)), (9000, 104, 16, dict(r=7, p=0.1)),
+    (8200, 256, 48, dict(keep=True, act="gelu", r=64)), (100, 4096, 33, dict(bias=True)), (70, 8192, 24, dict(pad=8, shift=8, residual=True)),
+    (4, 512, 128, dict(pad=16, shift=8, r=12, act="silu", keep=True))])
+def test_thin_products(m, n_in, n_out, parts, layout):
+    _case(m, n_in, n_out, layout=layout, **parts)
+
+
 def test_large_tiles_keep_nan_and_infinity_where_they_belong():
     for layout in ("nt", "nn"):
         def poison(x, w):
