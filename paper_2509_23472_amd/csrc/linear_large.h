@@ -1,8 +1,8 @@
-// P = X W^T + s T B for large bf16 maps: tiles of 256 x 256 on v_mfma_f32_16x16x32_bf16.
+// P = X W^T + s T B for bf16 maps whose rows are 16-byte pieces: tiles of 256 x 256 or 128 x 128 on v_mfma_f32_16x16x32_bf16.
 //
 // Slabs of 64 of K -- whole 128-byte lines of X and of W -- go from memory straight into LDS (asynchronous copies): three stages for
-// X, fetched up to three slabs ahead, and two for W, 160 KB in all.  A stage holds 256 rows as [row][64] or, for W stored
-// n_in x n_out, 64 rows of it as they lie ([k][256], read with the transposing LDS read).  A wave reads the fragments of the next 32 of K
+// X, fetched up to three slabs ahead, and two for W, 160 KB in all (80 KB for the smaller tiles, of which a CU holds two).  A
+// stage holds the tile's rows as [row][64] or, for W stored n_in x n_out, 64 rows of it as they lie ([k][columns], read with the transposing LDS read).  A wave reads the fragments of the next 32 of K
 // while it multiplies the present ones; there is one barrier per slab, behind the first products of its second half.
 #pragma once
 #include "linear_tile.h"
@@ -10,8 +10,6 @@
 #include <type_traits>
 
 #define LL_BK 64
-#define LL_WAVES 8
-#define LL_STAGE (256 * LL_BK * 2)    // bytes of one operand's slab
 #define LL_X_STAGES 3
 #define LL_W_STAGES 2
 
@@ -28,10 +26,11 @@ __device__ inline void ll_tile_of(int b, int tiles_m, int tiles_n, int* tm, int*
   *tm = band * LL_BAND + in - *tn * rows;
 }
 
+template <int PITCH>
 __device__ inline bf16x8 ll_read_tr(const unsigned char* lds, int off) {
   typedef __attribute__((address_space(3))) gb_s16x4* lds_ptr;
   const gb_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds + off));
-  const gb_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds + off + 4 * 512));
+  const gb_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds + off + 4 * PITCH));
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 // Where the 16-byte chunks of a row lie: chunk c of row r (along K) at c ^ ll_turn(r), chunk c of row k of W as it lies at
@@ -40,26 +39,33 @@ __device__ inline bf16x8 ll_read_tr(const unsigned char* lds, int off) {
 __device__ inline int ll_turn(int r) { return (r >> 1) & 7; }
 __device__ inline int ll_turn_k(int k) { return 4 * (k & 3) + ((k >> 2) & 2); }
 
-template <bool WKC>
-__global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearArgs g, int tiles_m, int tiles_n) {
-  constexpr int MT = 8, NT = 4, C = 32 / LL_WAVES;       // a wave: 8 x 4 products of 16 x 16; copies per operand and slab
-  __shared__ __attribute__((aligned(16))) unsigned char smem[(LL_X_STAGES + LL_W_STAGES) * LL_STAGE];
-  unsigned char* const smem_w = smem + LL_X_STAGES * LL_STAGE;
+// Waves of a tile (TILE / 2 x 64 each), in two rows.
+constexpr int ll_waves(int tile) { return tile / 32; }
+
+// blockIdx.x: tile, blockIdx.y: split of K.
+template <bool WKC, int TILE>
+__global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void linear_large_kernel(LinearArgs g, int tiles_m, int tiles_n) {
+  constexpr int WAVES = ll_waves(TILE), WN = TILE / 64, MT = TILE / 32, NT = 4;      // a wave: MT x NT products of 16 x 16
+  constexpr int C = TILE / 8 / WAVES;                    // copies of 1 KB per operand and slab
+  constexpr int STAGE = TILE * LL_BK * 2, PITCH = TILE * 2, LPK = PITCH / 16, KPC = 64 / LPK;      // W as it lies: lanes to a row, rows to a copy
+  __shared__ __attribute__((aligned(16))) unsigned char smem[(LL_X_STAGES + LL_W_STAGES) * STAGE];
+  unsigned char* const smem_w = smem + LL_X_STAGES * STAGE;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int wm = wave >> 2, wn = wave & 3;
+  const int wm = wave / WN, wn = wave % WN;
   int tm, tn;
   ll_tile_of(blockIdx.x, tiles_m, tiles_n, &tm, &tn);
-  const int64_t row0 = (int64_t)tm * 256, col0 = (int64_t)tn * 256;
-  const int k_len = (int)g.k, full = k_len / LL_BK, nslab = (k_len + LL_BK - 1) / LL_BK;
+  const int64_t row0 = (int64_t)tm * TILE, col0 = (int64_t)tn * TILE;
+  const int64_t k_beg = (int64_t)blockIdx.y * g.k_per_split;
+  const int k_len = (int)(k_beg + g.k_per_split < g.k ? g.k_per_split : g.k - k_beg), full = k_len / LL_BK, nslab = (k_len + LL_BK - 1) / LL_BK;
 
-  const char* const xb = (const char*)((const bf16_t*)g.X + row0 * g.ldx);
-  const char* const wb = (const char*)((const bf16_t*)g.W + (WKC ? col0 * g.ldw : col0));
+  const char* const xb = (const char*)((const bf16_t*)g.X + row0 * g.ldx + k_beg);
+  const char* const wb = (const char*)((const bf16_t*)g.W + (WKC ? col0 * g.ldw + k_beg : col0 + k_beg * g.ldw));
   const int64_t w_step = WKC ? 2 * LL_BK : 2 * LL_BK * g.ldw;
-  // copy c of a wave: 8 rows of 128 bytes along K, or two rows of 512 bytes of W as it lies
-  const int copy_row = 8 * wave * C + (lane >> 3), copy_k = 2 * wave * C + (lane >> 5);
+  // copy c of a wave: 8 rows of 128 bytes along K, or KPC whole rows of W as it lies
+  const int copy_row = 8 * wave * C + (lane >> 3), copy_k = KPC * wave * C + lane / LPK;
   auto chunk_of = [&](int c) { return (lane & 7) ^ ll_turn(copy_row + 8 * c); };
   auto col_of = [&](int c) {
-    const int64_t col = ((lane & 31) ^ ll_turn_k(copy_k + 2 * c)) * 8;
+    const int64_t col = ((lane % LPK) ^ ll_turn_k(copy_k + KPC * c)) * 8;
     return col0 + col < g.n ? col : g.n - 8 - col0;                         // columns past the end are never stored
   };
   unsigned xo[C], wo[C];
@@ -72,13 +78,13 @@ __global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearAr
       const int64_t wr = col0 + row < g.n ? row : g.n - 1 - col0;
       wo[c] = (unsigned)(wr * g.ldw * 2) + chunk_of(c) * 16;
     } else {
-      wo[c] = (unsigned)((copy_k + 2 * c) * g.ldw * 2) + (unsigned)col_of(c) * 2;
+      wo[c] = (unsigned)((copy_k + KPC * c) * g.ldw * 2) + (unsigned)col_of(c) * 2;
     }
   }
   // Slabs are numbered through: the one of T and B, if there is a low-rank term, then those of X and W.
-  const int r = g.T ? (int)g.r : 0, nlr = r ? 1 : 0, slabs = nlr + nslab;
-  auto x_stage = [&](int v) { return smem + v % LL_X_STAGES * LL_STAGE; };
-  auto w_stage = [&](int v) { return smem_w + v % LL_W_STAGES * LL_STAGE; };
+  const int r = g.T && blockIdx.y == 0 ? (int)g.r : 0, nlr = r ? 1 : 0, slabs = nlr + nslab;
+  auto x_stage = [&](int v) { return smem + v % LL_X_STAGES * STAGE; };
+  auto w_stage = [&](int v) { return smem_w + v % LL_W_STAGES * STAGE; };
   auto copy_x = [&](int v) {
     unsigned char* const st = x_stage(v) + wave * (C * 1024);
     if (v >= slabs) v = slabs - 1;                                         // (never multiplied)
@@ -103,7 +109,7 @@ __global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearAr
     const char* const ws = wb + (v - nlr) * w_step;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int kr = copy_k + 2 * c, chunk = chunk_of(c);
+      const int kr = copy_k + KPC * c, chunk = chunk_of(c);
       if (v < nlr)
         sb_async16((const bf16_t*)g.B + (int64_t)(kr < left ? kr : left - 1) * g.n + col0 + col_of(c), st + c * 1024);
       else if (WKC)
@@ -115,17 +121,17 @@ __global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearAr
 
   // fragments: 16 rows (columns), lane l holds row l % 16 and the eight k from 8 (l / 16) on of a half slab
   const int k_off[2] = {((lane >> 4) ^ ll_turn(lane & 15)) << 4, ((4 + (lane >> 4)) ^ ll_turn(lane & 15)) << 4};
-  const int xr_off = (wm * 128 + (lane & 15)) * 128, wr_off = (wn * 64 + (lane & 15)) * 128;
+  const int xr_off = (wm * (TILE / 2) + (lane & 15)) * 128, wr_off = (wn * 64 + (lane & 15)) * 128;
   int tr_off[NT];
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     const int s16 = lane & 15, kr = 8 * (lane >> 4) + (s16 >> 2), c = wn * 64 + 16 * j + 4 * (s16 & 3);
-    tr_off[j] = kr * 512 + (((c >> 3) ^ ll_turn_k(kr)) << 4) + (c & 7) * 2;
+    tr_off[j] = kr * PITCH + (((c >> 3) ^ ll_turn_k(kr)) << 4) + (c & 7) * 2;
   }
   bf16x8 x[2][MT], w[2][NT];
   // fragment f of half h of a slab: those of W, then those of X
   auto read_one = [&](const unsigned char* xs, const unsigned char* ws, int h, bool w_kc, int f) {
-    if (f < NT) w[h][f] = w_kc ? *(const bf16x8*)(ws + wr_off + k_off[h] + f * 2048) : ll_read_tr(ws, tr_off[f] + h * (32 * 512));
+    if (f < NT) w[h][f] = w_kc ? *(const bf16x8*)(ws + wr_off + k_off[h] + f * 2048) : ll_read_tr<PITCH>(ws, tr_off[f] + h * (32 * PITCH));
     else x[h][f - NT] = *(const bf16x8*)(xs + xr_off + k_off[h] + (f - NT) * 2048);
   };
   auto read = [&](int v, int h, bool w_kc) {
@@ -186,7 +192,7 @@ __global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearAr
 #pragma unroll
     for (int u = 0; u < MT * NT; ++u) {
       acc[u / NT][u % NT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[0][u % NT], x[0][u / NT], acc[u / NT][u % NT], 0, 0, 0);
-      if (u < 2 * (MT + NT) && u % 2 == 0) read_one(xs, ws, 1, WKC, u / 2);
+      if (u % 2 == 0 && u / 2 < MT + NT) read_one(xs, ws, 1, WKC, u / 2);
       __builtin_amdgcn_sched_barrier(0);
     }
     xs = x_stage(v + 1);
@@ -202,9 +208,10 @@ __global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearAr
         SB_WAIT_VMCNT(C);              // slab v + 1 has landed (behind it: X of slab v + 2); everyone has read slab v
         sb_barrier_lds();
       }
-      if (u >= 4 && u < 4 + 2 * (MT + NT) && u % 2 == 0) read_one(xs, ws, 0, WKC, (u - 4) / 2);
-      if (u >= 4 && u < 4 + 3 * 2 * C && u % 3 == 1) {
-        const int c = (u - 4) / 3;
+      constexpr int RS = TILE == 256 ? 2 : 1, CS = TILE == 256 ? 3 : 1;      // products from one read or copy to the next
+      if (u >= 4 && (u - 4) % RS == 0 && (u - 4) / RS < MT + NT) read_one(xs, ws, 0, WKC, (u - 4) / RS);
+      if (u >= 4 && (u - 4) % CS == 0 && (u - 4) / CS < 2 * C) {
+        const int c = (u - 4) / CS;
         if (c < C) sb_async16_at(w_src, wo[c % C], w_dst + (c % C) * 1024);
         else sb_async16_at(x_src, xo[c % C], x_dst + (c % C) * 1024);
       }
@@ -241,15 +248,15 @@ __global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearAr
   float* const cs = (float*)(smem + wave * (32 * LDC * 4));
   const int c8 = (lane % LPR) * 8, r8 = lane / LPR;
   const int64_t col = col0 + wn * PART + c8;
-  const bool in = col < g.n;
+  const bool in = col < g.n, split = gridDim.y > 1;
   float bias[8];
 #pragma unroll
-  for (int u = 0; u < 8; ++u) bias[u] = e.bias && in ? e.bias[col + u] : 0.0f;
+  for (int u = 0; u < 8; ++u) bias[u] = e.bias && in && !split ? e.bias[col + u] : 0.0f;
 #pragma unroll
   for (int i = 0; i < MT; i += 2) {
-    const int64_t row = row0 + wm * 128 + 16 * i + r8;
+    const int64_t row = row0 + wm * (TILE / 2) + 16 * i + r8;
     bf16x8 res[N8];
-    if (e.R) {
+    if (e.R && !split) {
 #pragma unroll
       for (int q = 0; q < N8; ++q) {
         const int64_t at = row + ROWS * q < g.m ? row + ROWS * q : g.m - 1;
@@ -272,6 +279,16 @@ __global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearAr
       }
     }
     sb_wave_sync();
+    if (split) {
+#pragma unroll
+      for (int q = 0; q < N8; ++q) {
+        if (!in || row + ROWS * q >= g.m) continue;
+        float* out = g.part + ((int64_t)blockIdx.y * g.m + row + ROWS * q) * g.n_pad + col;
+        *(f32x4*)out = (f32x4){y[q][0], y[q][1], y[q][2], y[q][3]};
+        *(f32x4*)(out + 4) = (f32x4){y[q][4], y[q][5], y[q][6], y[q][7]};
+      }
+      continue;
+    }
     if (e.Z && in) {
 #pragma unroll
       for (int q = 0; q < N8; ++q) {
@@ -321,17 +338,35 @@ __global__ __launch_bounds__(64 * LL_WAVES, 1) void linear_large_kernel(LinearAr
   }
 }
 
-// What the tiles of 256 x 256 need: 16-byte pieces of everything, and 32 bits for the byte offsets within a tile.
+// What these tiles need: 16-byte pieces of everything, and 32 bits for the byte offsets within a tile.
 static bool linear_large_fits(const LinearArgs& g, bool w_kc) {
   auto rows = [](const void* p, int64_t ld) { return !p || ((uintptr_t)p % 16 == 0 && ld % 8 == 0); };
-  return g.k % 8 == 0 && g.n % 8 == 0 && rows(g.X, g.ldx) && rows(g.W, g.ldw) && rows(g.e.R, g.e.ldr) &&
-         rows(g.e.Y, g.e.ldy) && rows(g.e.Z, g.e.ldz) && g.ldx < (1 << 22) && g.ldw < (w_kc ? 1 << 22 : 1 << 25) &&
-         ceil_div64(g.m, 256) * ceil_div64(g.n, 256) < (1 << 24);
+  return g.k % 8 == 0 && g.n % 8 == 0 && rows(g.X, g.ldx) && rows(g.W, g.ldw) && rows(g.e.R, g.e.ldr) && rows(g.e.Y, g.e.ldy) &&
+         rows(g.e.Z, g.e.ldz) && g.ldx < (1 << 22) && g.ldw < (w_kc ? 1 << 22 : 1 << 24);
 }
-static bool linear_large_pays(int64_t m, int64_t n, int64_t k) {
-  return ceil_div64(m, 256) * ceil_div64(n, 256) >= 128 && m >= 192 && n >= 192 && k >= 128;
+// Tile (0: another form) and K splits.
+//
+// Costs in hundredths of a round of 256 tiles of 256 x 256, one per CU: a last round of few of them takes two thirds of one; 512
+// tiles of 128 x 128, two per CU, take 62 (a quarter of the work at 40 % of the rate: half the products per byte fetched), 256
+// 35.  Measured (256 / 128 x 128): 2048 x 2048 -> 2048 46 / 26 us, 8192 x 4096 -> 1024 92 / 70, 6000 x 4096 -> 3000 177 / 165, 2048 x
+// 4096 -> 11008 195 / 195, 5000 x 2048 -> 2048 48 / 52, 4096 x 4096 -> 4096 123 / 155, 8192 x 4096 -> 11008 619 / 725.
+// Where even the smaller tiles leave CUs without work, K is split in parts of at least 512: 256 x 4096 -> 4096 36 -> 24 us, 128 x
+// 11008 -> 4096 124 -> 33; more than one workgroup per CU loses to the join (2048 x 2048 -> 2048 26 -> 39).
+struct LargePlan {
+  int tile, splits;
+};
+static LargePlan linear_large_plan(int64_t m, int64_t n, int64_t k) {
+  LargePlan p = {0, 1};
+  if (m <= 64 || n <= 64 || k < 64) return p;
+  const int64_t t256 = ceil_div64(m, 256) * ceil_div64(n, 256), t128 = ceil_div64(m, 128) * ceil_div64(n, 128);
+  if (t128 >= 1 << 23) return p;
+  const int64_t last256 = t256 % 256, last128 = t128 % 512;
+  const int64_t cost256 = t256 / 256 * 100 + (last256 ? 66 + 34 * last256 / 256 : 0);
+  const int64_t cost128 = t128 / 512 * 62 + (last128 > 256 ? 60 : (last128 ? 35 : 0));
+  p.tile = cost256 <= cost128 ? 256 : 128;
+  if (p.tile == 128) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / t128, k / 512));
+  return p;
 }
-
 // T and B where their rows are not 16-byte pieces: copies with the rank rounded up to a multiple of 8, zeros in between.
 __global__ __launch_bounds__(256) void linear_pad_kernel(const bf16_t* T, const bf16_t* B, int64_t m, int64_t n, int r, int rp, bf16_t* Tp, bf16_t* Bp) {
   const int64_t step = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -343,20 +378,35 @@ __global__ __launch_bounds__(256) void linear_pad_kernel(const bf16_t* T, const 
   for (int64_t e = first; e < rp * n; e += step) Bp[e] = e < r * n ? B[e] : (bf16_t)0.0f;
 }
 static int64_t linear_pad_rank(int64_t r) { return (r + 7) / 8 * 8; }
-static size_t linear_large_ws_bytes(int64_t m, int64_t n, int64_t r) { return r ? align_up((size_t)(m + n) * linear_pad_rank(r) * 2, 256) : 0; }
+// Padded T and B, then the splits' partial tiles.
+static size_t linear_large_pad_bytes(int64_t m, int64_t n, int64_t r) { return r ? align_up((size_t)(m + n) * linear_pad_rank(r) * 2, 256) : 0; }
+static size_t linear_large_ws_bytes(int64_t m, int64_t n, int64_t k, int64_t r) {
+  const LargePlan p = linear_large_plan(m, n, k);
+  if (!p.tile) return 0;
+  return linear_large_pad_bytes(m, n, r) + (p.splits > 1 ? (size_t)p.splits * m * align_up((size_t)n, 4) * 4 : 0);
+}
 
 static int launch_linear_large(hipStream_t s, LinearArgs g, bool w_kc) {
+  LargePlan p = linear_large_plan(g.m, g.n, g.k);
+  char* const ws = (char*)g.part;
+  g.part = (float*)(ws + linear_large_pad_bytes(g.m, g.n, g.T ? g.r : 0));
   if (g.T && (g.r % 8 || (uintptr_t)g.T % 16 || (uintptr_t)g.B % 16)) {
     const int rp = (int)linear_pad_rank(g.r);
-    bf16_t* const tp = (bf16_t*)g.part;
+    bf16_t* const tp = (bf16_t*)ws;
     bf16_t* const bp = tp + g.m * rp;                  // (m rp elements are a multiple of 16 bytes)
     const int64_t blocks = std::min<int64_t>(ceil_div64(std::max(g.m, g.n) * rp, 256), 1024);
     LORACT_LAUNCH("linear_pad", s, linear_pad_kernel, dim3((unsigned)blocks), dim3(256), 0, (const bf16_t*)g.T, (const bf16_t*)g.B, g.m, g.n,
                   (int)g.r, rp, tp, bp);
     g.T = tp; g.B = bp; g.r = rp;
   }
-  const int tm = (int)ceil_div64(g.m, 256), tn = (int)ceil_div64(g.n, 256);
-  if (w_kc) LORACT_LAUNCH("linear_large", s, (linear_large_kernel<true>), dim3((unsigned)(tm * tn)), dim3(64 * LL_WAVES), 0, g, tm, tn);
-  else LORACT_LAUNCH("linear_large", s, (linear_large_kernel<false>), dim3((unsigned)(tm * tn)), dim3(64 * LL_WAVES), 0, g, tm, tn);
-  return LORACT_OK;
+  g.k_per_split = ceil_div64(ceil_div64(g.k, p.splits), LL_BK) * LL_BK;
+  p.splits = (int)ceil_div64(g.k, g.k_per_split);
+  g.n_pad = g.n;                                       // (a multiple of 8)
+  const int tm = (int)ceil_div64(g.m, p.tile), tn = (int)ceil_div64(g.n, p.tile);
+  const dim3 grid((unsigned)(tm * tn), (unsigned)p.splits), block(64 * ll_waves(p.tile));
+#define LL_LAUNCH(KC, TILE) LORACT_LAUNCH("linear_large", s, (linear_large_kernel<KC, TILE>), grid, block, 0, g, tm, tn)
+  if (p.tile == 256) { if (w_kc) LL_LAUNCH(true, 256); else LL_LAUNCH(false, 256); }
+  else { if (w_kc) LL_LAUNCH(true, 128); else LL_LAUNCH(false, 128); }
+#undef LL_LAUNCH
+  return p.splits > 1 ? launch_linear_join<bf16_t>(s, g, p.splits) : LORACT_OK;
 }

@@ -264,17 +264,25 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_t_kernel(LinearArgs
 static int linear_thin_form(int64_t m, int64_t n, int64_t k, bool w_kc) {
   if (k % 8 || m > (1 << 27) || n > (1 << 27)) return 0;    // (2^32 threads to a grid)
   if (m <= 32) return w_kc ? 1 : (n % 8 == 0 ? 3 : 0);
-  if (n <= 64 && (w_kc || n % 8 == 0)) return 2;
+  // (33 to 64 outputs of many tokens: the tiles read W's columns once per 128 tokens; 8192 x 11008 -> 64 49 us against 67,
+  // 2048 x 4096 -> 64 17 against 14)
+  if ((n <= 32 || (n <= 64 && m <= 4096)) && (w_kc || n % 8 == 0)) return 2;
   return 0;
 }
 static bool linear_thin_fits(const LinearArgs& g) {
   return (uintptr_t)g.X % 16 == 0 && g.ldx % 8 == 0 && (uintptr_t)g.W % 16 == 0 && g.ldw % 8 == 0;
 }
-static int linear_thin_blocks(int64_t m) { return ceil_div64(m, 32) >= 256 ? 2 : 1; }
-// K splits between workgroups: as many as make 512 of them, of at least 1024 of K (128 per wave).
+// Blocks of 16 streamed rows per wave: two where 32 rows still give every CU a workgroup, and for two blocks of tokens, whose X
+// would otherwise be read by twice as many workgroups (32 tokens through 4096 -> 11008: 36 us with one block of W's rows, 34 with two).
+static int linear_thin_blocks(int64_t m, int form) { return form == 1 ? (m > 16 ? 2 : 1) : (ceil_div64(m, 32) >= 256 ? 2 : 1); }
+// K splits between workgroups: as many as make 256 of them, of at least 1024 of K (128 per wave).  More cost the launch that joins
+// them (8192 x 4096 -> 16: 19 us with one split, 23 with two; one token through 11008 -> 4096: 20 and 23), but W as it lies, read by
+// a third as many workgroups, takes four at up to 16 tokens (4096 -> 11008: 27 us with four splits, 31 with two; 32 tokens 35 and 29).
 static int linear_thin_splits(int64_t m, int64_t n, int64_t k, int form) {
-  const int64_t wgs = form == 1 ? ceil_div64(n, 16) : (form == 2 ? ceil_div64(m, 16 * linear_thin_blocks(m)) : ceil_div64(n, 128));
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / wgs, k / 1024), 64));
+  const int64_t rows = 16 * linear_thin_blocks(m, form);
+  const int64_t wgs = form == 1 ? ceil_div64(n, rows) : (form == 2 ? ceil_div64(m, rows) : ceil_div64(n, 128));
+  const int64_t want = std::max<int64_t>(256 / wgs, form == 3 && m <= 16 ? 4 : 1);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, k / 1024), 64));
 }
 static size_t linear_thin_part_bytes(int64_t m, int64_t n, int64_t k, bool w_kc) {
   const int form = linear_thin_form(m, n, k, w_kc);
@@ -291,11 +299,11 @@ static int launch_linear_thin(hipStream_t s, LinearArgs g, bool w_kc) {
   const dim3 block(64 * LN_WAVES);
 #define LN_LAUNCH(...) LORACT_LAUNCH("linear_thin", s, (linear_thin_kernel<__VA_ARGS__>), grid, block, 0, g)
   if (form == 1) {
-    const dim3 grid((unsigned)ceil_div64(g.n, 16), (unsigned)splits);
+    const dim3 grid((unsigned)ceil_div64(g.n, 16 * linear_thin_blocks(g.m, form)), (unsigned)splits);
     if (g.m <= 16) LN_LAUNCH(true, true, 1, 1);
-    else LN_LAUNCH(true, true, 1, 2);
+    else LN_LAUNCH(true, true, 2, 2);
   } else if (form == 2) {
-    const int blocks = linear_thin_blocks(g.m);
+    const int blocks = linear_thin_blocks(g.m, form);
     const dim3 grid((unsigned)ceil_div64(g.m, 16 * blocks), (unsigned)splits);
 #define LN_SMALL(KC, B)                                                                 \
     {                                                                                   \

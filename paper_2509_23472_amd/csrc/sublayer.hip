@@ -56,8 +56,7 @@ int loract_linear_workspace_bytes(const loract_linear_params* p, size_t* bytes) 
   *bytes = align_up(linear_tile_part_bytes(p->m, p->n_out, p->n_in, bf16), 256);
   // (whichever form the call's alignment allows)
   if (bf16) *bytes = std::max(*bytes, align_up(linear_thin_part_bytes(p->m, p->n_out, p->n_in, p->w_layout == LORACT_W_OUT_IN), 256));
-  if (bf16 && linear_large_pays(p->m, p->n_out, p->n_in))
-    *bytes = std::max(*bytes, linear_large_ws_bytes(p->m, p->n_out, p->r_lora));
+  if (bf16) *bytes = std::max(*bytes, align_up(linear_large_ws_bytes(p->m, p->n_out, p->n_in, p->r_lora), 256));
   return LORACT_OK;
 }
 
@@ -85,7 +84,7 @@ int loract_linear(const void* X_dev, const void* W_dev, const float* bias_dev, c
   e.vec = p->n_out % 4 == 0 && aligned_rows(R_dev, p->ldr, 4, quad) && aligned_rows(Z_dev, p->ldz, 4, quad) &&
           aligned_rows(Y_dev, p->ldy, 4, e.y_f32 ? 16 : 8);
   if (bf16 && linear_thin_form(g.m, g.n, g.k, w_kc) && linear_thin_fits(g)) return launch_linear_thin((hipStream_t)stream, g, w_kc);
-  if (bf16 && linear_large_pays(g.m, g.n, g.k) && linear_large_fits(g, w_kc)) return launch_linear_large((hipStream_t)stream, g, w_kc);
+  if (bf16 && linear_large_plan(g.m, g.n, g.k).tile && linear_large_fits(g, w_kc)) return launch_linear_large((hipStream_t)stream, g, w_kc);
   return bf16 ? launch_linear_tile<bf16_t>((hipStream_t)stream, g, w_kc) : launch_linear_tile<float>((hipStream_t)stream, g, w_kc);
 }
 

@@ -67,7 +67,7 @@ def test_product(m, n_in, n_out, layout, dtype):
     _case(m, n_in, n_out, dtype=dtype, layout=layout)
 
 
-# large enough for the tiles of 256 x 256 (128 of them): K of one slab and of several, whole and ragged, edges in both directions
+# many tiles: K of one slab and of several, whole and ragged, edges in both directions
 @pytest.mark.parametrize("layout", ["nt", "nn"])
 @pytest.mark.parametrize("m,n_in,n_out,parts", [
     (2816, 128, 3080, dict()), (2817, 136, 2824, dict(keep=True)), (4000, 200, 2048, dict(r=16, act="silu", bias=True, keep=True)),
@@ -76,6 +76,19 @@ def test_product(m, n_in, n_out, layout, dtype):
     (260, 448, 33000, dict(r=40, residual=True)), (3001, 1000, 2808, dict(p=0.3)), (2816, 384, 2816, dict(pad=8, shift=8, r=16, residual=True)),
     (2816, 152, 2816, dict(pad=24, shift=16, r=12, act="gelu", bias=True, p=0.1))])
 def test_large_tiles(m, n_in, n_out, parts, layout):
+    _case(m, n_in, n_out, layout=layout, **parts)
+
+
+# 256 tiles of 256 x 256, the smaller tiles with K split and whole, edges in both directions
+@pytest.mark.parametrize("layout", ["nt", "nn"])
+@pytest.mark.parametrize("m,n_in,n_out,parts", [
+    (3900, 136, 4088, dict(keep=True)), (4096, 200, 4096, dict(r=16, act="silu", bias=True, keep=True)), (3841, 264, 3848, dict(r=33, p=0.1, residual=True)),
+    (4000, 456, 3992, dict(r=64, act="gelu", out_dtype="f32")), (65536, 64, 256, dict(r=40, act="relu", bias=True)), (256, 328, 65536, dict(p=0.2, residual=True)),
+    (4090, 72, 4000, dict(pad=8, shift=8, r=12, residual=True)), (65, 2056, 72, dict(r=16, act="silu", bias=True, keep=True)),
+    (300, 2400, 200, dict(residual=True, p=0.1)), (127, 8192, 136, dict(r=33, out_dtype="f32")), (129, 1096, 264, dict(act="gelu")),
+    (70, 64, 80, dict(r=64)), (1000, 648, 520, dict(pad=16, shift=8, r=8, residual=True)), (66, 4168, 4096, dict(keep=True, r=5)),
+    (2000, 128, 1000, dict(p=0.1)), (333, 1480, 408, dict(bias=True))])
+def test_both_tiles(m, n_in, n_out, parts, layout):
     _case(m, n_in, n_out, layout=layout, **parts)
 
 
@@ -101,6 +114,9 @@ def test_large_tiles_keep_nan_and_infinity_where_they_belong():
         got = _case(2816, 200, 2816, layout=layout, poison=poison).float().cpu()
         bad = ~torch.isfinite(got)
         assert bad[17].all() and bad[:, 2815].all() and int(bad.sum()) == 2816 * 2 - 1
+        got = _case(3900, 200, 4096, layout=layout, poison=poison).float().cpu()
+        bad = ~torch.isfinite(got)
+        assert bad[17].all() and bad[:, 2815].all() and int(bad.sum()) == 3900 + 4096 - 1
 
 
 @pytest.mark.parametrize("layout", ["nt", "nn"])
