@@ -131,11 +131,22 @@ template <bool KC, int R> struct LinOperand<float, KC, R> {
   typedef f32x4 piece;
   typedef f32x4 frag;
 };
-__device__ inline f32x16 lin_mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-__device__ inline f32x16 lin_mfma(f32x4 a, f32x4 b, f32x16 c) {
+// One step of a wave's MT x NT products.  float32: the k in turn for all of them, so that a product does not wait for the one before.
+template <int MT, int NT>
+__device__ inline void lin_multiply(const bf16x8 (&w)[NT], const bf16x8 (&x)[MT], f32x16 (&acc)[MT][NT]) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
-  return c;
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[j], x[i], acc[i][j], 0, 0, 0);
+}
+template <int MT, int NT>
+__device__ inline void lin_multiply(const f32x4 (&w)[NT], const f32x4 (&x)[MT], f32x16 (&acc)[MT][NT]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[j][e], x[i][e], acc[i][j], 0, 0, 0);
 }
 
 // WKC: W is n_out x n_in (rows along K), else n_in x n_out.  BM x BN tile, four waves of BM/2 x BN/2; blockIdx.z: split of K.
@@ -188,10 +199,7 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
         for (int i = 0; i < MT; ++i) x[i] = OpX::frag(smem, x_off[i], ks, lane);
 #pragma unroll
         for (int j = 0; j < NT; ++j) w[j] = OpB::frag(smem, w_off[j], ks, lane);
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int j = 0; j < NT; ++j) acc[i][j] = lin_mfma(w[j], x[i], acc[i][j]);
+        lin_multiply<MT, NT>(w, x, acc);
       }
       sb_barrier_lds();
     }
@@ -231,10 +239,7 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
       for (int i = 0; i < MT; ++i) x[i] = OpX::frag(st, x_off[i], ks, lane);
 #pragma unroll
       for (int j = 0; j < NT; ++j) w[j] = OpW::frag(st, w_off[j], ks, lane);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = lin_mfma(w[j], x[i], acc[i][j]);
+      lin_multiply<MT, NT>(w, x, acc);
     }
   };
   fetch(0, 0);
@@ -259,20 +264,27 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
   }
 }
 
-// K splits: as many as give every CU two workgroups, of at least 256 of K each (float32: 128), at most 64.
-static inline int linear_tile_splits(int64_t m, int64_t n, int64_t k, int bm, int bn, bool bf16) {
-  const int64_t tiles = ceil_div64(m, bm) * ceil_div64(n, bn);
-  const int64_t s = std::min<int64_t>(512 / tiles, k / (bf16 ? 256 : 128));
-  return (int)std::max<int64_t>(1, std::min<int64_t>(s, 64));
-}
-static inline void linear_tile_shape(int64_t m, int64_t n, int* bm, int* bn) {
-  *bm = m <= 64 ? 64 : 128;
-  *bn = m <= 64 || n <= 64 ? 64 : 128;
+// Tiles: 128 x 128 (64 in a direction that has no more), but 64 x 64 for float32 where the large ones leave CUs without work or
+// need a second round for less than half of the card: a float32 tile of 128 x 128 is matrix instructions for 55 us per 1024 of K
+// whatever feeds it, so small ones lose nothing but traffic and balance better (1024 x 256 -> 256 20 -> 13 us, 500 x 500 -> 500 26 -> 15,
+// 12608 x 768 -> 768 210 -> 190; 4096 x 1024 -> 4096, which they do not take, 305 -> 339).
+// K splits: as many as make 512 workgroups (1024 of the small float32 tiles), of at least 256 of K each, at most 64.
+struct TilePlan {
+  int bm, bn, splits;
+};
+static inline TilePlan linear_tile_plan(int64_t m, int64_t n, int64_t k, bool bf16) {
+  TilePlan p;
+  const int64_t large = ceil_div64(m, 128) * ceil_div64(n, 128);
+  const bool fine = !bf16 && (large < 256 || (large > 512 && large < 768));
+  p.bm = m <= 64 || fine ? 64 : 128;
+  p.bn = m <= 64 || n <= 64 || fine ? 64 : 128;
+  const int64_t tiles = ceil_div64(m, p.bm) * ceil_div64(n, p.bn);
+  const int64_t s = std::min<int64_t>((fine ? 1024 : 512) / tiles, k / 256);
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(s, 64));
+  return p;
 }
 static inline size_t linear_tile_part_bytes(int64_t m, int64_t n, int64_t k, bool bf16) {
-  int bm, bn;
-  linear_tile_shape(m, n, &bm, &bn);
-  const int s = linear_tile_splits(m, n, k, bm, bn, bf16);
+  const int s = linear_tile_plan(m, n, k, bf16).splits;
   return s > 1 ? (size_t)s * m * align_up((size_t)n, 4) * 4 : 0;
 }
 
@@ -288,9 +300,9 @@ template <typename T>
 static int launch_linear_tile(hipStream_t s, LinearArgs g, bool w_kc) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int BK = 128 / (int)sizeof(T);
-  int bm, bn;
-  linear_tile_shape(g.m, g.n, &bm, &bn);
-  int splits = linear_tile_splits(g.m, g.n, g.k, bm, bn, BF);
+  const TilePlan p = linear_tile_plan(g.m, g.n, g.k, BF);
+  const int bm = p.bm, bn = p.bn;
+  int splits = p.splits;
   g.k_per_split = ceil_div64(ceil_div64(g.k, splits), BK) * BK;
   splits = (int)ceil_div64(g.k, g.k_per_split);
   g.n_pad = (int64_t)align_up((size_t)g.n, 4);
