@@ -39,7 +39,6 @@ constexpr int lb_columns(int size, int rb) { return size == 2 && rb <= 2 ? 8 : 4
 template <typename T, bool VEC, int RB>
 __global__ __launch_bounds__(64 * LB_WAVES) void linear_backward_kernel(LinBackArgs g) {
   constexpr int E = lb_columns(sizeof(T), RB), U = E == 4 && sizeof(T) == 2 ? 4 : 2;
-  constexpr bool FAST = sizeof(T) == 2;
   typedef T piece __attribute__((ext_vector_type(E)));
   typedef T t_piece __attribute__((ext_vector_type(RB ? RB : 1)));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -117,7 +116,7 @@ __global__ __launch_bounds__(64 * LB_WAVES) void linear_backward_kernel(LinBackA
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < E; ++e) p[u][e] *= lin_act_slope<FAST>(act, (float)z[u][e]);
+        for (int e = 0; e < E; ++e) p[u][e] *= lin_act_slope<sizeof(T) == 4>(act, (float)z[u][e]);
     };
     if (g.act == LORACT_ACT_RELU) slopes(LORACT_ACT_RELU);
     else if (g.act == LORACT_ACT_GELU) slopes(LORACT_ACT_GELU);

@@ -4,16 +4,32 @@
 #pragma once
 #include "dropout.h"
 
-// The activations and their slopes.  FAST (bf16 inputs): exp and the reciprocal by the hardware's instructions, and Phi from
+// The activations and their slopes: exp and the reciprocal by the hardware's instructions (both within one unit), and Phi from
 //   erfc(x) = q(t) exp(-x^2),  t = 1 / (1 + 0.4 x),  x >= 0,
-// q a polynomial fitted here to the least relative error (1.4e-7, 4e-7 evaluated in float32): relative errors below 2^-20
-// wherever the result matters to 8 bits, at a fifth of the instructions of erff, expf and a division -- an epilogue of a large tile is
-// vector instructions that nothing hides (8192 x 11008 with SiLU, 4096 in: 986 -> 706 us).  Float32 inputs take the device library's functions.
-__device__ inline float lin_exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
-__device__ inline float lin_sigmoid_fast(float z) { return __builtin_amdgcn_rcpf(1.0f + lin_exp_fast(-z)); }
+// q a polynomial fitted here to the least relative error (1.4e-7, 4e-7 evaluated in float32).  EXACT (float32 inputs): the
+// rounding of exp's argument is made good and the reciprocal takes a Newton step, which leaves 4e-7; without, bf16 inputs lose up to
+// 2^-20, far below their last rounding.  A fifth of the instructions of erff, expf and a division, which an epilogue has nothing to hide
+// behind: 8192 x 4096 -> 11008 with SiLU 990 us with those, 660 so; the backward of 12608 x 768 float32 GELU 38 us, XX so.
+template <bool EXACT>
+__device__ inline float lin_exp(float x) {
+  constexpr float L = 1.44269504088896341f, L_REST = 1.92596299112661746e-8f;      // log2(e) and what its rounding leaves
+  const float t = x * L;
+  const float e = __builtin_amdgcn_exp2f(t);
+  if (!EXACT) return e;
+  const float rest = fmaf(x, L_REST, fmaf(x, L, -t));                              // (not a number where t overflows)
+  return fabsf(t) < 150.0f ? fmaf(e, 0.693147180559945309f * rest, e) : e;
+}
+template <bool EXACT>
+__device__ inline float lin_reciprocal(float x) {                                  // x >= 1
+  const float r = __builtin_amdgcn_rcpf(x);
+  return EXACT && x < 0x1p120f ? fmaf(fmaf(-x, r, 1.0f), r, r) : r;
+}
+template <bool EXACT>
+__device__ inline float lin_sigmoid(float z) { return lin_reciprocal<EXACT>(1.0f + lin_exp<EXACT>(-z)); }
 // Phi(z); *density: exp(-z^2 / 2)
-__device__ inline float lin_phi_fast(float z, float* density) {
-  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.4f * 0.70710678118654752f, 1.0f));
+template <bool EXACT>
+__device__ inline float lin_phi(float z, float* density) {
+  const float t = lin_reciprocal<EXACT>(fmaf(fabsf(z), 0.4f * 0.70710678118654752f, 1.0f));
   float q = 0.05026593804359436f;
   q = fmaf(q, t, -0.182917058467865f);
   q = fmaf(q, t, 0.16911154985427856f);
@@ -23,36 +39,33 @@ __device__ inline float lin_phi_fast(float z, float* density) {
   q = fmaf(q, t, 0.20784316956996918f);
   q = fmaf(q, t, 0.22566956281661987f);
   q = fmaf(q, t, 0.22567586600780487f);
-  *density = lin_exp_fast(-0.5f * z * z);
+  *density = lin_exp<EXACT>(-0.5f * z * z);
   const float half = 0.5f * q * t * *density;
   return z < 0.0f ? half : 1.0f - half;
 }
-template <bool FAST>
+template <bool EXACT>
 __device__ inline float lin_act(int act, float z) {
   switch (act) {
-    case LORACT_ACT_RELU: return z < 0.0f ? 0.0f : z;                       // (a NaN stays one)
+    case LORACT_ACT_RELU: return z < 0.0f ? 0.0f : z;                              // (a NaN stays one)
     case LORACT_ACT_GELU: {
       float density;
-      return FAST ? z * lin_phi_fast(z, &density) : 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+      return z * lin_phi<EXACT>(z, &density);
     }
-    case LORACT_ACT_SILU: return FAST ? z * lin_sigmoid_fast(z) : z / (1.0f + expf(-z));
+    case LORACT_ACT_SILU: return z * lin_sigmoid<EXACT>(z);
     default: return z;
   }
 }
-template <bool FAST>
+template <bool EXACT>
 __device__ inline float lin_act_slope(int act, float z) {
   switch (act) {
     case LORACT_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
     case LORACT_ACT_GELU: {
-      if (FAST) {
-        float density;
-        const float phi = lin_phi_fast(z, &density);
-        return phi + z * (density * 0.39894228040143268f);
-      }
-      return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * (expf(-0.5f * z * z) * 0.39894228040143268f);
+      float density;
+      const float phi = lin_phi<EXACT>(z, &density);
+      return phi + z * (density * 0.39894228040143268f);
     }
     case LORACT_ACT_SILU: {
-      const float s = FAST ? lin_sigmoid_fast(z) : 1.0f / (1.0f + expf(-z));
+      const float s = lin_sigmoid<EXACT>(z);
       return s * (1.0f + z * (1.0f - s));
     }
     default: return 1.0f;
@@ -79,25 +92,33 @@ struct LinQuad {
   typedef T type __attribute__((ext_vector_type(4)));
 };
 
-// Four columns col .. col + 3 (col a multiple of 4) of one row.
+// Four columns col .. col + 3 (col a multiple of 4) of one row: the residual, to be loaded ahead, and the rest.
 template <typename T>
-__device__ inline void lin_store4(const LinEpilogue& e, int64_t row, int64_t col, f32x4 v) {
-  if (row >= e.m || col >= e.n) return;
+__device__ inline f32x4 lin_load4(const LinEpilogue& e, int64_t row, int64_t col) {
+  f32x4 r = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (!e.R || row >= e.m || col >= e.n) return r;
   typedef typename LinQuad<T>::type quad;
-  float b[4] = {0.0f, 0.0f, 0.0f, 0.0f}, r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   const T* rp = (const T*)e.R + row * e.ldr + col;
-  T* zp = (T*)e.Z + row * e.ldz + col;
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const bool in = col + u < e.n;
-    if (e.bias && in) b[u] = e.bias[col + u];
-    if (e.R && !e.vec && in) r[u] = (float)rp[u];
-  }
-  if (e.R && e.vec) {
+  if (e.vec) {
     const quad q = *(const quad*)rp;
 #pragma unroll
     for (int u = 0; u < 4; ++u) r[u] = (float)q[u];
+  } else {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (col + u < e.n) r[u] = (float)rp[u];
   }
+  return r;
+}
+template <typename T>
+__device__ inline void lin_store4(const LinEpilogue& e, int64_t row, int64_t col, f32x4 v, f32x4 r) {
+  if (row >= e.m || col >= e.n) return;
+  typedef typename LinQuad<T>::type quad;
+  float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  T* zp = (T*)e.Z + row * e.ldz + col;
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+    if (e.bias && col + u < e.n) b[u] = e.bias[col + u];
   quad zq;
   f32x4 y;
   const uint64_t word = e.d.thr ? drop_word(e.d, row, col / 4) : 0;
@@ -105,7 +126,7 @@ __device__ inline void lin_store4(const LinEpilogue& e, int64_t row, int64_t col
   for (int u = 0; u < 4; ++u) {
     const float z = v[u] + b[u];
     zq[u] = (T)z;
-    float a = lin_act<sizeof(T) == 2>(e.act, z);
+    float a = lin_act<sizeof(T) == 4>(e.act, z);
     if (e.d.thr) a = drop_one(e.d, word, u, a);
     y[u] = e.R ? a + r[u] : a;
   }
@@ -138,6 +159,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const float* part, int
     const int64_t row = i / quads, col = (i - row * quads) * 4;
     const float* src = part + row * n_pad + col;
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    const f32x4 r = lin_load4<T>(e, row, col);
     for (int z = 0; z < splits; z += 4) {
       f32x4 v[4];
 #pragma unroll
@@ -146,6 +168,6 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const float* part, int
       for (int u = 0; u < 4; ++u)
         if (z + u < splits) s += v[u];
     }
-    lin_store4<T>(e, row, col, s);
+    lin_store4<T>(e, row, col, s, r);
   }
 }

@@ -302,7 +302,7 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
 #pragma unroll
       for (int q = 0; q < N8; ++q)
 #pragma unroll
-        for (int u = 0; u < 8; ++u) y[q][u] = lin_act<true>(e.act, y[q][u]);
+        for (int u = 0; u < 8; ++u) y[q][u] = lin_act<false>(e.act, y[q][u]);
     }
     if (e.d.thr) {
 #pragma unroll

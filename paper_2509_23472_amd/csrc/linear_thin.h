@@ -35,12 +35,12 @@ __device__ inline bf16x8 ln_rank_w(const LinearArgs& g, int64_t col, int r0) {
 template <typename Place>
 __device__ inline void ln_finish(const LinearArgs& g, const f32x4* part, int quads, Place place) {
   for (int i = threadIdx.x; i < quads; i += 64 * LN_WAVES) {
+    int64_t row, col;
+    place(i, &row, &col);
     f32x4 s = part[i];
 #pragma unroll
     for (int w = 1; w < LN_WAVES; ++w) s += part[w * quads + i];
-    int64_t row, col;
-    place(i, &row, &col);
-    if (gridDim.y == 1) lin_store4<bf16_t>(g.e, row, col, s);
+    if (gridDim.y == 1) lin_store4<bf16_t>(g.e, row, col, s, lin_load4<bf16_t>(g.e, row, col));
     else if (row < g.m && col < g.n_pad) *(f32x4*)(g.part + ((int64_t)blockIdx.y * g.m + row) * g.n_pad + col) = s;
   }
 }
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_t_kernel(LinearArgs
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] += ((const float*)(part + w * QUADS + ((4 * half + j) * SMALL + s) * 64 + l))[u];
     const int64_t row = 16 * s + m16, col = first + 8 * at16 + 4 * half;
-    if (gridDim.y == 1) lin_store4<bf16_t>(g.e, row, col, v);
+    if (gridDim.y == 1) lin_store4<bf16_t>(g.e, row, col, v, lin_load4<bf16_t>(g.e, row, col));
     else if (row < g.m && col < g.n_pad) *(f32x4*)(g.part + ((int64_t)blockIdx.y * g.m + row) * g.n_pad + col) = v;
   }
 }

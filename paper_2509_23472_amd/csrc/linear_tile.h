@@ -248,19 +248,37 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
   for (; s + 2 <= nslab; s += 2) { step(0, s); step(1, s + 1); }
   if (s < nslab) step(0, s);
 
-  // accumulator register 4 q + u of lane l: column 8 q + 4 (l / 32) + u, row l % 32 of its tile
+  // Accumulator register 4 q + u of lane l: column 8 q + 4 (l / 32) + u, row l % 32 of its tile.  They leave 32 rows at a time through LDS, so
+  // that neighbouring lanes hold neighbouring columns, with all loads of the residual ahead.
+  constexpr int PART = BN / 2, LDC = PART + 4, QPR = PART / 4, ROWS = 64 / QPR, N4 = 32 / ROWS;
+  static_assert(4 * 32 * LDC * 4 <= 2 * STAGE, "staging of the output");
+  sb_barrier_lds();                                // the last slab has been read
+  float* const cs = (float*)(smem + wave * (32 * LDC * 4));
+  const int c4 = lane % QPR * 4, r0 = lane / QPR;
+  const int64_t col = col0 + wn * PART + c4;
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int64_t row = row0 + wm * (BM / 2) + 32 * i + (lane & 31);
+    const int64_t row = row0 + wm * (BM / 2) + 32 * i + r0;
+    f32x4 res[N4];
+    if (gridDim.z == 1) {
+#pragma unroll
+      for (int q = 0; q < N4; ++q) res[q] = lin_load4<T>(g.e, row + ROWS * q, col);
+    }
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t col = col0 + wn * (BN / 2) + 32 * j + 8 * q + 4 * (lane >> 5);
-        const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        if (gridDim.z == 1) lin_store4<T>(g.e, row, col, v);
-        else if (row < g.m && col < g.n_pad) *(f32x4*)(g.part + ((int64_t)blockIdx.z * g.m + row) * g.n_pad + col) = v;
-      }
+      for (int q = 0; q < 4; ++q)
+        *(f32x4*)(cs + (lane & 31) * LDC + 32 * j + 8 * q + 4 * (lane >> 5)) =
+            (f32x4){acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    sb_wave_sync();
+#pragma unroll
+    for (int q = 0; q < N4; ++q) {
+      const f32x4 v = *(const f32x4*)(cs + (r0 + ROWS * q) * LDC + c4);
+      const int64_t at = row + ROWS * q;
+      if (gridDim.z == 1) lin_store4<T>(g.e, at, col, v, res[q]);
+      else if (at < g.m && col < g.n_pad) *(f32x4*)(g.part + ((int64_t)blockIdx.z * g.m + at) * g.n_pad + col) = v;
+    }
+    sb_wave_sync();
   }
 }
 
