@@ -492,13 +492,15 @@ def loract_rope_table(n_pos: int, rot: int, theta: float = 10000.0, first: int =
     return table
 
 
-def _heads(t: torch.Tensor, m: int, heads: int, d: int, dtype: torch.dtype, what: str) -> Tuple[int, int]:
-    """Token and head strides of a GPU tensor tokens x heads x d with contiguous heads."""
+def _heads(t: torch.Tensor, m: int, heads: int, d: int, dtype: torch.dtype, what: str, written: bool = False) -> Tuple[int, int]:
+    """Token and head strides of a GPU tensor tokens x heads x d with contiguous heads, which must not overlap if `written`."""
     if t.shape != (m, heads, d) or t.dtype is not dtype or not t.is_cuda:
         raise ValueError("%s must be a GPU tensor of %d tokens x %d heads x %d of %s" % (what, m, heads, d, dtype))
     token, head, step = t.stride()
     if step != 1 and d > 1:
         raise ValueError("the heads of %s must be contiguous" % what)
+    if written and ((token < d and m > 1) or (head < d and heads > 1)):
+        raise ValueError("the heads of %s must not overlap" % what)
     return token, head
 
 
@@ -519,8 +521,8 @@ def _qk_call(q, k, gamma_q, gamma_k, table, positions, eps, interleaved, q_out, 
         raise ValueError("positions must be a contiguous int32 GPU tensor with one entry per token")
     strides = _heads(q, m, hq, d, dt, "q")
     strides += (0, 0) if k is None else _heads(k, m, hk, d, dt, "k")
-    strides += (hq * d, d) if q_out is None else _heads(q_out, m, hq, d, dt, "out")
-    strides += (hk * d, d) if k_out is None else _heads(k_out, m, hk, d, dt, "out")
+    strides += (hq * d, d) if q_out is None else _heads(q_out, m, hq, d, dt, "out", True)
+    strides += (hk * d, d) if k_out is None else _heads(k_out, m, hk, d, dt, "out", True)
     strides += (0, 0) if dq is None else _heads(dq, m, hq, d, dt, "dq_out")
     strides += (0, 0) if dk is None else _heads(dk, m, hk, d, dt, "dk_out")
     params = _QK_PARAMS.pack(m, hq, hk, d, rot, 1 if interleaved else 0, _dtype_code(dt), n_pos, eps, *strides)

@@ -170,6 +170,61 @@ def test_dropped_places_hide_whatever_was_there():
     assert (dp.cpu()[~keep] == 0).all() and torch.isnan(dp.cpu()[keep]).all()
 
 
+def test_operands_that_do_not_fit_are_refused():
+    import paper_2509_23472_amd as L
+    x, w = torch.zeros((8, 64), device="cuda"), torch.zeros((32, 64), device="cuda")
+    t, b = torch.zeros((8, 4), device="cuda"), torch.zeros((4, 32), device="cuda")
+    calls = [lambda: L.loract_linear(x, w.bfloat16()), lambda: L.loract_linear(x, w, w_transposed=True), lambda: L.loract_linear(x, w, lora_t=t),
+             lambda: L.loract_linear(x, w, lora_t=t, lora_b=b[:3]), lambda: L.loract_linear(x, w, torch.zeros(31, device="cuda")),
+             lambda: L.loract_linear(x, w, torch.zeros(32, device="cuda").half()), lambda: L.loract_linear(x, w, residual=x), lambda: L.loract_linear(x, w, act="tanh"),
+             lambda: L.loract_linear(x, w, out=torch.zeros((8, 1), device="cuda").expand(8, 32)), lambda: L.loract_linear(x.t(), w), lambda: L.loract_linear(x[0], w),
+             lambda: L.loract_linear_backward(x, act="silu"), lambda: L.loract_linear_backward(x, x[:4], act="silu"), lambda: L.loract_linear_backward(x, lora_t=t[:4]),
+             lambda: L.loract_dropout(x, 0.1, 0, residual=w), lambda: L.loract_dropout(x[:1].expand(8, 64), 0.1, 0)]
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: L.loract_linear(x, w, p_drop=1.0), lambda: L.loract_dropout(x, -0.5, 0), lambda: L.loract_linear(x, w, out_dtype=torch.bfloat16),
+                 lambda: L.loract_linear(x, w, lora_t=torch.zeros((8, 65), device="cuda"), lora_b=torch.zeros((65, 32), device="cuda"))):
+        with pytest.raises(L.LoractError):
+            call()
+    with pytest.raises(TypeError):
+        L.loract_linear(x.half(), w.half())
+
+
+def test_calls_can_be_captured_and_replayed():
+    """Nothing is enqueued but kernels, and every replay gives what the call gives, with other work in between."""
+    import paper_2509_23472_amd as L
+    gen = torch.Generator().manual_seed(9)
+    x, w, wt = (_rand(gen, *s, dtype=torch.bfloat16).cuda() for s in ((300, 512), (256, 512), (512, 24)))
+    lt = _rand(gen, 300, 8, dtype=torch.bfloat16).cuda()
+    lb = _rand(gen, 8, 256, dtype=torch.bfloat16).cuda()
+    table, gamma = L.loract_rope_table(300, 64), torch.ones(64, device="cuda")
+
+    def work():
+        y, z = L.loract_linear(x, w, lora_t=lt, lora_b=lb, act="gelu", p_drop=0.1, seed=3, save_preact=True)
+        t = L.loract_linear(x, wt, w_transposed=True)
+        back = L.loract_linear_backward(y, z, lora_t=lt, act="gelu", p_drop=0.1, seed=3)
+        heads = y.view(300, 4, 64)
+        return (y, z, t) + back + L.loract_qknorm_rope_backward(heads, None, gamma, None, table, heads, None)[::2] + (L.loract_dropout(y, 0.5, 1),)
+
+    want = [v.clone() for v in work()]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        work()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = work()
+    for _ in range(4):
+        for v in got:
+            v.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        torch.randn(1000, 1000, device="cuda") @ torch.randn(1000, 1000, device="cuda")
+
+
 def test_no_tokens():
     import paper_2509_23472_amd as L
     x, w = torch.zeros((0, 64), device="cuda"), torch.zeros((32, 64), device="cuda")

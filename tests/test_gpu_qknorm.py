@@ -158,6 +158,14 @@ def test_in_place_on_a_side_stream_and_repeated():
     assert torch.equal(q, fwd[0]) and torch.equal(k, fwd[1])
 
 
+def test_outputs_that_overlap_are_refused():
+    import paper_2509_23472_amd as L
+    x = torch.zeros((4, 2, 64), device="cuda")
+    for bad in (x[:1].expand(4, 2, 64), x[:, :1].expand(4, 2, 64), x[:, :, ::2], x[:, :1], x.double()):
+        with pytest.raises(ValueError):
+            L.loract_qknorm_rope_forward(x, None, None, None, None, out=(bad, None))
+
+
 def test_no_tokens():
     import paper_2509_23472_amd as L
     x, gamma, table = torch.zeros((0, 2, 64), device="cuda"), torch.ones(64, device="cuda"), L.loract_rope_table(4, 64)
