@@ -9,6 +9,9 @@
 
 #include <type_traits>
 
+typedef bf16x8 bf16x8_any __attribute__((aligned(2)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+
 #define LL_BK 64
 #define LL_X_STAGES 3
 #define LL_W_STAGES 2
@@ -64,9 +67,9 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
   // copy c of a wave: 8 rows of 128 bytes along K, or KPC whole rows of W as it lies
   const int copy_row = 8 * wave * C + (lane >> 3), copy_k = KPC * wave * C + lane / LPK;
   auto chunk_of = [&](int c) { return (lane & 7) ^ ll_turn(copy_row + 8 * c); };
-  auto col_of = [&](int c) {
+  auto col_of = [&](int c, int64_t n8) {
     const int64_t col = ((lane % LPK) ^ ll_turn_k(copy_k + KPC * c)) * 8;
-    return col0 + col < g.n ? col : g.n - 8 - col0;                         // columns past the end are never stored
+    return col0 + col < n8 ? col : n8 - 8 - col0;                           // columns past the end are never stored
   };
   unsigned xo[C], wo[C];
 #pragma unroll
@@ -78,7 +81,7 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
       const int64_t wr = col0 + row < g.n ? row : g.n - 1 - col0;
       wo[c] = (unsigned)(wr * g.ldw * 2) + chunk_of(c) * 16;
     } else {
-      wo[c] = (unsigned)((copy_k + KPC * c) * g.ldw * 2) + (unsigned)col_of(c) * 2;
+      wo[c] = (unsigned)((copy_k + KPC * c) * g.ldw * 2) + (unsigned)col_of(c, g.w_n8) * 2;
     }
   }
   // Slabs are numbered through: the one of T and B, if there is a low-rank term, then those of X and W.
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
     for (int c = 0; c < C; ++c) {
       const int kr = copy_k + KPC * c, chunk = chunk_of(c);
       if (v < nlr)
-        sb_async16((const bf16_t*)g.B + (int64_t)(kr < left ? kr : left - 1) * g.n + col0 + col_of(c), st + c * 1024);
+        sb_async16((const bf16_t*)g.B + (int64_t)(kr < left ? kr : left - 1) * g.ldb + col0 + col_of(c, g.b_n8), st + c * 1024);
       else if (WKC)
         sb_async16_at(ws, wo[c] - (chunk * 8 < left ? 0 : chunk * 16), st + c * 1024);
       else
@@ -248,10 +251,23 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
   float* const cs = (float*)(smem + wave * (32 * LDC * 4));
   const int c8 = (lane % LPR) * 8, r8 = lane / LPR;
   const int64_t col = col0 + wn * PART + c8;
-  const bool in = col < g.n, split = gridDim.y > 1;
+  // (pieces of R, Z and Y at any address; the last one of a row whose length is no multiple of 8 goes element by element)
+  const bool in = col < g.n, whole = col + 8 <= g.n, split = gridDim.y > 1;
+  auto store = [&](bf16_t* out, const float (&v)[8]) {
+    bf16x8 o;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) o[u] = (bf16_t)v[u];
+    if (whole) {
+      *(bf16x8_any*)out = o;
+    } else {
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (col + u < g.n) out[u] = o[u];
+    }
+  };
   float bias[8];
 #pragma unroll
-  for (int u = 0; u < 8; ++u) bias[u] = e.bias && in && !split ? e.bias[col + u] : 0.0f;
+  for (int u = 0; u < 8; ++u) bias[u] = e.bias && col + u < g.n && !split ? e.bias[col + u] : 0.0f;
 #pragma unroll
   for (int i = 0; i < MT; i += 2) {
     const int64_t row = row0 + wm * (TILE / 2) + 16 * i + r8;
@@ -260,7 +276,13 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
 #pragma unroll
       for (int q = 0; q < N8; ++q) {
         const int64_t at = row + ROWS * q < g.m ? row + ROWS * q : g.m - 1;
-        res[q] = *(const bf16x8*)((const bf16_t*)e.R + at * e.ldr + (in ? col : 0));
+        const bf16_t* const src = (const bf16_t*)e.R + at * e.ldr + col;
+        if (whole) {
+          res[q] = *(const bf16x8_any*)src;
+        } else {
+#pragma unroll
+          for (int u = 0; u < 8; ++u) res[q][u] = col + u < g.n ? src[u] : (bf16_t)0.0f;
+        }
       }
     }
 #pragma unroll
@@ -283,7 +305,7 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
 #pragma unroll
       for (int q = 0; q < N8; ++q) {
         if (!in || row + ROWS * q >= g.m) continue;
-        float* out = g.part + ((int64_t)blockIdx.y * g.m + row + ROWS * q) * g.n_pad + col;
+        float* out = g.part + ((int64_t)blockIdx.y * g.m + row + ROWS * q) * g.n_pad + col;       // (n_pad: a multiple of 8)
         *(f32x4*)out = (f32x4){y[q][0], y[q][1], y[q][2], y[q][3]};
         *(f32x4*)(out + 4) = (f32x4){y[q][4], y[q][5], y[q][6], y[q][7]};
       }
@@ -291,12 +313,8 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
     }
     if (e.Z && in) {
 #pragma unroll
-      for (int q = 0; q < N8; ++q) {
-        bf16x8 z;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) z[u] = (bf16_t)y[q][u];
-        if (row + ROWS * q < g.m) *(bf16x8*)((bf16_t*)e.Z + (row + ROWS * q) * e.ldz + col) = z;
-      }
+      for (int q = 0; q < N8; ++q)
+        if (row + ROWS * q < g.m) store((bf16_t*)e.Z + (row + ROWS * q) * e.ldz + col, y[q]);
     }
     if (e.act != LORACT_ACT_NONE) {
 #pragma unroll
@@ -324,26 +342,23 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
 #pragma unroll
     for (int q = 0; q < N8; ++q) {
       if (!in || row + ROWS * q >= g.m) continue;
-      if (e.y_f32) {
-        float* out = (float*)e.Y + (row + ROWS * q) * e.ldy + col;
-        *(f32x4*)out = (f32x4){y[q][0], y[q][1], y[q][2], y[q][3]};
-        *(f32x4*)(out + 4) = (f32x4){y[q][4], y[q][5], y[q][6], y[q][7]};
+      if (!e.y_f32) {
+        store((bf16_t*)e.Y + (row + ROWS * q) * e.ldy + col, y[q]);
+        continue;
+      }
+      float* const out = (float*)e.Y + (row + ROWS * q) * e.ldy + col;
+      if (whole) {
+        *(f32x4_any*)out = (f32x4){y[q][0], y[q][1], y[q][2], y[q][3]};
+        *(f32x4_any*)(out + 4) = (f32x4){y[q][4], y[q][5], y[q][6], y[q][7]};
       } else {
-        bf16x8 o;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) o[u] = (bf16_t)y[q][u];
-        *(bf16x8*)((bf16_t*)e.Y + (row + ROWS * q) * e.ldy + col) = o;
+        for (int u = 0; u < 8; ++u)
+          if (col + u < g.n) out[u] = y[q][u];
       }
     }
   }
 }
 
-// What these tiles need: 16-byte pieces of everything, and 32 bits for the byte offsets within a tile.
-static bool linear_large_fits(const LinearArgs& g, bool w_kc) {
-  auto rows = [](const void* p, int64_t ld) { return !p || ((uintptr_t)p % 16 == 0 && ld % 8 == 0); };
-  return g.k % 8 == 0 && g.n % 8 == 0 && rows(g.X, g.ldx) && rows(g.W, g.ldw) && rows(g.e.R, g.e.ldr) && rows(g.e.Y, g.e.ldy) &&
-         rows(g.e.Z, g.e.ldz) && g.ldx < (1 << 22) && g.ldw < (w_kc ? 1 << 22 : 1 << 24);
-}
 // Tile (0: another form) and K splits.
 //
 // Costs in hundredths of a round of 256 tiles of 256 x 256, one per CU: a last round of few of them takes two thirds of one; 512
@@ -367,41 +382,101 @@ static LargePlan linear_large_plan(int64_t m, int64_t n, int64_t k) {
   if (p.tile == 128) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / t128, k / 512));
   return p;
 }
-// T and B where their rows are not 16-byte pieces: copies with the rank rounded up to a multiple of 8, zeros in between.
-__global__ __launch_bounds__(256) void linear_pad_kernel(const bf16_t* T, const bf16_t* B, int64_t m, int64_t n, int r, int rp, bf16_t* Tp, bf16_t* Bp) {
-  const int64_t step = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  for (int64_t e = first; e < m * rp; e += step) {
-    const int64_t row = e / rp;
-    const int c = (int)(e - row * rp);
-    Tp[e] = c < r ? T[row * r + c] : (bf16_t)0.0f;
+// Operands whose rows are not 16-byte pieces are copied first: rows x cols into rows_p x cols_p (a multiple of 8), zeros in between.
+struct PadArgs {
+  const bf16_t* src;
+  int64_t ld, rows, cols;
+  bf16_t* dst;
+  int64_t rows_p, cols_p;
+};
+__global__ __launch_bounds__(256) void linear_pad_kernel(PadArgs a, PadArgs b) {
+  const PadArgs& p = blockIdx.y ? b : a;
+  const int64_t per_row = p.cols_p / 8, step = (int64_t)gridDim.x * 256;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < p.rows_p * per_row; e += step) {
+    const int64_t row = e / per_row, c = (e - row * per_row) * 8;
+    const bf16_t* src = p.src + row * p.ld + c;
+    bf16x8 v = {};
+    if (row < p.rows) {
+      if (c + 8 <= p.cols) {
+        v = *(const bf16x8_any*)src;
+      } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (c + u < p.cols) v[u] = src[u];
+      }
+    }
+    *(bf16x8*)(p.dst + e * 8) = v;
   }
-  for (int64_t e = first; e < rp * n; e += step) Bp[e] = e < r * n ? B[e] : (bf16_t)0.0f;
 }
-static int64_t linear_pad_rank(int64_t r) { return (r + 7) / 8 * 8; }
-// Padded T and B, then the splits' partial tiles.
-static size_t linear_large_pad_bytes(int64_t m, int64_t n, int64_t r) { return r ? align_up((size_t)(m + n) * linear_pad_rank(r) * 2, 256) : 0; }
-static size_t linear_large_ws_bytes(int64_t m, int64_t n, int64_t k, int64_t r) {
-  const LargePlan p = linear_large_plan(m, n, k);
-  if (!p.tile) return 0;
-  return linear_large_pad_bytes(m, n, r) + (p.splits > 1 ? (size_t)p.splits * m * align_up((size_t)n, 4) * 4 : 0);
+static int launch_linear_pad(hipStream_t s, PadArgs a, PadArgs b) {
+  if (!a.src && !b.src) return LORACT_OK;
+  if (!a.src) a = b;
+  const int64_t pieces = std::max(a.rows_p * a.cols_p, b.src ? b.rows_p * b.cols_p : 0) / 8;
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div64(pieces, 256), 2048), b.src && b.dst != a.dst ? 2 : 1);
+  LORACT_LAUNCH("linear_pad", s, linear_pad_kernel, grid, dim3(256), 0, a, b);
+  return LORACT_OK;
 }
 
-static int launch_linear_large(hipStream_t s, LinearArgs g, bool w_kc) {
-  LargePlan p = linear_large_plan(g.m, g.n, g.k);
+// What a call copies, by sizes and strides alone, so that the workspace can be told in advance.
+struct LargeSpace {
+  bool pad_x, pad_w;
+  int64_t k8, n8, r8;
+  size_t off_t, off_b, off_x, off_w, off_part, total;
+};
+static LargeSpace linear_large_space(const LargePlan& p, int64_t m, int64_t n, int64_t k, int64_t r, int64_t ldx, int64_t ldw, bool w_kc) {
+  LargeSpace q;
+  auto up8 = [](int64_t v) { return (v + 7) / 8 * 8; };
+  q.k8 = up8(k); q.n8 = up8(n); q.r8 = up8(r);
+  q.pad_x = k % 8 || ldx % 8;
+  q.pad_w = ldw % 8 || k % 8 || (!w_kc && n % 8);
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
+  q.off_t = take((size_t)m * q.r8 * 2);
+  q.off_b = take((size_t)q.r8 * q.n8 * 2);
+  q.off_x = take(q.pad_x ? (size_t)m * q.k8 * 2 : 0);
+  q.off_w = take(q.pad_w ? (size_t)(w_kc ? n * q.k8 : q.k8 * q.n8) * 2 : 0);
+  q.off_part = take(p.splits > 1 ? (size_t)p.splits * m * q.n8 * 4 : 0);
+  q.total = off;
+  return q;
+}
+// The copies read and write X and W once, the general tiles take twice the time: 8192 x 4095 -> 4096 251 us against 474, 2001 x 501 ->
+// 2001 19 / 26, 513 x 3001 -> 2001 29 / 34; 700 x 1030 -> 700 21 / 18, 100 x 4001 -> 4001 31 / 25.
+static bool linear_large_pays(const LargeSpace& q, int64_t m, int64_t n) {
+  return (!q.pad_x && !q.pad_w) || m * n >= (m + n) * 400;
+}
+// 32 bits have to do for the byte offsets within a tile; an operand that is not copied has to start on 16 bytes.
+static bool linear_large_fits(const LinearArgs& g, bool w_kc, const LargeSpace& q) {
+  return (q.pad_x || ((uintptr_t)g.X % 16 == 0 && g.ldx < (1 << 22))) && q.k8 < (1 << 22) && q.n8 < (1 << 24) &&
+         (q.pad_w || ((uintptr_t)g.W % 16 == 0 && g.ldw < (w_kc ? 1 << 22 : 1 << 24)));
+}
+
+static int launch_linear_large(hipStream_t s, LinearArgs g, bool w_kc, LargePlan p, const LargeSpace& q) {
   char* const ws = (char*)g.part;
-  g.part = (float*)(ws + linear_large_pad_bytes(g.m, g.n, g.T ? g.r : 0));
-  if (g.T && (g.r % 8 || (uintptr_t)g.T % 16 || (uintptr_t)g.B % 16)) {
-    const int rp = (int)linear_pad_rank(g.r);
-    bf16_t* const tp = (bf16_t*)ws;
-    bf16_t* const bp = tp + g.m * rp;                  // (m rp elements are a multiple of 16 bytes)
-    const int64_t blocks = std::min<int64_t>(ceil_div64(std::max(g.m, g.n) * rp, 256), 1024);
-    LORACT_LAUNCH("linear_pad", s, linear_pad_kernel, dim3((unsigned)blocks), dim3(256), 0, (const bf16_t*)g.T, (const bf16_t*)g.B, g.m, g.n,
-                  (int)g.r, rp, tp, bp);
-    g.T = tp; g.B = bp; g.r = rp;
+  g.part = (float*)(ws + q.off_part);
+  PadArgs pt{}, pb{}, px{}, pw{};
+  g.ldb = g.n;
+  g.b_n8 = g.n;
+  if (g.T && (g.r % 8 || (uintptr_t)g.T % 16 || (uintptr_t)g.B % 16 || g.n % 8)) {
+    pt = {(const bf16_t*)g.T, g.r, g.m, g.r, (bf16_t*)(ws + q.off_t), g.m, q.r8};
+    pb = {(const bf16_t*)g.B, g.n, g.r, g.n, (bf16_t*)(ws + q.off_b), q.r8, q.n8};
+    g.T = pt.dst; g.B = pb.dst; g.r = q.r8; g.ldb = g.b_n8 = q.n8;
   }
+  g.w_n8 = g.n;
+  if (q.pad_x) {
+    px = {(const bf16_t*)g.X, g.ldx, g.m, g.k, (bf16_t*)(ws + q.off_x), g.m, q.k8};
+    g.X = px.dst; g.ldx = q.k8;
+  }
+  if (q.pad_w) {
+    pw = {(const bf16_t*)g.W, g.ldw, w_kc ? g.n : g.k, w_kc ? g.k : g.n, (bf16_t*)(ws + q.off_w), w_kc ? g.n : q.k8, w_kc ? q.k8 : q.n8};
+    g.W = pw.dst; g.ldw = w_kc ? q.k8 : q.n8; g.w_n8 = q.n8;
+  }
+  LORACT_TRY(launch_linear_pad(s, pt, pb));
+  LORACT_TRY(launch_linear_pad(s, px, pw));
+  // (an operand that is not copied has whole pieces along K, or is the one that decides that neither is)
+  g.k = q.pad_x && q.pad_w ? q.k8 : g.k;
   g.k_per_split = ceil_div64(ceil_div64(g.k, p.splits), LL_BK) * LL_BK;
   p.splits = (int)ceil_div64(g.k, g.k_per_split);
-  g.n_pad = g.n;                                       // (a multiple of 8)
+  g.n_pad = q.n8;
   const int tm = (int)ceil_div64(g.m, p.tile), tn = (int)ceil_div64(g.n, p.tile);
   const dim3 grid((unsigned)(tm * tn), (unsigned)p.splits), block(64 * ll_waves(p.tile));
 #define LL_LAUNCH(KC, TILE) LORACT_LAUNCH("linear_large", s, (linear_large_kernel<KC, TILE>), grid, block, 0, g, tm, tn)

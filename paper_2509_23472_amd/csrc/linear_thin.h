@@ -10,10 +10,19 @@
 
 #define LN_WAVES 8
 
-// Eight consecutive k of a row along K, zero past the end of K.
+// Rows may start anywhere: pieces of eight elements are read at whatever address they have.
+// Eight consecutive k of a row along K, zero past the end of K (k_len >= 8).
 __device__ inline bf16x8 ln_load(const bf16_t* row, int64_t k, int64_t k_len) {
-  bf16x8 v = *(const bf16x8*)(row + (k < k_len ? k : k_len - 8));
-  return k < k_len ? v : (bf16x8){};
+  return __builtin_bit_cast(bf16x8, gb_shift(gb_load(row, k < k_len ? k : k_len, k_len), k < k_len ? k : k_len, k_len));
+}
+// Eight consecutive columns from `col` on of a row of n columns.
+__device__ inline bf16x8 ln_columns(const bf16_t* row, int64_t col, int64_t n) {
+  if (col + 8 <= n) return *(const bf16x8_any*)(row + col);
+  bf16x8 v = {};
+#pragma unroll
+  for (int u = 0; u < 8; ++u)
+    if (col + u < n) v[u] = row[col + u];
+  return v;
 }
 // Fragment of T (row `row`) or of B (column `col`), 32 of the rank from r0 on.
 __device__ inline bf16x8 ln_rank_x(const LinearArgs& g, int64_t row, int r0) {
@@ -57,6 +66,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_kernel(LinearArgs g
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
   const int64_t first = (int64_t)blockIdx.x * (16 * BLOCKS);
+  const bool inside = g.n >= 16 * SMALL;                 // (uniform; of the columns that TURN reads)
   const int64_t rows = OF_W ? g.n : g.m, others = OF_W ? g.m : g.n;
   const bf16_t *stream[BLOCKS], *small[SMALL];
 #pragma unroll
@@ -67,8 +77,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_kernel(LinearArgs g
 #pragma unroll
   for (int b = 0; b < SMALL; ++b) {
     const int64_t row = 16 * b + c < others ? 16 * b + c : others - 1;
-    if (TURN) small[b] = (const bf16_t*)g.W + (16 * b + 8 * (lane & 1) < g.n ? 16 * b + 8 * (lane & 1) : 0);   // (n is a multiple of 8)
-    else small[b] = OF_W ? (const bf16_t*)g.X + row * g.ldx : (const bf16_t*)g.W + row * g.ldw;
+    small[b] = OF_W ? (const bf16_t*)g.X + row * g.ldx : (const bf16_t*)g.W + row * g.ldw;
   }
   f32x4 acc[BLOCKS][SMALL];
 #pragma unroll
@@ -106,10 +115,16 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_kernel(LinearArgs g
       for (int u = 0; u < U; ++u) {
         const int64_t k = k0 + 32 * u;
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) st[u][b] = *(const bf16x8*)(stream[b] + k + 8 * q);
+        for (int b = 0; b < BLOCKS; ++b) st[u][b] = *(const bf16x8_any*)(stream[b] + k + 8 * q);
 #pragma unroll
         for (int s = 0; s < SMALL; ++s)
-          sm[u][s] = TURN ? *(const bf16x8*)(small[s] + (k + (lane >> 1)) * g.ldw) : *(const bf16x8*)(small[s] + k + 8 * q);
+          if (TURN) {
+            const bf16_t* const row = (const bf16_t*)g.W + (k + (lane >> 1)) * g.ldw;
+            const int at = 16 * s + 8 * (lane & 1);
+            sm[u][s] = inside ? (bf16x8) * (const bf16x8_any*)(row + at) : ln_columns(row, at, g.n);
+          } else {
+            sm[u][s] = *(const bf16x8_any*)(small[s] + k + 8 * q);
+          }
       }
     } else {
 #pragma unroll
@@ -121,7 +136,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_kernel(LinearArgs g
         for (int s = 0; s < SMALL; ++s) {
           if (TURN) {
             const int64_t kr = k + (lane >> 1);
-            sm[u][s] = *(const bf16x8*)(small[s] + (kr < k_end ? kr : k_end - 1) * g.ldw);
+            sm[u][s] = ln_columns((const bf16_t*)g.W + (kr < k_end ? kr : k_end - 1) * g.ldw, 16 * s + 8 * (lane & 1), g.n);
             if (kr >= k_end) sm[u][s] = (bf16x8){};
           } else {
             sm[u][s] = ln_load(small[s], k + 8 * q, k_end);
@@ -177,7 +192,8 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_t_kernel(LinearArgs
   __shared__ __attribute__((aligned(16))) unsigned char smem[LN_WAVES / 2 * QUADS * 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
-  const int64_t first = (int64_t)blockIdx.x * 128, col0 = first + 8 * c < g.n ? first + 8 * c : g.n - 8;
+  const int64_t first = (int64_t)blockIdx.x * 128, col0 = first + 8 * c;
+  const bool inside = first + 128 <= g.n;            // (uniform)
   const bf16_t* small[SMALL];
 #pragma unroll
   for (int s = 0; s < SMALL; ++s) small[s] = (const bf16_t*)g.X + (16 * s + c < g.m ? 16 * s + c : g.m - 1) * g.ldx;
@@ -193,7 +209,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_t_kernel(LinearArgs
       const bf16x8 sm = ln_rank_x(g, 16 * s + c < g.m ? 16 * s + c : g.m - 1, r0);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        acc[j][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ln_rank_w(g, col0 + j, r0), sm, acc[j][s], 0, 0, 0) * g.lora_scale;
+        acc[j][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ln_rank_w(g, col0 + j < g.n ? col0 + j : g.n - 1, r0), sm, acc[j][s], 0, 0, 0) * g.lora_scale;
     }
   }
   const int64_t k_beg0 = (int64_t)blockIdx.y * g.k_per_split, k_end0 = k_beg0 + g.k_per_split < g.k ? k_beg0 + g.k_per_split : g.k;
@@ -217,7 +233,8 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_t_kernel(LinearArgs
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t k = k0 + 8 * q + i;
-      v[i] = *(const u32x4_t*)((const bf16_t*)g.W + (whole || k < k_end ? k : k_end - 1) * g.ldw + col0);
+      const bf16_t* const row = (const bf16_t*)g.W + (whole || k < k_end ? k : k_end - 1) * g.ldw;
+      v[i] = __builtin_bit_cast(u32x4_t, inside ? (bf16x8) * (const bf16x8_any*)(row + col0) : ln_columns(row, col0, g.n));
       if (!whole && k >= k_end) v[i] = (u32x4_t){0u, 0u, 0u, 0u};
     }
 #pragma unroll
@@ -262,15 +279,12 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_t_kernel(LinearArgs
 
 // Which of the forms: 0 none, 1 rows of W are streamed, 2 rows of X, 3 W as it lies.
 static int linear_thin_form(int64_t m, int64_t n, int64_t k, bool w_kc) {
-  if (k % 8 || m > (1 << 27) || n > (1 << 27)) return 0;    // (2^32 threads to a grid)
-  if (m <= 32) return w_kc ? 1 : (n % 8 == 0 ? 3 : 0);
+  if (k < 8 || m > (1 << 27) || n > (1 << 27)) return 0;    // (2^32 threads to a grid)
+  if (m <= 32) return w_kc ? 1 : 3;
   // (33 to 64 outputs of many tokens: the tiles read W's columns once per 128 tokens; 8192 x 11008 -> 64 49 us against 67,
   // 2048 x 4096 -> 64 17 against 14)
-  if ((n <= 32 || (n <= 64 && m <= 4096)) && (w_kc || n % 8 == 0)) return 2;
+  if (n <= 32 || (n <= 64 && m <= 4096)) return 2;
   return 0;
-}
-static bool linear_thin_fits(const LinearArgs& g) {
-  return (uintptr_t)g.X % 16 == 0 && g.ldx % 8 == 0 && (uintptr_t)g.W % 16 == 0 && g.ldw % 8 == 0;
 }
 // Blocks of 16 streamed rows per wave: two where 32 rows still give every CU a workgroup, and for two blocks of tokens, whose X
 // would otherwise be read by twice as many workgroups (32 tokens through 4096 -> 11008: 36 us with one block of W's rows, 34 with two).

@@ -18,8 +18,9 @@ struct LinearArgs {
   const void* W;
   int64_t ldw;
   const void* T;         // m x r contiguous, or null
-  const void* B;         // r x n_out contiguous
+  const void* B;         // r x n_out contiguous (large tiles: rows of ldb)
   int64_t r;
+  int64_t ldb, b_n8, w_n8;   // large tiles: columns of B and of W as it lies that can be read, multiples of 8
   float lora_scale;
   int64_t m, n, k;       // tokens, outputs, inputs
   float* part;           // [split][m][n_pad] when the K range is split
