@@ -18,7 +18,7 @@ typedef f32x4 f32x4_any __attribute__((aligned(4)));
 
 // XCD b % 8 takes a run of consecutive tiles; within it tiles go in bands of LL_BAND tile rows, so that the tiles that are in
 // flight on one XCD share rows of X and of W in its L2.
-#define LL_BAND 8
+#define LL_BAND 4
 __device__ inline void ll_tile_of(int b, int tiles_m, int tiles_n, int* tm, int* tn) {
   const int total = tiles_m * tiles_n;
   const int xcd = b & 7, per = total >> 3, rest = total & 7;
@@ -439,8 +439,8 @@ static LargeSpace linear_large_space(const LargePlan& p, int64_t m, int64_t n, i
   q.total = off;
   return q;
 }
-// The copies read and write X and W once, the general tiles take twice the time: 8192 x 4095 -> 4096 251 us against 474, 2001 x 501 ->
-// 2001 19 / 26, 513 x 3001 -> 2001 29 / 34; 700 x 1030 -> 700 21 / 18, 100 x 4001 -> 4001 31 / 25.
+// The copies read and write X and W once, the general tiles take twice the time: 8192 x 4095 -> 4096 248 us against 444, 2001 x 501 ->
+// 2001 19 / 23, 513 x 3001 -> 2001 30 / 32; 700 x 1030 -> 700 20 / 16, 100 x 4001 -> 4001 31 / 23.
 static bool linear_large_pays(const LargeSpace& q, int64_t m, int64_t n) {
   return (!q.pad_x && !q.pad_w) || m * n >= (m + n) * 400;
 }

@@ -1,8 +1,8 @@
 // P = X W^T + s T B on tiles of 128 x 128 (128 x 64, 64 x 64): the form of loract_linear that takes every size, stride, alignment
 // and type.
 //
-// The slabs (128 bytes of K per row: 64 bf16 or 32 float32) pass through registers into a double-buffered LDS tile, two
-// slabs ahead of the one that is multiplied; the operands are those of gemm_bf16.h and their float32 counterparts below.
+// The slabs (64 of K of bf16, 16 of float32) pass through registers into a double-buffered LDS tile, two
+// slabs ahead of the one that is multiplied.
 // The low-rank term comes first: acc = T B, acc *= s, then the slabs of X W^T on top of it, so that it costs one
 // slab or two and its scale is applied in float32.  The products are formed transposed (the weights' fragment first), so that a lane holds
 // four consecutive columns of a row: one group of the dropout generator, one 8- or 16-byte store.
@@ -29,109 +29,104 @@ struct LinearArgs {
   LinEpilogue e;
 };
 
-// The float32 counterpart of GbOperand: R rows (or columns) of the output x 32 of K.
-__device__ inline f32x4 lf_load(const float* row, int64_t at, int64_t len) {
-  typedef f32x4 any __attribute__((aligned(4)));
-  if (len >= 4) return *(const any*)(row + (at + 4 <= len ? at : len - 4));
-  f32x4 v;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = at + e < len ? row[at + e] : 0.0f;
-  return v;
-}
-__device__ inline f32x4 lf_shift(f32x4 v, int64_t at, int64_t len) {
-  if (len < 4 || at + 4 <= len) return v;
-  const int64_t over = at + 4 - len;
-  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (over == 1) { o[0] = v[1]; o[1] = v[2]; o[2] = v[3]; }
-  if (over == 2) { o[0] = v[2]; o[1] = v[3]; }
-  if (over == 3) o[0] = v[3];
-  return o;
-}
+// One operand's share of a slab: R rows (or columns) of the output x BK of K, in pieces of 16 bytes at whatever address they have;
+// K-strided operands lie in LDS as in memory and are read transposed (bf16) or element by element (float32).
+// A piece that crosses the end of a row is loaded from the row's last whole piece and shifted, which also fills in the zeros.
+// TINY: rows may be shorter than a piece; they are read element by element.  (As a choice at run time this puts a branch around
+// every load, and the compiler a wait for the slabs in flight: 8192 x 1024 -> 4096 float32 608 us, without 568.)
+template <typename T, bool KC, int R, bool TINY>
+struct LinOperand {
+  static constexpr int E = 16 / sizeof(T);
+  static constexpr int BK = sizeof(T) == 2 ? 64 : 16, STEPS = sizeof(T) == 2 ? 4 : 2;
+  static constexpr int CPR = KC ? BK / E : R / E;  // pieces per row of the slab
+  static constexpr int BYTES = R * BK * (int)sizeof(T), NCH = BYTES / 16 / 256, RPP = 256 / CPR;      // rows per round of the 256 threads
+  typedef T piece __attribute__((ext_vector_type(E)));
+  typedef piece piece_any __attribute__((aligned(sizeof(T))));
+  typedef piece frag_t;
+  const T* base[KC ? NCH : 1];
+  int64_t ld;
+  int k_len, at, r0, len;                          // len: of a row
 
-template <bool KC, int R>
-struct LfOperand {
-  static constexpr int NCH = R / 32;
-  static constexpr int CPR = R / 4;                // K-strided: pieces per row of the slab
-  static constexpr int BYTES = R * 128;
-  const float* row[KC ? NCH : 1];
-  int64_t ld, k_len, col, n_len;
-  int lds_off[NCH], kr0;
-
-  __device__ void init(const float* P, int64_t ld_, const int32_t*, int64_t first, int64_t count, int64_t K, int t) {
+  __device__ void init(const T* P, int64_t ld_, int64_t first, int64_t count, int64_t K, int t) {
     ld = ld_;
-    k_len = K;
-    n_len = count;
+    k_len = (int)K;
+    r0 = t / CPR;
     if (KC) {
-      col = (t & 7) * 4;
+      at = t % CPR * E;
+      len = (int)K;
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
-        const int r = (t >> 3) + 32 * i;
-        int64_t g = first + r;
+        int64_t g = first + r0 + RPP * i;
         if (g > count - 1) g = count - 1;          // rows past the end are never stored
-        row[i] = P + g * ld;
-        lds_off[i] = r * 128 + (((t & 7) ^ (r & 7)) << 4);
+        base[i] = P + g * ld;
       }
     } else {
-      const int c = t % CPR;
-      kr0 = t / CPR;
-      col = first + c * 4;
-      row[0] = P;
-#pragma unroll
-      for (int i = 0; i < NCH; ++i) lds_off[i] = (kr0 + (256 / CPR) * i) * (R * 4) + c * 16;
+      len = (int)count;
+      at = (int)first + t % CPR * E;
+      base[0] = P;
     }
   }
-  __device__ void load(f32x4* v, int64_t k0, bool) const {
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      if (KC) {
-        v[i] = lf_load(row[i], k0 + col, k_len);
-      } else {
-        int64_t k = k0 + kr0 + (256 / CPR) * i;
-        if (k > k_len - 1) k = k_len - 1;
-        v[i] = lf_load(row[0] + k * ld, col < n_len ? col : n_len, n_len);
-      }
-    }
+  __device__ static int place(int r, int c) {      // of piece c of row r in LDS
+    if (sizeof(T) == 2) return KC ? r * 128 + ((c ^ (r & 7)) << 4) : r * (R * 2) + ((c ^ (2 * (r & 3))) << 4);
+    return KC ? r * 64 + ((c ^ ((r >> 2) & 3)) << 4) : r * (R * 4) + (c << 4);
   }
-  __device__ void put(const f32x4* v, unsigned char* lds, int64_t k0, bool edge, bool) const {
+  __device__ static piece load_piece(const T* row, int at, int len) {
+    if (!TINY) return *(const piece_any*)(row + (at < len - E ? at : len - E));
+    piece v;
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      f32x4 w = v[i];
-      if (edge) {
-        if (KC) {
-          w = lf_shift(w, k0 + col, k_len);
-        } else {
-          w = lf_shift(w, col < n_len ? col : n_len, n_len);
-          if (k0 + kr0 + (256 / CPR) * i >= k_len) w = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
-        }
-      }
-      *(f32x4*)(lds + lds_off[i]) = w;
-    }
-  }
-  __device__ static int frag_off(int base, int lane) {
-    if (KC) return (base + (lane & 31)) * 128;
-    return 4 * (lane >> 5) * (R * 4) + (base + (lane & 31)) * 4;
-  }
-  // the four k of this lane in step ks: 8 ks + 4 (lane / 32) ..
-  __device__ static f32x4 frag(const unsigned char* lds, int off, int ks, int lane) {
-    if (KC) return *(const f32x4*)(lds + off + (((2 * ks + (lane >> 5)) ^ (lane & 7)) << 4));
-    f32x4 v;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = *(const float*)(lds + off + (8 * ks + j) * (R * 4));
+    for (int e = 0; e < E; ++e) v[e] = at + e < len ? row[at + e] : (T)0.0f;
     return v;
+  }
+  __device__ static piece shift(piece v, int at, int len) {
+    if (TINY || at + E <= len) return v;
+    const int over = at + E - len;
+    if (over >= E) return (piece){};
+    return __builtin_bit_cast(piece, __builtin_bit_cast(unsigned __int128, v) >> (8 * (int)sizeof(T) * over));
+  }
+  __device__ void load(piece* v, int k0) const {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int k = k0 + r0 + RPP * i;
+      v[i] = KC ? load_piece(base[KC ? i : 0], k0 + at, len) : load_piece(base[0] + (int64_t)(k < k_len ? k : k_len - 1) * ld, at, len);
+    }
+  }
+  // `edge`: the slab or the tile touches the end of the matrix (uniform)
+  __device__ void put(const piece* v, unsigned char* lds, int k0, bool edge) const {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      piece w = v[i];
+      if (edge) {
+        w = shift(w, KC ? k0 + at : at, len);
+        if (!KC && k0 + r0 + RPP * i >= k_len) w = (piece){};
+      }
+      *(piece*)(lds + place(r0 + RPP * i, KC ? at / E : threadIdx.x % CPR)) = w;
+    }
+  }
+  // fragment address of a 32-wide group that starts at row (or column) `base` of the tile
+  __device__ static int frag_off(int base, int lane) {
+    if (KC) return (base + (lane & 31)) * (BK * (int)sizeof(T));
+    if (sizeof(T) == 4) return 4 * (lane >> 5) * (R * 4) + (base + (lane & 31)) * 4;
+    const int s16 = lane & 15, c = base + 16 * ((lane >> 4) & 1) + 4 * (s16 & 3);
+    return (8 * (lane >> 5) + (s16 >> 2)) * (R * 2) + (((c >> 3) ^ (2 * (s16 >> 2))) << 4) + (c & 7) * 2;
+  }
+  // bf16: the eight k 16 ks + 8 (lane / 32) ..; float32: the four k 8 ks + 4 (lane / 32) ..
+  __device__ static piece frag(const unsigned char* lds, int off, int ks, int lane) {
+    if constexpr (KC) {
+      return *(const piece*)(lds + off + (((2 * ks + (lane >> 5)) ^ (sizeof(T) == 2 ? lane & 7 : (lane >> 2) & 3)) << 4));
+    } else if constexpr (sizeof(T) == 2) {
+      typedef __attribute__((address_space(3))) gb_s16x4* lds_ptr;
+      const gb_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds + off + 16 * ks * (R * 2)));
+      const gb_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds + off + (16 * ks + 4) * (R * 2)));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      piece v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = *(const float*)(lds + off + (8 * ks + j) * (R * 4));
+      return v;
+    }
   }
 };
 
-template <typename T, bool KC, int R> struct LinOperand;
-template <bool KC, int R> struct LinOperand<bf16_t, KC, R> {
-  typedef GbOperand<KC, R> type;
-  typedef gb_u32x4 piece;
-  typedef bf16x8 frag;
-};
-template <bool KC, int R> struct LinOperand<float, KC, R> {
-  typedef LfOperand<KC, R> type;
-  typedef f32x4 piece;
-  typedef f32x4 frag;
-};
 // One step of a wave's MT x NT products.  float32: the k in turn for all of them, so that a product does not wait for the one before.
 template <int MT, int NT>
 __device__ inline void lin_multiply(const bf16x8 (&w)[NT], const bf16x8 (&x)[MT], f32x16 (&acc)[MT][NT]) {
@@ -150,23 +145,26 @@ __device__ inline void lin_multiply(const f32x4 (&w)[NT], const f32x4 (&x)[MT], 
       for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[j][e], x[i][e], acc[i][j], 0, 0, 0);
 }
 
+// TINY: K, or the rows of W stored n_in x n_out, are shorter than a piece (the low-rank term's always may be).
 // WKC: W is n_out x n_in (rows along K), else n_in x n_out.  BM x BN tile, four waves of BM/2 x BN/2; blockIdx.z: split of K.
-template <typename T, bool WKC, int BM, int BN>
+template <typename T, bool WKC, int BM, int BN, bool TINY>
 __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
-  constexpr int MT = BM / 64, NT = BN / 64, BK = 128 / (int)sizeof(T);
-  typedef typename LinOperand<T, true, BM>::type OpX;
-  typedef typename LinOperand<T, WKC, BN>::type OpW;
-  typedef typename LinOperand<T, false, BN>::type OpB;
-  typedef typename LinOperand<T, true, BM>::piece piece;
-  typedef typename LinOperand<T, true, BM>::frag frag_t;
+  typedef LinOperand<T, true, BM, TINY> OpX;
+  typedef LinOperand<T, WKC, BN, TINY> OpW;
+  typedef LinOperand<T, true, BM, true> OpT;
+  typedef LinOperand<T, false, BN, true> OpB;
+  constexpr int MT = BM / 64, NT = BN / 64, BK = OpX::BK, STEPS = OpX::STEPS;
+  typedef typename OpX::piece piece;
+  typedef piece frag_t;
   constexpr int STAGE = OpX::BYTES + OpW::BYTES;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[2 * STAGE];
+  constexpr int OUT = 4 * 32 * (BN / 2 + 4) * 4;     // staging of the output
+  __shared__ __attribute__((aligned(16))) unsigned char smem[2 * STAGE > OUT ? 2 * STAGE : OUT];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int wm = wave >> 1, wn = wave & 1;
   const int64_t row0 = (int64_t)blockIdx.x * BM, col0 = (int64_t)blockIdx.y * BN;
-  const int64_t kbeg = (int64_t)blockIdx.z * g.k_per_split;
-  const int64_t kend = (kbeg + g.k_per_split < g.k) ? kbeg + g.k_per_split : g.k;
-  const int nslab = (int)((kend - kbeg + BK - 1) / BK);
+  const int kbeg = (int)(blockIdx.z * g.k_per_split);
+  const int kend = (int)(kbeg + g.k_per_split < g.k ? kbeg + g.k_per_split : g.k);
+  const int nslab = (kend - kbeg + BK - 1) / BK;
   int x_off[MT], w_off[NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) x_off[i] = OpX::frag_off(wm * (BM / 2) + 32 * i, lane);
@@ -182,19 +180,19 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
   if (g.T && blockIdx.z == 0) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) w_off[j] = OpX::BYTES + OpB::frag_off(wn * (BN / 2) + 32 * j, lane);
-    OpX ot;
+    OpT ot;
     OpB ob;
-    ot.init((const T*)g.T, g.r, nullptr, row0, g.m, g.r, t);
-    ob.init((const T*)g.B, g.n, nullptr, col0, g.n, g.r, t);
-    for (int64_t k0 = 0; k0 < g.r; k0 += BK) {
-      piece vt[OpX::NCH], vb[OpB::NCH];
-      ot.load(vt, k0, false);
-      ob.load(vb, k0, false);
-      ot.put(vt, smem, k0, true, false);
-      ob.put(vb, smem + OpX::BYTES, k0, true, false);
+    ot.init((const T*)g.T, g.r, row0, g.m, g.r, t);
+    ob.init((const T*)g.B, g.n, col0, g.n, g.r, t);
+    for (int k0 = 0; k0 < (int)g.r; k0 += BK) {
+      piece vt[OpT::NCH], vb[OpB::NCH];
+      ot.load(vt, k0);
+      ob.load(vb, k0);
+      ot.put(vt, smem, k0, true);
+      ob.put(vb, smem + OpX::BYTES, k0, true);
       sb_barrier_lds();
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
+      for (int ks = 0; ks < STEPS; ++ks) {
         frag_t x[MT], w[NT];
 #pragma unroll
         for (int i = 0; i < MT; ++i) x[i] = OpX::frag(smem, x_off[i], ks, lane);
@@ -214,27 +212,27 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
 
   OpX ox;
   OpW ow;
-  ox.init((const T*)g.X, g.ldx, nullptr, row0, g.m, g.k, t);
-  ow.init((const T*)g.W, g.ldw, nullptr, col0, g.n, g.k, t);
+  ox.init((const T*)g.X, g.ldx, row0, g.m, g.k, t);
+  ow.init((const T*)g.W, g.ldw, col0, g.n, g.k, t);
 #pragma unroll
   for (int j = 0; j < NT; ++j) w_off[j] = OpX::BYTES + OpW::frag_off(wn * (BN / 2) + 32 * j, lane);
   const bool tile_edge = !WKC && col0 + BN > g.n;
   piece vx[2][OpX::NCH], vw[2][OpW::NCH];
   auto fetch = [&](int p, int s) {                 // slabs past the last one repeat it and are not multiplied
-    const int64_t k0 = kbeg + (int64_t)(s < nslab ? s : nslab - 1) * BK;
-    ox.load(vx[p], k0, false);
-    ow.load(vw[p], k0, false);
+    const int k0 = kbeg + (s < nslab ? s : nslab - 1) * BK;
+    ox.load(vx[p], k0);
+    ow.load(vw[p], k0);
   };
   auto step = [&](int p, int s) {
-    const int64_t k0 = kbeg + (int64_t)s * BK;
+    const int k0 = kbeg + s * BK;
     unsigned char* st = smem + p * STAGE;
-    const bool edge = tile_edge || k0 + BK > g.k;
-    ox.put(vx[p], st, k0, edge, false);
-    ow.put(vw[p], st + OpX::BYTES, k0, edge, false);
+    const bool edge = tile_edge || k0 + BK > (int)g.k;
+    ox.put(vx[p], st, k0, edge);
+    ow.put(vw[p], st + OpX::BYTES, k0, edge);
     sb_barrier_lds();                              // (the half of slab s - 2 was left before slab s - 1's barrier)
     fetch(p, s + 2);
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
+    for (int ks = 0; ks < STEPS; ++ks) {
       frag_t x[MT], w[NT];
 #pragma unroll
       for (int i = 0; i < MT; ++i) x[i] = OpX::frag(st, x_off[i], ks, lane);
@@ -252,7 +250,6 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
   // Accumulator register 4 q + u of lane l: column 8 q + 4 (l / 32) + u, row l % 32 of its tile.  They leave 32 rows at a time through LDS, so
   // that neighbouring lanes hold neighbouring columns, with all loads of the residual ahead.
   constexpr int PART = BN / 2, LDC = PART + 4, QPR = PART / 4, ROWS = 64 / QPR, N4 = 32 / ROWS;
-  static_assert(4 * 32 * LDC * 4 <= 2 * STAGE, "staging of the output");
   sb_barrier_lds();                                // the last slab has been read
   float* const cs = (float*)(smem + wave * (32 * LDC * 4));
   const int c4 = lane % QPR * 4, r0 = lane / QPR;
@@ -318,8 +315,11 @@ static int launch_linear_join(hipStream_t s, const LinearArgs& g, int splits) {
 template <typename T>
 static int launch_linear_tile(hipStream_t s, LinearArgs g, bool w_kc) {
   constexpr bool BF = sizeof(T) == 2;
-  constexpr int BK = 128 / (int)sizeof(T);
-  const TilePlan p = linear_tile_plan(g.m, g.n, g.k, BF);
+  constexpr int BK = LinOperand<T, true, 64, false>::BK;
+  constexpr int E = 16 / (int)sizeof(T);
+  const bool tiny = g.k < E || (!w_kc && g.n < E);
+  TilePlan p = linear_tile_plan(g.m, g.n, g.k, BF);
+  if (tiny) p.bm = p.bn = 64;
   const int bm = p.bm, bn = p.bn;
   int splits = p.splits;
   g.k_per_split = ceil_div64(ceil_div64(g.k, splits), BK) * BK;
@@ -327,15 +327,17 @@ static int launch_linear_tile(hipStream_t s, LinearArgs g, bool w_kc) {
   g.n_pad = (int64_t)align_up((size_t)g.n, 4);
   const dim3 grid((unsigned)ceil_div64(g.m, bm), (unsigned)ceil_div64(g.n, bn), (unsigned)splits);
   if (grid.y > 65535) return LORACT_ERR_UNSUPPORTED;
-#define LT_LAUNCH(WKC, BM, BN) LORACT_LAUNCH("linear_tile", s, (linear_tile_kernel<T, WKC, BM, BN>), grid, dim3(256), 0, g)
+#define LT_LAUNCH(WKC, BM, BN, TINY) LORACT_LAUNCH("linear_tile", s, (linear_tile_kernel<T, WKC, BM, BN, TINY>), grid, dim3(256), 0, g)
   if (w_kc) {
-    if (bm == 64) LT_LAUNCH(true, 64, 64);
-    else if (bn == 64) LT_LAUNCH(true, 128, 64);
-    else LT_LAUNCH(true, 128, 128);
+    if (tiny) LT_LAUNCH(true, 64, 64, true);
+    else if (bm == 64) LT_LAUNCH(true, 64, 64, false);
+    else if (bn == 64) LT_LAUNCH(true, 128, 64, false);
+    else LT_LAUNCH(true, 128, 128, false);
   } else {
-    if (bm == 64) LT_LAUNCH(false, 64, 64);
-    else if (bn == 64) LT_LAUNCH(false, 128, 64);
-    else LT_LAUNCH(false, 128, 128);
+    if (tiny) LT_LAUNCH(false, 64, 64, true);
+    else if (bm == 64) LT_LAUNCH(false, 64, 64, false);
+    else if (bn == 64) LT_LAUNCH(false, 128, 64, false);
+    else LT_LAUNCH(false, 128, 128, false);
   }
 #undef LT_LAUNCH
   return splits > 1 ? launch_linear_join<T>(s, g, splits) : LORACT_OK;

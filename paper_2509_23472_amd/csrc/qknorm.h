@@ -102,6 +102,7 @@ __global__ __launch_bounds__(64 * QK_WAVES) void qknorm_rope_kernel(QkArgs g) {
       piece x[U], dy[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
+        if (h0 + u * HPW >= h_end) break;            // (uniform)
         int h = h0 + u * HPW + sub;
         if (h > h_end - 1) h = h_end - 1;            // heads past the end repeat the last one and are not stored
         const int a = on ? at : 0;
@@ -110,6 +111,7 @@ __global__ __launch_bounds__(64 * QK_WAVES) void qknorm_rope_kernel(QkArgs g) {
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
+        if (h0 + u * HPW >= h_end) break;
         const int h = h0 + u * HPW + sub;
         const bool store = on && h < h_end;
         float v[E], t[E];
