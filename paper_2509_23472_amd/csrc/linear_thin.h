@@ -10,19 +10,10 @@
 
 #define LN_WAVES 8
 
-// Rows may start anywhere: pieces of eight elements are read at whatever address they have.
+// Rows along K may start at any multiple of 4 bytes.
 // Eight consecutive k of a row along K, zero past the end of K (k_len >= 8).
 __device__ inline bf16x8 ln_load(const bf16_t* row, int64_t k, int64_t k_len) {
   return __builtin_bit_cast(bf16x8, gb_shift(gb_load(row, k < k_len ? k : k_len, k_len), k < k_len ? k : k_len, k_len));
-}
-// Eight consecutive columns from `col` on of a row of n columns.
-__device__ inline bf16x8 ln_columns(const bf16_t* row, int64_t col, int64_t n) {
-  if (col + 8 <= n) return *(const bf16x8_any*)(row + col);
-  bf16x8 v = {};
-#pragma unroll
-  for (int u = 0; u < 8; ++u)
-    if (col + u < n) v[u] = row[col + u];
-  return v;
 }
 // Fragment of T (row `row`) or of B (column `col`), 32 of the rank from r0 on.
 __device__ inline bf16x8 ln_rank_x(const LinearArgs& g, int64_t row, int r0) {
@@ -66,7 +57,6 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_kernel(LinearArgs g
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
   const int64_t first = (int64_t)blockIdx.x * (16 * BLOCKS);
-  const bool inside = g.n >= 16 * SMALL;                 // (uniform; of the columns that TURN reads)
   const int64_t rows = OF_W ? g.n : g.m, others = OF_W ? g.m : g.n;
   const bf16_t *stream[BLOCKS], *small[SMALL];
 #pragma unroll
@@ -77,7 +67,8 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_kernel(LinearArgs g
 #pragma unroll
   for (int b = 0; b < SMALL; ++b) {
     const int64_t row = 16 * b + c < others ? 16 * b + c : others - 1;
-    small[b] = OF_W ? (const bf16_t*)g.X + row * g.ldx : (const bf16_t*)g.W + row * g.ldw;
+    if (TURN) small[b] = (const bf16_t*)g.W + (16 * b + 8 * (lane & 1) < g.n ? 16 * b + 8 * (lane & 1) : 0);   // (n is a multiple of 8)
+    else small[b] = OF_W ? (const bf16_t*)g.X + row * g.ldx : (const bf16_t*)g.W + row * g.ldw;
   }
   f32x4 acc[BLOCKS][SMALL];
 #pragma unroll
@@ -118,13 +109,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_kernel(LinearArgs g
         for (int b = 0; b < BLOCKS; ++b) st[u][b] = *(const bf16x8_any*)(stream[b] + k + 8 * q);
 #pragma unroll
         for (int s = 0; s < SMALL; ++s)
-          if (TURN) {
-            const bf16_t* const row = (const bf16_t*)g.W + (k + (lane >> 1)) * g.ldw;
-            const int at = 16 * s + 8 * (lane & 1);
-            sm[u][s] = inside ? (bf16x8) * (const bf16x8_any*)(row + at) : ln_columns(row, at, g.n);
-          } else {
-            sm[u][s] = *(const bf16x8_any*)(small[s] + k + 8 * q);
-          }
+          sm[u][s] = TURN ? *(const bf16x8*)(small[s] + (k + (lane >> 1)) * g.ldw) : *(const bf16x8_any*)(small[s] + k + 8 * q);
       }
     } else {
 #pragma unroll
@@ -136,7 +121,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_kernel(LinearArgs g
         for (int s = 0; s < SMALL; ++s) {
           if (TURN) {
             const int64_t kr = k + (lane >> 1);
-            sm[u][s] = ln_columns((const bf16_t*)g.W + (kr < k_end ? kr : k_end - 1) * g.ldw, 16 * s + 8 * (lane & 1), g.n);
+            sm[u][s] = *(const bf16x8*)(small[s] + (kr < k_end ? kr : k_end - 1) * g.ldw);
             if (kr >= k_end) sm[u][s] = (bf16x8){};
           } else {
             sm[u][s] = ln_load(small[s], k + 8 * q, k_end);
@@ -192,8 +177,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_t_kernel(LinearArgs
   __shared__ __attribute__((aligned(16))) unsigned char smem[LN_WAVES / 2 * QUADS * 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
-  const int64_t first = (int64_t)blockIdx.x * 128, col0 = first + 8 * c;
-  const bool inside = first + 128 <= g.n;            // (uniform)
+  const int64_t first = (int64_t)blockIdx.x * 128, col0 = first + 8 * c < g.n ? first + 8 * c : g.n - 8;   // (n is a multiple of 8)
   const bf16_t* small[SMALL];
 #pragma unroll
   for (int s = 0; s < SMALL; ++s) small[s] = (const bf16_t*)g.X + (16 * s + c < g.m ? 16 * s + c : g.m - 1) * g.ldx;
@@ -209,7 +193,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_t_kernel(LinearArgs
       const bf16x8 sm = ln_rank_x(g, 16 * s + c < g.m ? 16 * s + c : g.m - 1, r0);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        acc[j][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ln_rank_w(g, col0 + j < g.n ? col0 + j : g.n - 1, r0), sm, acc[j][s], 0, 0, 0) * g.lora_scale;
+        acc[j][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ln_rank_w(g, col0 + j, r0), sm, acc[j][s], 0, 0, 0) * g.lora_scale;
     }
   }
   const int64_t k_beg0 = (int64_t)blockIdx.y * g.k_per_split, k_end0 = k_beg0 + g.k_per_split < g.k ? k_beg0 + g.k_per_split : g.k;
@@ -233,8 +217,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_t_kernel(LinearArgs
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t k = k0 + 8 * q + i;
-      const bf16_t* const row = (const bf16_t*)g.W + (whole || k < k_end ? k : k_end - 1) * g.ldw;
-      v[i] = __builtin_bit_cast(u32x4_t, inside ? (bf16x8) * (const bf16x8_any*)(row + col0) : ln_columns(row, col0, g.n));
+      v[i] = *(const u32x4_t*)((const bf16_t*)g.W + (whole || k < k_end ? k : k_end - 1) * g.ldw + col0);
       if (!whole && k >= k_end) v[i] = (u32x4_t){0u, 0u, 0u, 0u};
     }
 #pragma unroll
@@ -277,15 +260,18 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_t_kernel(LinearArgs
   }
 }
 
-// Which of the forms: 0 none, 1 rows of W are streamed, 2 rows of X, 3 W as it lies.
-static int linear_thin_form(int64_t m, int64_t n, int64_t k, bool w_kc) {
+// Which of the forms: 0 none, 1 rows of W are streamed, 2 rows of X, 3 W as it lies.  Rows along K at multiples of 4 bytes, W as it
+// lies in whole pieces: at 2 bytes the general tiles are faster (one token through 4095 -> 11007 44 us against 31, 8192 x 4095 -> 16 31
+// against 21), at 8 they are not (one token through 4092 -> 11008 20 against 27); W as it lies at 8 bytes 53 against 32.
+static int linear_thin_form(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw, bool w_kc) {
   if (k < 8 || m > (1 << 27) || n > (1 << 27)) return 0;    // (2^32 threads to a grid)
+  if (ldx % 2 || (w_kc ? ldw % 2 : (ldw % 8 || n % 8))) return 0;
   if (m <= 32) return w_kc ? 1 : 3;
   // (33 to 64 outputs of many tokens: the tiles read W's columns once per 128 tokens; 8192 x 11008 -> 64 49 us against 67,
   // 2048 x 4096 -> 64 17 against 14)
-  if (n <= 32 || (n <= 64 && m <= 4096)) return 2;
-  return 0;
+  return n <= 32 || (n <= 64 && m <= 4096) ? 2 : 0;
 }
+static bool linear_thin_fits(const LinearArgs& g, bool w_kc) { return (uintptr_t)g.X % 4 == 0 && (uintptr_t)g.W % (w_kc ? 4 : 16) == 0; }
 // Blocks of 16 streamed rows per wave: two where 32 rows still give every CU a workgroup, and for two blocks of tokens, whose X
 // would otherwise be read by twice as many workgroups (32 tokens through 4096 -> 11008: 36 us with one block of W's rows, 34 with two).
 static int linear_thin_blocks(int64_t m, int form) { return form == 1 ? (m > 16 ? 2 : 1) : (ceil_div64(m, 32) >= 256 ? 2 : 1); }
@@ -298,14 +284,12 @@ static int linear_thin_splits(int64_t m, int64_t n, int64_t k, int form) {
   const int64_t want = std::max<int64_t>(256 / wgs, form == 3 && m <= 16 ? 4 : 1);
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, k / 1024), 64));
 }
-static size_t linear_thin_part_bytes(int64_t m, int64_t n, int64_t k, bool w_kc) {
-  const int form = linear_thin_form(m, n, k, w_kc);
-  const int s = form ? linear_thin_splits(m, n, k, form) : 1;
-  return s > 1 ? (size_t)s * m * align_up((size_t)n, 4) * 4 : 0;
+static size_t linear_thin_part_bytes(int64_t m, int64_t n, int64_t k, int form) {
+  const int s = linear_thin_splits(m, n, k, form);
+  return s > 1 ? align_up((size_t)s * m * align_up((size_t)n, 4) * 4, 256) : 0;
 }
 
-static int launch_linear_thin(hipStream_t s, LinearArgs g, bool w_kc) {
-  const int form = linear_thin_form(g.m, g.n, g.k, w_kc);
+static int launch_linear_thin(hipStream_t s, LinearArgs g, bool w_kc, int form) {
   int splits = linear_thin_splits(g.m, g.n, g.k, form);
   g.k_per_split = ceil_div64(ceil_div64(g.k, splits), 256) * 256;
   splits = (int)ceil_div64(g.k, g.k_per_split);
