@@ -54,13 +54,10 @@ int loract_linear_workspace_bytes(const loract_linear_params* p, size_t* bytes) 
   LORACT_TRY(check_linear_forward(p));
   const bool bf16 = p->dtype == LORACT_BF16;
   *bytes = align_up(linear_tile_part_bytes(p->m, p->n_out, p->n_in, bf16), 256);
-  if (!bf16) return LORACT_OK;
   const bool w_kc = p->w_layout == LORACT_W_OUT_IN;                   // (whichever form the call's addresses allow)
-  const int form = linear_thin_form(p->m, p->n_out, p->n_in, p->ldx, p->ldw, w_kc);
-  if (form) {
-    *bytes = std::max(*bytes, linear_thin_part_bytes(p->m, p->n_out, p->n_in, form));
-    return LORACT_OK;
-  }
+  const int form = linear_thin_form(p->m, p->n_out, p->n_in, p->ldx, p->ldw, w_kc, bf16);
+  if (form) *bytes = std::max(*bytes, linear_thin_part_bytes(p->m, p->n_out, p->n_in, form, bf16));
+  if (form || !bf16) return LORACT_OK;
   const LargePlan plan = linear_large_plan(p->m, p->n_out, p->n_in);
   const LargeSpace space = linear_large_space(plan, p->m, p->n_out, p->n_in, p->r_lora, p->ldx, p->ldw, w_kc);
   if (plan.tile && linear_large_pays(space, p->m, p->n_out)) *bytes = std::max(*bytes, space.total);
@@ -90,12 +87,13 @@ int loract_linear(const void* X_dev, const void* W_dev, const float* bias_dev, c
   const size_t quad = bf16 ? 8 : 16;
   e.vec = p->n_out % 4 == 0 && aligned_rows(R_dev, p->ldr, 4, quad) && aligned_rows(Z_dev, p->ldz, 4, quad) &&
           aligned_rows(Y_dev, p->ldy, 4, e.y_f32 ? 16 : 8);
-  if (bf16) {
-    const int form = linear_thin_form(g.m, g.n, g.k, g.ldx, g.ldw, w_kc);
-    if (form && linear_thin_fits(g, w_kc)) return launch_linear_thin((hipStream_t)stream, g, w_kc, form);
+  const int form = linear_thin_form(g.m, g.n, g.k, g.ldx, g.ldw, w_kc, bf16);
+  if (form && linear_thin_fits(g, w_kc))
+    return bf16 ? launch_linear_thin<bf16_t>((hipStream_t)stream, g, w_kc, form) : launch_linear_thin<float>((hipStream_t)stream, g, w_kc, form);
+  if (bf16 && !form) {
     const LargePlan plan = linear_large_plan(g.m, g.n, g.k);
     const LargeSpace space = linear_large_space(plan, g.m, g.n, g.k, p->r_lora, g.ldx, g.ldw, w_kc);
-    if (!form && plan.tile && linear_large_pays(space, g.m, g.n) && linear_large_fits(g, w_kc, space))
+    if (plan.tile && linear_large_pays(space, g.m, g.n) && linear_large_fits(g, w_kc, space))
       return launch_linear_large((hipStream_t)stream, g, w_kc, plan, space);
   }
   return bf16 ? launch_linear_tile<bf16_t>((hipStream_t)stream, g, w_kc) : launch_linear_tile<float>((hipStream_t)stream, g, w_kc);

@@ -105,6 +105,17 @@ def test_thin_products(m, n_in, n_out, parts, layout):
     _case(m, n_in, n_out, layout=layout, **parts)
 
 
+@pytest.mark.parametrize("layout", ["nt", "nn"])
+@pytest.mark.parametrize("m,n_in,n_out,parts", [
+    (1, 8, 4, dict()), (1, 9, 12, dict(r=3)), (1, 4101, 132, dict(r=64, act="silu", bias=True, keep=True)), (7, 1027, 260, dict(r=33, residual=True)),
+    (16, 260, 1000, dict(p=0.2, act="gelu")), (17, 517, 516, dict(r=16, keep=True)), (32, 72, 4096, dict(r=8, residual=True, p=0.1)),
+    (32, 5003, 44, dict(act="relu", r=48)), (2, 32, 5, dict()), (300, 267, 16, dict(r=16)), (333, 1031, 8, dict(act="silu", bias=True)),
+    (9000, 101, 28, dict(r=7, p=0.1)), (8200, 256, 32, dict(keep=True, act="gelu", r=64)), (70, 4099, 20, dict(pad=4, shift=8, residual=True)),
+    (100, 640, 17, dict(pad=3, shift=1, r=5)), (4, 512, 128, dict(pad=12, shift=4, r=12, act="silu", keep=True))])
+def test_thin_products_of_float32(m, n_in, n_out, parts, layout):
+    _case(m, n_in, n_out, dtype="f32", layout=layout, **parts)
+
+
 def test_large_tiles_keep_nan_and_infinity_where_they_belong():
     for layout in ("nt", "nn"):
         def poison(x, w):
