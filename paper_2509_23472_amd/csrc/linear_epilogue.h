@@ -7,10 +7,10 @@
 // The activations and their slopes: exp and the reciprocal by the hardware's instructions (both within one unit), and Phi from
 //   erfc(x) = q(t) exp(-x^2),  t = 1 / (1 + 0.4 x),  x >= 0,
 // q a polynomial fitted here to the least relative error (1.4e-7, 4e-7 evaluated in float32).  EXACT (float32 inputs): the
-// rounding of exp's argument is made good and the reciprocal takes a Newton step, which leaves 4e-7; without, bf16 inputs lose up to
-// 2^-20, far below their last rounding.  A fifth of the instructions of erff, expf and a division, which an epilogue has nothing to hide
+// rounding of exp's argument is made good, the reciprocal takes a Newton step and SiLU divides, which leaves 4e-7; without, bf16 inputs
+// lose up to 2^-20, far below their last rounding.  A fifth of the instructions of erff, expf and a division, which an epilogue has nothing to hide
 // behind: 8192 x 4096 -> 11008 with SiLU 747 us with those and 685 so (642 without an activation), the backward of 8192 x 11008 SiLU
-// 169 and 123, GELU 215 and 131, of 12608 x 768 float32 GELU 38 and 33.
+// 169 and 123, GELU 215 and 131, of 12608 x 768 float32 GELU 38 and 33 (SiLU's division: 32.6 us, 32.0 with the reciprocal).
 template <bool EXACT>
 __device__ inline float lin_exp(float x) {
   constexpr float L = 1.44269504088896341f, L_REST = 1.92596299112661746e-8f;      // log2(e) and what its rounding leaves
@@ -18,15 +18,20 @@ __device__ inline float lin_exp(float x) {
   const float e = __builtin_amdgcn_exp2f(t);
   if (!EXACT) return e;
   const float rest = fmaf(x, L_REST, fmaf(x, L, -t));                              // (not a number where t overflows)
-  return fabsf(t) < 150.0f ? fmaf(e, 0.693147180559945309f * rest, e) : e;
+  return t > -150.0f && t < 128.0f ? fmaf(e, 0.693147180559945309f * rest, e) : e;  // (from 128 on e is infinite: nothing to make good)
 }
 template <bool EXACT>
 __device__ inline float lin_reciprocal(float x) {                                  // x >= 1
   const float r = __builtin_amdgcn_rcpf(x);
   return EXACT && x < 0x1p120f ? fmaf(fmaf(-x, r, 1.0f), r, r) : r;
 }
+// 1 / (1 + exp(-z)) and z times it.  EXACT: by a division, since the reciprocal's instruction makes zero of what is below 2^-126 (z < -87.3),
+// of which z times as much need not be.
 template <bool EXACT>
-__device__ inline float lin_sigmoid(float z) { return lin_reciprocal<EXACT>(1.0f + lin_exp<EXACT>(-z)); }
+__device__ inline float lin_sigmoid(float z, float times) {
+  const float below = 1.0f + lin_exp<EXACT>(-z);
+  return EXACT ? times / below : times * lin_reciprocal<EXACT>(below);
+}
 // Phi(z); *density: exp(-z^2 / 2)
 template <bool EXACT>
 __device__ inline float lin_phi(float z, float* density) {
@@ -52,7 +57,7 @@ __device__ inline float lin_act(int act, float z) {
       float density;
       return z * lin_phi<EXACT>(z, &density);
     }
-    case LORACT_ACT_SILU: return z * lin_sigmoid<EXACT>(z);
+    case LORACT_ACT_SILU: return lin_sigmoid<EXACT>(z, z);
     default: return z;
   }
 }
@@ -66,7 +71,7 @@ __device__ inline float lin_act_slope(int act, float z) {
       return phi + z * (density * 0.39894228040143268f);
     }
     case LORACT_ACT_SILU: {
-      const float s = lin_sigmoid<EXACT>(z);
+      const float s = lin_sigmoid<EXACT>(z, 1.0f);
       return s * (1.0f + z * (1.0f - s));
     }
     default: return 1.0f;
