@@ -64,7 +64,11 @@ _workspaces: Dict[Tuple[int, int], torch.Tensor] = {}
 
 
 def _workspace(nbytes: int, device: torch.device) -> torch.Tensor:
-    """A cached uint8 device buffer of at least `nbytes` (grown on demand, never shrunk)."""
+    """A uint8 device buffer of at least `nbytes`, to be held until the call that takes it has been enqueued: the stream's cached one
+    (grown on demand, never shrunk), or while the stream is being captured one of the graph's own memory.  The cached one
+    is replaced when it grows and is the eager calls', and replays use the address that they were captured with."""
+    if torch._C._cuda_isCurrentStreamCapturing():
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
     key = (device.index if device.index is not None else torch.cuda.current_device(), _stream_ptr())
     ws = _workspaces.get(key)
     if ws is None or ws.numel() < nbytes:
@@ -354,18 +358,16 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _scratch(query, where: str, params: bytes, t: torch.Tensor, stream: int) -> Tuple[Optional[int], int]:
-    """Workspace (pointer, bytes) for a call with these parameters on the stream."""
+def _scratch(query, where: str, params: bytes, t: torch.Tensor) -> Tuple[Optional[torch.Tensor], Optional[int], int]:
+    """Workspace for a call with these parameters (what holds it, pointer, bytes)."""
     nbytes = ctypes.c_size_t()
     code = query(params, ctypes.byref(nbytes))
     if code:
         raise LoractError(code, where)
     if not nbytes.value:
-        return None, 0
-    ws = _workspaces.get((t.get_device(), stream))
-    if ws is None or ws.numel() < nbytes.value:
-        ws = _workspace(nbytes.value, t.device)
-    return ws.data_ptr(), ws.numel()
+        return None, None, 0
+    ws = _workspace(nbytes.value, t.device)
+    return ws, ws.data_ptr(), ws.numel()
 
 
 def _act_code(act: str) -> int:
@@ -434,7 +436,7 @@ def loract_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor]
         params = _LINEAR_PARAMS.pack(m, n_in, n_out, ldx, ldw, ldr, ldy, n_out, 0, _dtype_code(dt), _dtype_code(odt),
                                      W_IN_OUT if w_transposed else W_OUT_IN, _act_code(act), r, lora_scale, p_drop, seed & _SEED)
         lib, stream = _lib.load(), _stream_ptr()
-        ws, size = _scratch(lib.loract_linear_workspace_bytes, "loract_linear_workspace_bytes", params, x, stream)
+        held, ws, size = _scratch(lib.loract_linear_workspace_bytes, "loract_linear_workspace_bytes", params, x)
         code = lib.loract_linear(x.data_ptr(), w.data_ptr(), bias_ptr, t_ptr, b_ptr, r_ptr, params, out.data_ptr(), _ptr(z), ws,
                                  size, stream)
         if code:
@@ -474,9 +476,9 @@ def loract_linear_backward(dy: torch.Tensor, z: Optional[torch.Tensor] = None, *
         return out, db if db is None else db.zero_(), d_b if d_b is None else d_b.zero_()
     params = _LINEAR_PARAMS.pack(m, 1, n, 0, 0, 0, ldy, ldz, ldp, _dtype_code(dt), 0, 0, act_code, r, lora_scale, p_drop, seed & _SEED)
     lib, stream = _lib.load(), _stream_ptr()
-    ws, size = None, 0
+    held, ws, size = None, None, 0
     if bias_grad or r:
-        ws, size = _scratch(lib.loract_linear_backward_workspace_bytes, "loract_linear_backward_workspace_bytes", params, dy, stream)
+        held, ws, size = _scratch(lib.loract_linear_backward_workspace_bytes, "loract_linear_backward_workspace_bytes", params, dy)
     code = lib.loract_linear_backward(dy.data_ptr(), z_ptr, t_ptr, params, out.data_ptr(), _ptr(db), _ptr(d_b), ws, size, stream)
     if code:
         raise LoractError(code, "loract_linear_backward")
@@ -570,9 +572,9 @@ def loract_qknorm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], gamm
     if q.shape[0] == 0:
         return dq, dk, dgq if dgq is None else dgq.zero_(), dgk if dgk is None else dgk.zero_()
     lib, stream = _lib.load(), _stream_ptr()
-    ws, size = None, 0
+    held, ws, size = None, None, 0
     if dgq is not None or dgk is not None:
-        ws, size = _scratch(lib.loract_qknorm_rope_workspace_bytes, "loract_qknorm_rope_workspace_bytes", params, q, stream)
+        held, ws, size = _scratch(lib.loract_qknorm_rope_workspace_bytes, "loract_qknorm_rope_workspace_bytes", params, q)
     code = lib.loract_qknorm_rope_backward(q.data_ptr(), _ptr(k), params, gq, gk, _ptr(table), _ptr(positions), dq_out.data_ptr(),
                                            _ptr(dk_out), dq.data_ptr(), _ptr(dk), _ptr(dgq), _ptr(dgk), ws, size, stream)
     if code:
