@@ -330,6 +330,7 @@ def loract_prenorm_backward(a: torch.Tensor, rms: torch.Tensor, gamma: torch.Ten
 _LINEAR_PARAMS = struct.Struct("9q5ifdQ")
 _QK_PARAMS = struct.Struct("q6iqf4x12q")
 _SEED = 2 ** 64 - 1
+_WORKSPACE_TOO_SMALL = -2
 
 
 def _rows(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str) -> int:
@@ -358,16 +359,19 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _scratch(query, where: str, params: bytes, t: torch.Tensor) -> Tuple[Optional[torch.Tensor], Optional[int], int]:
-    """Workspace for a call with these parameters (what holds it, pointer, bytes)."""
-    nbytes = ctypes.c_size_t()
-    code = query(params, ctypes.byref(nbytes))
+def _enqueue(call, args: tuple, query, params: bytes, t: torch.Tensor, where: str) -> None:
+    """call(*args, workspace, its bytes, stream) on the stream's cached workspace, or where that is too small (which a call says before it
+    enqueues anything) or the stream is being captured on one of the size that `query` gives."""
+    stream = _stream_ptr()
+    held = None if torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((t.get_device(), stream))
+    code = call(*args, None, 0, stream) if held is None else call(*args, held.data_ptr(), held.numel(), stream)
+    if code == _WORKSPACE_TOO_SMALL:
+        nbytes = ctypes.c_size_t()
+        _check(query(params, ctypes.byref(nbytes)), where + "_workspace_bytes")
+        held = _workspace(nbytes.value, t.device)
+        code = call(*args, held.data_ptr(), held.numel(), stream)
     if code:
         raise LoractError(code, where)
-    if not nbytes.value:
-        return None, None, 0
-    ws = _workspace(nbytes.value, t.device)
-    return ws, ws.data_ptr(), ws.numel()
 
 
 def _act_code(act: str) -> int:
@@ -435,12 +439,9 @@ def loract_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor]
     if m:
         params = _LINEAR_PARAMS.pack(m, n_in, n_out, ldx, ldw, ldr, ldy, n_out, 0, _dtype_code(dt), _dtype_code(odt),
                                      W_IN_OUT if w_transposed else W_OUT_IN, _act_code(act), r, lora_scale, p_drop, seed & _SEED)
-        lib, stream = _lib.load(), _stream_ptr()
-        held, ws, size = _scratch(lib.loract_linear_workspace_bytes, "loract_linear_workspace_bytes", params, x)
-        code = lib.loract_linear(x.data_ptr(), w.data_ptr(), bias_ptr, t_ptr, b_ptr, r_ptr, params, out.data_ptr(), _ptr(z), ws,
-                                 size, stream)
-        if code:
-            raise LoractError(code, "loract_linear")
+        lib = _lib.load()
+        _enqueue(lib.loract_linear, (x.data_ptr(), w.data_ptr(), bias_ptr, t_ptr, b_ptr, r_ptr, params, out.data_ptr(), _ptr(z)),
+                 lib.loract_linear_workspace_bytes, params, x, "loract_linear")
     return (out, z) if save_preact else out
 
 
@@ -475,13 +476,9 @@ def loract_linear_backward(dy: torch.Tensor, z: Optional[torch.Tensor] = None, *
     if m == 0:
         return out, db if db is None else db.zero_(), d_b if d_b is None else d_b.zero_()
     params = _LINEAR_PARAMS.pack(m, 1, n, 0, 0, 0, ldy, ldz, ldp, _dtype_code(dt), 0, 0, act_code, r, lora_scale, p_drop, seed & _SEED)
-    lib, stream = _lib.load(), _stream_ptr()
-    held, ws, size = None, None, 0
-    if bias_grad or r:
-        held, ws, size = _scratch(lib.loract_linear_backward_workspace_bytes, "loract_linear_backward_workspace_bytes", params, dy)
-    code = lib.loract_linear_backward(dy.data_ptr(), z_ptr, t_ptr, params, out.data_ptr(), _ptr(db), _ptr(d_b), ws, size, stream)
-    if code:
-        raise LoractError(code, "loract_linear_backward")
+    lib = _lib.load()
+    _enqueue(lib.loract_linear_backward, (dy.data_ptr(), z_ptr, t_ptr, params, out.data_ptr(), _ptr(db), _ptr(d_b)),
+             lib.loract_linear_backward_workspace_bytes, params, dy, "loract_linear_backward")
     return out, db, d_b
 
 
@@ -571,14 +568,10 @@ def loract_qknorm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], gamm
     dgk = None if gk is None else q.new_empty((d,), dtype=torch.float32)
     if q.shape[0] == 0:
         return dq, dk, dgq if dgq is None else dgq.zero_(), dgk if dgk is None else dgk.zero_()
-    lib, stream = _lib.load(), _stream_ptr()
-    held, ws, size = None, None, 0
-    if dgq is not None or dgk is not None:
-        held, ws, size = _scratch(lib.loract_qknorm_rope_workspace_bytes, "loract_qknorm_rope_workspace_bytes", params, q)
-    code = lib.loract_qknorm_rope_backward(q.data_ptr(), _ptr(k), params, gq, gk, _ptr(table), _ptr(positions), dq_out.data_ptr(),
-                                           _ptr(dk_out), dq.data_ptr(), _ptr(dk), _ptr(dgq), _ptr(dgk), ws, size, stream)
-    if code:
-        raise LoractError(code, "loract_qknorm_rope_backward")
+    lib = _lib.load()
+    _enqueue(lib.loract_qknorm_rope_backward, (q.data_ptr(), _ptr(k), params, gq, gk, _ptr(table), _ptr(positions), dq_out.data_ptr(),
+                                               _ptr(dk_out), dq.data_ptr(), _ptr(dk), _ptr(dgq), _ptr(dgk)),
+             lib.loract_qknorm_rope_workspace_bytes, params, q, "loract_qknorm_rope_backward")
     return dq, dk, dgq, dgk
 
 
