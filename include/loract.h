@@ -220,6 +220,8 @@ int loract_prenorm_backward(const void* A_dev, int64_t m, int64_t n, int64_t lda
 /*
  * The sub-layer around a compressed activation (Section 3.3: Z = F(Norm(X)) + X): the linear maps with what
  * follows them, their backward pass, dropout, and the norm and rotation of queries and keys.
+ * Outputs that share memory with each other, with the workspace or with what the call reads are refused (LORACT_ERR_INVALID_ARG), but
+ * where an output may be an input: the same address and strides, so that every element is written by whoever has read it.
  */
 
 /* Activations of loract_linear: none, max(z, 0), z Phi(z) (by erf), z / (1 + exp(-z)). */
@@ -280,7 +282,7 @@ int loract_linear(const void* X_dev, const void* W_dev, const float* bias_dev, c
  * Backward of loract_linear up to the products, one pass over dY and Z:
  *   dP = act'(Z) D(dY),   dbias_j = sum_i dP_ij,   dB_lora = lora_scale T^T dP
  * Z_dev     what the forward call kept; not read (may be NULL) without an activation.
- * dP_dev    out, m x n_out of dtype.   dbias_dev out, n_out floats, or NULL.   dB_dev out, r_lora x n_out floats, or NULL
+ * dP_dev    out, m x n_out of dtype; may be dY or Z with the same ld.   dbias_dev out, n_out floats, or NULL.   dB_dev out, r_lora x n_out floats, or NULL
  *           (then T_dev is not read).  The sums are of the unrounded float32 dP.
  * The rest of the backward pass are calls on dP: dT = lora_scale dP B_lora^T and dX = dP W + dT A^T by loract_linear,
  * dA by loract_lora_grad.  Workspace: loract_linear_backward_workspace_bytes.

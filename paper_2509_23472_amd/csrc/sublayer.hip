@@ -6,6 +6,7 @@
 #include "linear_large.h"
 #include "linear_thin.h"
 #include "linear_tile.h"
+#include "overlap.h"
 #include "qknorm.h"
 
 #include <algorithm>
@@ -34,6 +35,34 @@ static int check_linear_forward(const loract_linear_params* p) {
   return LORACT_OK;
 }
 
+// Outputs of the linear map within what it reads, but the residual in place, or within each other.
+static bool linear_outputs_meet(const loract_linear_params* p, const void* X, const void* W, const float* bias, const void* T, const void* B, const void* R,
+                                const void* Y, const void* Z, const void* ws, size_t ws_bytes) {
+  const int64_t size = p->dtype == LORACT_BF16 ? 2 : 4, y_size = p->out_dtype == LORACT_BF16 ? 2 : 4;
+  const bool w_kc = p->w_layout == LORACT_W_OUT_IN;
+  const Extent y = extent_rows(Y, p->m, p->ldy, p->n_out, y_size), z = extent_rows(Z, p->m, p->ldz, p->n_out, size);
+  const Extent r = extent_rows(R, p->m, p->ldr, p->n_out, size);
+  const Extent in[] = {extent_rows(X, p->m, p->ldx, p->n_in, size),
+                       extent_rows(W, w_kc ? p->n_out : p->n_in, p->ldw, w_kc ? p->n_in : p->n_out, size), extent_bytes(bias, p->n_out * 4),
+                       extent_bytes(p->r_lora ? T : nullptr, p->m * p->r_lora * size),
+                       extent_bytes(p->r_lora ? B : nullptr, p->n_out * p->r_lora * size), extent_bytes(ws_bytes ? ws : nullptr, ws_bytes)};
+  for (const Extent& e : in)
+    if (extents_meet(y, e) || extents_meet(z, e)) return true;
+  return extents_meet(y, z) || extents_meet(z, r) || meets_but_in_place(y, r);
+}
+// The same of its backward pass: dP in place of dY or Z.
+static bool linear_backward_outputs_meet(const loract_linear_params* p, const void* dY, const void* Z, const void* T, const void* dP, const float* dbias,
+                                         const float* dB, const void* ws, size_t ws_bytes) {
+  const int64_t size = p->dtype == LORACT_BF16 ? 2 : 4;
+  const Extent dy = extent_rows(dY, p->m, p->ldy, p->n_out, size), z = extent_rows(Z, p->m, p->ldz, p->n_out, size);
+  const Extent dp = extent_rows(dP, p->m, p->ldp, p->n_out, size), t = extent_bytes(dB ? T : nullptr, p->m * p->r_lora * size);
+  const Extent db = extent_bytes(dbias, p->n_out * 4), d_b = extent_bytes(dB, p->n_out * p->r_lora * 4);
+  const Extent scratch = extent_bytes(dbias || dB ? ws : nullptr, ws_bytes);
+  for (const Extent& e : {dy, z, dp, t, scratch})
+    if (extents_meet(db, e) || extents_meet(d_b, e)) return true;
+  return extents_meet(db, d_b) || meets_but_in_place(dp, dy) || meets_but_in_place(dp, z) || extents_meet(dp, t) || extents_meet(dp, scratch);
+}
+
 extern "C" {
 
 int loract_dropout(const void* X_dev, int64_t ldx, const void* R_dev, int64_t ldr, int64_t m, int64_t n, int32_t dtype,
@@ -41,6 +70,9 @@ int loract_dropout(const void* X_dev, int64_t ldx, const void* R_dev, int64_t ld
   if (!X_dev || !Y_dev || m < 1 || n < 1 || ldx < n || ldy < n || (R_dev && ldr < n)) return LORACT_ERR_INVALID_ARG;
   if (!dtype_ok(dtype) || !(p >= 0.0 && p < 1.0)) return LORACT_ERR_INVALID_ARG;
   if (!extent_ok(m) || !extent_ok(n)) return LORACT_ERR_UNSUPPORTED;
+  const int64_t size = dtype == LORACT_BF16 ? 2 : 4;
+  const Extent y = extent_rows(Y_dev, m, ldy, n, size);
+  if (meets_but_in_place(y, extent_rows(X_dev, m, ldx, n, size)) || meets_but_in_place(y, extent_rows(R_dev, m, ldr, n, size))) return LORACT_ERR_INVALID_ARG;
   DropoutArgs g;
   g.X = X_dev; g.ldx = ldx; g.R = R_dev; g.ldr = R_dev ? ldr : 0; g.Y = Y_dev; g.ldy = ldy; g.m = m; g.n = n;
   g.d = drop_args(p, seed, n);
@@ -76,6 +108,7 @@ int loract_linear(const void* X_dev, const void* W_dev, const float* bias_dev, c
   LORACT_TRY(loract_linear_workspace_bytes(p, &need));
   if (need && (!ws_dev || ws_bytes < need)) return LORACT_ERR_WORKSPACE_TOO_SMALL;
   if (need && ((uintptr_t)ws_dev) % 16 != 0) return LORACT_ERR_INVALID_ARG;
+  if (linear_outputs_meet(p, X_dev, W_dev, bias_dev, T_dev, Blora_dev, R_dev, Y_dev, Z_dev, ws_dev, need)) return LORACT_ERR_INVALID_ARG;
   LinearArgs g;
   g.X = X_dev; g.ldx = p->ldx; g.W = W_dev; g.ldw = p->ldw; g.r = p->r_lora; g.lora_scale = p->lora_scale;
   g.T = p->r_lora ? T_dev : nullptr; g.B = p->r_lora ? Blora_dev : nullptr;
@@ -116,6 +149,7 @@ int loract_linear_backward(const void* dY_dev, const void* Z_dev, const void* T_
   const bool sums = dbias_dev || dB_dev;
   if (sums && (!ws_dev || ws_bytes < plan.bytes)) return LORACT_ERR_WORKSPACE_TOO_SMALL;
   if (sums && ((uintptr_t)ws_dev) % 16 != 0) return LORACT_ERR_INVALID_ARG;
+  if (linear_backward_outputs_meet(p, dY_dev, act ? Z_dev : nullptr, T_dev, dP_dev, dbias_dev, dB_dev, ws_dev, plan.bytes)) return LORACT_ERR_INVALID_ARG;
   LinBackArgs g;
   g.dY = dY_dev; g.lddy = p->ldy; g.Z = act ? Z_dev : nullptr; g.ldz = act ? p->ldz : 0; g.T = dB_dev ? T_dev : nullptr;
   g.r = dB_dev ? p->r_lora : 0; g.dP = dP_dev; g.lddp = p->ldp; g.m = p->m; g.n = p->n_out; g.act = p->act;
@@ -145,6 +179,28 @@ static int check_qk(const loract_qk_params* p, bool bwd) {
   (void)bwd;
   return LORACT_OK;
 }
+static Extent qk_extent(const loract_qk_params* p, const void* at, int heads, int64_t token, int64_t head) {
+  return extent_heads(heads ? at : nullptr, p->m, token, heads, head, p->d, p->dtype == LORACT_BF16 ? 2 : 4);
+}
+// Whether the outputs (written) share memory with what is read, but one in place of the inputs of its own stream, or with each other.
+struct QkOperands {
+  Extent q, k, dq_out, dk_out;
+  const float *gamma_q, *gamma_k, *table;
+  const int32_t* pos;
+};
+static bool qk_outputs_meet(const loract_qk_params* p, const QkOperands& in, const Extent& oq, const Extent& ok, const Extent& scratch, const float* dgq,
+                            const float* dgk) {
+  const Extent read[] = {extent_bytes(in.gamma_q, p->d * 4), extent_bytes(in.gamma_k, p->d * 4), extent_bytes(p->rot ? in.table : nullptr, (wide_t)p->n_pos * p->rot * 4),
+                         extent_bytes(in.pos, p->m * 4), scratch};
+  const Extent g[] = {extent_bytes(dgq, p->d * 4), extent_bytes(dgk, p->d * 4)};
+  for (const Extent& e : read)
+    if (extents_meet(oq, e) || extents_meet(ok, e) || extents_meet(g[0], e) || extents_meet(g[1], e)) return true;
+  for (const Extent& e : {in.q, in.k, in.dq_out, in.dk_out, oq, ok})
+    if (extents_meet(g[0], e) || extents_meet(g[1], e)) return true;
+  return !extent_distinct(oq) || (ok.at && !extent_distinct(ok)) || extents_meet(oq, ok) || extents_meet(g[0], g[1]) || meets_but_in_place(oq, in.q) ||
+         meets_but_in_place(oq, in.dq_out) || meets_but_in_place(ok, in.k) || meets_but_in_place(ok, in.dk_out) || extents_meet(oq, in.k) ||
+         extents_meet(oq, in.dk_out) || extents_meet(ok, in.q) || extents_meet(ok, in.dq_out);
+}
 static bool qk_strides(const void* p, int64_t token, int64_t head, int elems, size_t bytes) {
   return ((uintptr_t)p) % bytes == 0 && token % elems == 0 && head % elems == 0;
 }
@@ -166,6 +222,11 @@ int loract_qknorm_rope_forward(const void* q_dev, const void* k_dev, const lorac
   LORACT_TRY(check_qk(p, false));
   const bool keys = p->heads_k > 0;
   if (!q_dev || !q_out_dev || (keys && (!k_dev || !k_out_dev)) || (p->rot && !table_dev)) return LORACT_ERR_INVALID_ARG;
+  const QkOperands in = {qk_extent(p, q_dev, p->heads_q, p->q_token, p->q_head), qk_extent(p, k_dev, p->heads_k, p->k_token, p->k_head), {}, {},
+                         gamma_q_dev, gamma_k_dev, table_dev, pos_dev};
+  if (qk_outputs_meet(p, in, qk_extent(p, q_out_dev, p->heads_q, p->qo_token, p->qo_head), qk_extent(p, k_out_dev, p->heads_k, p->ko_token, p->ko_head), {},
+                      nullptr, nullptr))
+    return LORACT_ERR_INVALID_ARG;
   const bool bf16 = p->dtype == LORACT_BF16;
   auto aligned = [&](int elems) {
     const size_t b = (size_t)elems * (bf16 ? 2 : 4);
@@ -202,6 +263,12 @@ int loract_qknorm_rope_backward(const void* q_dev, const void* k_dev, const lora
   const bool sums = dgamma_q_dev || dgamma_k_dev;
   if (sums && (!ws_dev || ws_bytes < plan.part_bytes)) return LORACT_ERR_WORKSPACE_TOO_SMALL;
   if (sums && ((uintptr_t)ws_dev) % 16 != 0) return LORACT_ERR_INVALID_ARG;
+  const QkOperands in = {qk_extent(p, q_dev, p->heads_q, p->q_token, p->q_head), qk_extent(p, k_dev, p->heads_k, p->k_token, p->k_head),
+                         qk_extent(p, dq_out_dev, p->heads_q, p->dq_token, p->dq_head), qk_extent(p, dk_out_dev, p->heads_k, p->dk_token, p->dk_head),
+                         gamma_q_dev, gamma_k_dev, table_dev, pos_dev};
+  if (qk_outputs_meet(p, in, qk_extent(p, dq_dev, p->heads_q, p->qo_token, p->qo_head), qk_extent(p, dk_dev, p->heads_k, p->ko_token, p->ko_head),
+                      extent_bytes(sums ? ws_dev : nullptr, plan.part_bytes), dgamma_q_dev, dgamma_k_dev))
+    return LORACT_ERR_INVALID_ARG;
   QkArgs g{};
   g.m = p->m; g.d = p->d; g.rot = p->rot; g.pos = pos_dev; g.n_pos = p->rot ? p->n_pos : INT64_MAX; g.table = table_dev; g.eps = p->eps;
   g.q.x = q_dev; g.q.ldt = p->q_token; g.q.ldh = p->q_head; g.q.out = dq_dev; g.q.out_ldt = p->qo_token; g.q.out_ldh = p->qo_head;
