@@ -5,12 +5,14 @@
 #include "dropout.h"
 
 // The activations and their slopes: exp and the reciprocal by the hardware's instructions (both within one unit), and Phi from
-//   erfc(x) = q(t) exp(-x^2),  t = 1 / (1 + 0.4 x),  x >= 0,
-// q a polynomial fitted here to the least relative error (1.4e-7, 4e-7 evaluated in float32).  EXACT (float32 inputs): the
-// rounding of exp's argument is made good, the reciprocal takes a Newton step and SiLU divides, which leaves 4e-7; without, bf16 inputs
-// lose up to 2^-20, far below their last rounding.  A fifth of the instructions of erff, expf and a division, which an epilogue has nothing to hide
-// behind: 8192 x 4096 -> 11008 with SiLU 747 us with those and 685 so (642 without an activation), the backward of 8192 x 11008 SiLU
-// 169 and 123, GELU 215 and 131, of 12608 x 768 float32 GELU 38 and 33 (SiLU's division: 32.6 us, 32.0 with the reciprocal).
+//   erfc(x) = t q(t) exp(-x^2),  t = 1 / (1 + 0.4 x),  x >= 0,
+// q a polynomial of least relative error (1.4e-7, 4e-7 evaluated in float32).  bf16 results need no more: they lose up to 2^-20, far below their
+// last rounding.  EXACT (float32): the rounding of exp's argument is made good, SiLU divides, and Phi near 0 comes from a polynomial in z, which
+// leaves what erff, expf and a division would: largest relative errors in units of 2^-24 (with those) SiLU 3.6 (3.0), GELU above -1 4.3
+// (4.5), from there to -6, where 1 + erf cancels, 21 (all).
+// Those functions have five times the instructions, which an epilogue has nothing to hide behind: 8192 x 4096 -> 11008 bf16 with SiLU 747 us with
+// them and 685 so (642 without an activation), the backward of 8192 x 11008 SiLU 169 and 123, GELU 215 and 131, of 12608 x 768
+// float32 GELU 38 and 34 (33.4 without the polynomial in z), SiLU's division 32.6 (the reciprocal: 32.0).
 template <bool EXACT>
 __device__ inline float lin_exp(float x) {
   constexpr float L = 1.44269504088896341f, L_REST = 1.92596299112661746e-8f;      // log2(e) and what its rounding leaves
@@ -20,22 +22,17 @@ __device__ inline float lin_exp(float x) {
   const float rest = fmaf(x, L_REST, fmaf(x, L, -t));                              // (not a number where t overflows)
   return t > -150.0f && t < 128.0f ? fmaf(e, 0.693147180559945309f * rest, e) : e;  // (from 128 on e is infinite: nothing to make good)
 }
-template <bool EXACT>
-__device__ inline float lin_reciprocal(float x) {                                  // x >= 1
-  const float r = __builtin_amdgcn_rcpf(x);
-  return EXACT && x < 0x1p120f ? fmaf(fmaf(-x, r, 1.0f), r, r) : r;
-}
 // 1 / (1 + exp(-z)) and z times it.  EXACT: by a division, since the reciprocal's instruction makes zero of what is below 2^-126 (z < -87.3),
 // of which z times as much need not be.
 template <bool EXACT>
 __device__ inline float lin_sigmoid(float z, float times) {
   const float below = 1.0f + lin_exp<EXACT>(-z);
-  return EXACT ? times / below : times * lin_reciprocal<EXACT>(below);
+  return EXACT ? times / below : times * __builtin_amdgcn_rcpf(below);
 }
 // Phi(z); *density: exp(-z^2 / 2)
 template <bool EXACT>
 __device__ inline float lin_phi(float z, float* density) {
-  const float t = lin_reciprocal<EXACT>(fmaf(fabsf(z), 0.4f * 0.70710678118654752f, 1.0f));
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.4f * 0.70710678118654752f, 1.0f));
   float q = 0.05026593804359436f;
   q = fmaf(q, t, -0.182917058467865f);
   q = fmaf(q, t, 0.16911154985427856f);
@@ -47,7 +44,18 @@ __device__ inline float lin_phi(float z, float* density) {
   q = fmaf(q, t, 0.22567586600780487f);
   *density = lin_exp<EXACT>(-0.5f * z * z);
   const float half = 0.5f * q * t * *density;
-  return z < 0.0f ? half : 1.0f - half;
+  const float tail = z < 0.0f ? half : 1.0f - half;
+  if (!EXACT) return tail;
+  // within sqrt(2) of 0, where the tail's error would be most of the result's: Phi = 1/2 + z r(z^2), r within 2e-8 / z
+  const float u = z * z;
+  float r = 4.3545057337723847e-07f;
+  r = fmaf(r, u, -8.859667104843538e-06f);
+  r = fmaf(r, u, 0.00011466867726994678f);
+  r = fmaf(r, u, -0.0011868048459291458f);
+  r = fmaf(r, u, 0.009973385371267796f);
+  r = fmaf(r, u, -0.06649035960435867f);
+  r = fmaf(r, u, 0.3989422917366028f);
+  return u < 2.0f ? fmaf(z, r, 0.5f) : tail;
 }
 template <bool EXACT>
 __device__ inline float lin_act(int act, float z) {

@@ -74,3 +74,15 @@ def test_float32_slopes_at_the_ends_of_the_range(act, r):
     if act == "silu":
         bound = torch.where(z < -2, 16 * 2.0 ** -24 * want.abs() + 1e-36, bound)
     ref.check(dp, want, bound, act)
+
+
+@pytest.mark.parametrize("form", ["few_outputs", "tiles", "tiles_split"])
+def test_float32_gelu_near_zero_and_above(form):
+    """In units of 2^-24: Phi = 1/2 + z r rounded (Phi) and multiplied with z (Phi), z r half of a unit by r's rounding and a quarter by
+    its polynomial; above sqrt(2), 1 less a tail of at most 0.08 that is up to 16 units off itself."""
+    z = torch.cat([torch.linspace(-1.0, 1.0, 4096), torch.linspace(1.0, 20.0, 2048), torch.logspace(-12, 0, 2048)])
+    z, y = _forward(z, form, "gelu")
+    z = z.double()
+    phi = 0.5 * torch.special.erfc(-z / math.sqrt(2))
+    bound = z.abs() * (2 * phi + torch.where(z > math.sqrt(2), 1.25, 0.75)) * 2.0 ** -24
+    ref.check(y, (z * phi)[:, None].expand(y.shape), bound[:, None], "gelu")
