@@ -6,13 +6,15 @@
 
 // The activations and their slopes: exp and the reciprocal by the hardware's instructions (both within one unit), and Phi from
 //   erfc(x) = t q(t) exp(-x^2),  t = 1 / (1 + 0.4 x),  x >= 0,
-// q a polynomial of least relative error (1.4e-7, 4e-7 evaluated in float32).  bf16 results need no more: they lose up to 2^-20, far below their
-// last rounding.  EXACT (float32): the rounding of exp's argument is made good, SiLU divides, and Phi near 0 comes from a polynomial in z, which
-// leaves what erff, expf and a division would: largest relative errors in units of 2^-24 (with those) SiLU 3.6 (3.0), GELU above -1 4.3
-// (4.5), from there to -6, where 1 + erf cancels, 21 (all).
+// q a polynomial of least relative error (1.4e-7, 4e-7 evaluated in float32).  What is stored as bf16 needs no more: the argument of exp is rounded
+// once, which costs |x| 2^-23 of the result at most, up to 2^-17 where exp itself is 2^-126.  EXACT (what is stored as float32, and the
+// slopes of float32 operands): that rounding is made good, SiLU divides, and Phi near 0 comes from a polynomial in z, which leaves what
+// erff, expf and a division would: largest relative errors in units of 2^-24 (with those) SiLU 3.6 (3.0), GELU above -1 4.3 (4.5), from there to -6,
+// where 1 + erf cancels, 21 (all).
 // Those functions have five times the instructions, which an epilogue has nothing to hide behind: 8192 x 4096 -> 11008 bf16 with SiLU 747 us with
 // them and 685 so (642 without an activation), the backward of 8192 x 11008 SiLU 169 and 123, GELU 215 and 131, of 12608 x 768
-// float32 GELU 38 and 34 (33.4 without the polynomial in z), SiLU's division 32.6 (the reciprocal: 32.0).
+// float32 GELU 38 and 34 (33.4 without the polynomial in z), SiLU's division 32.6 (the reciprocal: 32.0).  8192 x 4096 -> 4096 of bf16 to
+// float32: GELU 253 us (243 as for bf16), SiLU 239 (236).
 template <bool EXACT>
 __device__ inline float lin_exp(float x) {
   constexpr float L = 1.44269504088896341f, L_REST = 1.92596299112661746e-8f;      // log2(e) and what its rounding leaves
@@ -57,16 +59,21 @@ __device__ inline float lin_phi(float z, float* density) {
   r = fmaf(r, u, 0.3989422917366028f);
   return u < 2.0f ? fmaf(z, r, 0.5f) : tail;
 }
-template <bool EXACT>
-__device__ inline float lin_act(int act, float z) {
-  switch (act) {
-    case LORACT_ACT_RELU: return z < 0.0f ? 0.0f : z;                              // (a NaN stays one)
-    case LORACT_ACT_GELU: {
+// (one choice for all of them: the values' chains of operations then run side by side)
+template <bool EXACT, int N>
+__device__ inline void lin_act(int act, float (&v)[N]) {
+  if (act == LORACT_ACT_RELU) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) v[u] = v[u] < 0.0f ? 0.0f : v[u];                  // (a NaN stays one)
+  } else if (act == LORACT_ACT_GELU) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
       float density;
-      return z * lin_phi<EXACT>(z, &density);
+      v[u] *= lin_phi<EXACT>(v[u], &density);
     }
-    case LORACT_ACT_SILU: return lin_sigmoid<EXACT>(z, z);
-    default: return z;
+  } else if (act == LORACT_ACT_SILU) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) v[u] = lin_sigmoid<EXACT>(v[u], v[u]);
   }
 }
 template <bool EXACT>
@@ -135,14 +142,19 @@ __device__ inline void lin_store4(const LinEpilogue& e, int64_t row, int64_t col
     if (e.bias && col + u < e.n) b[u] = e.bias[col + u];
   quad zq;
   f32x4 y;
+  float a[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    a[u] = v[u] + b[u];
+    zq[u] = (T)a[u];
+  }
+  if (sizeof(T) == 4 || e.y_f32) lin_act<true>(e.act, a);
+  else lin_act<false>(e.act, a);
   const uint64_t word = e.d.thr ? drop_word(e.d, row, col / 4) : 0;
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
-    const float z = v[u] + b[u];
-    zq[u] = (T)z;
-    float a = lin_act<sizeof(T) == 4>(e.act, z);
-    if (e.d.thr) a = drop_one(e.d, word, u, a);
-    y[u] = e.R ? a + r[u] : a;
+    if (e.d.thr) a[u] = drop_one(e.d, word, u, a[u]);
+    y[u] = e.R ? a[u] + r[u] : a[u];
   }
   if (e.vec) {
     if (e.Z) *(quad*)zp = zq;

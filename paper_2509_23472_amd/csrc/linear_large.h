@@ -53,8 +53,8 @@ __device__ inline int ll_turn_k(int k) { return 4 * (k & 3) + ((k >> 2) & 2); }
 // Waves of a tile (TILE / 2 x 64 each), in two rows.
 constexpr int ll_waves(int tile) { return tile / 32; }
 
-// blockIdx.x: tile, blockIdx.y: split of K.
-template <bool WKC, int TILE>
+// blockIdx.x: tile, blockIdx.y: split of K.  Y_F32: Y is float32, and its activations the refined ones.
+template <bool WKC, int TILE, bool Y_F32>
 __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void linear_large_kernel(LinearArgs g, int tiles_m, int tiles_n) {
   constexpr int WAVES = ll_waves(TILE), WN = TILE / 64, MT = TILE / 32, NT = 4;      // a wave: MT x NT products of 16 x 16
   constexpr int C = TILE / 8 / WAVES;                    // copies of 1 KB per operand and slab
@@ -324,12 +324,8 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
       for (int q = 0; q < N8; ++q)
         if (row + ROWS * q < g.m) store((bf16_t*)e.Z + (row + ROWS * q) * e.ldz + col, y[q]);
     }
-    if (e.act != LORACT_ACT_NONE) {
 #pragma unroll
-      for (int q = 0; q < N8; ++q)
-#pragma unroll
-        for (int u = 0; u < 8; ++u) y[q][u] = lin_act<false>(e.act, y[q][u]);
-    }
+    for (int q = 0; q < N8; ++q) lin_act<Y_F32>(e.act, y[q]);
     if (e.d.thr) {
 #pragma unroll
       for (int q = 0; q < N8; ++q) {
@@ -350,7 +346,7 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
 #pragma unroll
     for (int q = 0; q < N8; ++q) {
       if (!in || row + ROWS * q >= g.m) continue;
-      if (!e.y_f32) {
+      if (!Y_F32) {
         store((bf16_t*)e.Y + (row + ROWS * q) * e.ldy + col, y[q]);
         continue;
       }
@@ -487,9 +483,13 @@ static int launch_linear_large(hipStream_t s, LinearArgs g, bool w_kc, LargePlan
   g.n_pad = q.n8;
   const int tm = (int)ceil_div64(g.m, p.tile), tn = (int)ceil_div64(g.n, p.tile);
   const dim3 grid((unsigned)(tm * tn), (unsigned)p.splits), block(64 * ll_waves(p.tile));
-#define LL_LAUNCH(KC, TILE) LORACT_LAUNCH("linear_large", s, (linear_large_kernel<KC, TILE>), grid, block, 0, g, tm, tn)
-  if (p.tile == 256) { if (w_kc) LL_LAUNCH(true, 256); else LL_LAUNCH(false, 256); }
-  else { if (w_kc) LL_LAUNCH(true, 128); else LL_LAUNCH(false, 128); }
+#define LL_LAUNCH(KC, TILE)                                                                                                          \
+  {                                                                                                                                 \
+    if (g.e.y_f32) LORACT_LAUNCH("linear_large", s, (linear_large_kernel<KC, TILE, true>), grid, block, 0, g, tm, tn);                \
+    else LORACT_LAUNCH("linear_large", s, (linear_large_kernel<KC, TILE, false>), grid, block, 0, g, tm, tn);                         \
+  }
+  if (p.tile == 256) { if (w_kc) LL_LAUNCH(true, 256) else LL_LAUNCH(false, 256) }
+  else { if (w_kc) LL_LAUNCH(true, 128) else LL_LAUNCH(false, 128) }
 #undef LL_LAUNCH
   return p.splits > 1 ? launch_linear_join<bf16_t>(s, g, p.splits) : LORACT_OK;
 }

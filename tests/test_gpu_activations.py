@@ -32,7 +32,7 @@ def _act(name, z):
 
 def _forward(z, form, act, dtype=torch.float32, out_dtype=None):
     import paper_2509_23472_amd as L
-    n_in, n_out, at_once, layout = FORMS[form]
+    n_in, n_out, at_once, layout = FORMS.get(form) or LARGE[form]
     z = z[:256] if at_once < 64 else z
     w = torch.zeros(n_out, n_in, dtype=dtype, device="cuda")
     w[:, 0] = 1.0
@@ -86,3 +86,23 @@ def test_float32_gelu_near_zero_and_above(form):
     phi = 0.5 * torch.special.erfc(-z / math.sqrt(2))
     bound = z.abs() * (2 * phi + torch.where(z > math.sqrt(2), 1.25, 0.75)) * 2.0 ** -24
     ref.check(y, (z * phi)[:, None].expand(y.shape), bound[:, None], "gelu")
+
+
+# tiles of bf16 operands: 128 x 128 whole and with K split, and 256 x 256
+LARGE = {"large": (64, 200, 4096, "nt"), "large_as_it_lies": (64, 200, 4096, "nn"), "large_split": (2048, 128, 512, "nt"),
+         "large_256": (64, 256, 65536, "nt")}
+
+
+@pytest.mark.parametrize("form", list(FORMS) + list(LARGE))
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+def test_float32_results_of_bf16_operands(act, form):
+    """What follows the product of bf16 operands is rounded no earlier than its result is."""
+    z = torch.unique(torch.cat([_ends(), torch.linspace(-20.0, 20.0, 4096)]).bfloat16())
+    at_once = (FORMS.get(form) or LARGE[form])[2]
+    z = z.float()
+    z = z[::16] if at_once < 64 else z.repeat(1 + at_once // len(z))[:max(at_once, len(z))]
+    z, y = _forward(z, form, act, torch.bfloat16, torch.float32)
+    assert y.dtype == torch.float32
+    want = _act(act, z.double())[:, None].expand(y.shape)
+    rel = 2.0 ** -24 * (16 + z.double().square() / 2 if act == "gelu" else torch.full_like(z.double(), 8.0))
+    ref.check(y, want, (rel * want[:, 0].abs())[:, None] + 1e-36, act)
