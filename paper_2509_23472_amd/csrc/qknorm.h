@@ -52,6 +52,16 @@ __device__ inline int qk_position(const QkArgs& g, int64_t token, int64_t* row) 
   return p < 0 ? QK_PAD : (p < g.n_pos ? QK_LIVE : QK_PAST);
 }
 
+// a c + b s.  For float32 gradients to one rounding of the whole: what the rounding of b s left is added, so that a difference of nearly
+// equal terms keeps its digits (b s may be infinite, then what it left is no number and must not count).  A bf16 gradient has none to keep,
+// and its pass of 8192 x (32 + 8) x 128 would take 55.7 us instead of 51.8 (float32: 104.2, 102.9).
+template <typename T>
+__device__ inline float qk_turn_back(float a, float c, float b, float s) {
+  if (sizeof(T) < 4) return a * c + b * s;
+  const float p = b * s;
+  return fmaf(a, c, p) + fmaxf(fmaf(b, s, -p), -1e30f);
+}
+
 // T: element type.  E: elements per piece.  L: lanes per head (a power of two, L E >= d).  INTER: interleaved pairs.  d, rot and
 // (unless INTER) rot / 2 are multiples of E.
 template <typename T, int E, int L, bool INTER, bool BWD>
@@ -129,14 +139,15 @@ __global__ __launch_bounds__(64 * QK_WAVES) void qknorm_rope_kernel(QkArgs g) {
 #pragma unroll
             for (int e = 0; e < E / 2; ++e) {
               const float a = t[2 * e], b = t[2 * e + 1];
-              t[2 * e] = a * c[e] + b * s[e];
-              t[2 * e + 1] = b * c[e] - a * s[e];
+              t[2 * e] = qk_turn_back<T>(a, c[e], b, s[e]);
+              t[2 * e + 1] = qk_turn_back<T>(b, c[e], a, -s[e]);
             }
           } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
               const float o = __shfl(t[e], partner);
-              t[e] = turn ? t[e] * c[e] - sign * (o * s[e]) : t[e];
+              if (sizeof(T) == 4) t[e] = turn ? qk_turn_back<T>(t[e], c[e], o, -sign * s[e]) : t[e];
+              else t[e] = turn ? t[e] * c[e] - sign * (o * s[e]) : t[e];
             }
           }
 #pragma unroll
@@ -237,8 +248,8 @@ __global__ __launch_bounds__(64 * QK_WAVES) void qknorm_rope_any_kernel(QkArgs g
         float ta = 0.0f, tb = 0.0f;
         if (BWD) {
           const float da = (float)dy[ia], db = pair ? (float)dy[ib] : 0.0f;
-          ta = da * c + db * s;
-          tb = db * c - da * s;
+          ta = qk_turn_back<T>(da, c, db, s);
+          tb = qk_turn_back<T>(db, c, da, -s);
           if (state != QK_LIVE) { ta = tb = state == QK_PAST ? NAN : 0.0f; }
         }
         if (sweep == 0) {
