@@ -119,7 +119,7 @@ __global__ __launch_bounds__(64 * LB_WAVES) void linear_backward_kernel(LinBackA
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < E; ++e) p[u][e] *= lin_act_slope<sizeof(T) == 4>(act, (float)z[u][e]);
+        for (int e = 0; e < E; ++e) p[u][e] = lin_act_back<sizeof(T) == 4>(act, (float)z[u][e], p[u][e]);
     };
     if (g.act == LORACT_ACT_RELU) slopes(LORACT_ACT_RELU);
     else if (g.act == LORACT_ACT_GELU) slopes(LORACT_ACT_GELU);

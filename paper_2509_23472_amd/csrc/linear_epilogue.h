@@ -76,20 +76,21 @@ __device__ inline void lin_act(int act, float (&v)[N]) {
     for (int u = 0; u < N; ++u) v[u] = lin_sigmoid<EXACT>(v[u], v[u]);
   }
 }
+// act'(z) g.  Where max(z, 0) is flat the gradient is 0 whatever g holds: selected, as a dropped element is.
 template <bool EXACT>
-__device__ inline float lin_act_slope(int act, float z) {
+__device__ inline float lin_act_back(int act, float z, float g) {
   switch (act) {
-    case LORACT_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
+    case LORACT_ACT_RELU: return z > 0.0f ? g : 0.0f;
     case LORACT_ACT_GELU: {
       float density;
       const float phi = lin_phi<EXACT>(z, &density);
-      return phi + z * (density * 0.39894228040143268f);
+      return g * (phi + z * (density * 0.39894228040143268f));
     }
     case LORACT_ACT_SILU: {
       const float s = lin_sigmoid<EXACT>(z, 1.0f);
-      return s * (1.0f + z * (1.0f - s));
+      return g * (s * (1.0f + z * (1.0f - s)));
     }
-    default: return 1.0f;
+    default: return g;
   }
 }
 
