@@ -271,6 +271,7 @@ typedef struct {
  *           T = X A (itself a call with W = A), as B_lora of loract_lora_grad; not read if r_lora is 0.
  * R_dev     m x n_out, or NULL.   Y_dev out, m x n_out of out_dtype; Y may be R where their types and ld are the same.
  * Z_dev     out, m x n_out of dtype, or NULL: P rounded to dtype, what the backward pass reads.
+ * m, n_in, n_out up to 2^30 (n_in below 8, or n_out below 8 with LORACT_W_IN_OUT: m up to 2^30 - 64), else LORACT_ERR_UNSUPPORTED, of the query too.
  * Sums are float32.  Workspace: loract_linear_workspace_bytes.  NaN and infinities of X and W reach the outputs they belong to.
  */
 int loract_linear_workspace_bytes(const loract_linear_params* p, size_t* bytes);

@@ -46,7 +46,9 @@ __global__ __launch_bounds__(64 * LB_WAVES) void linear_backward_kernel(LinBackA
   typedef T t_piece __attribute__((ext_vector_type(RB ? RB : 1)));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = lane & 15, k = lane >> 4;
-  const int64_t col = (int64_t)blockIdx.x * (16 * E) + c * E;
+  const int64_t strip = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
+  if (strip * (16 * E) >= g.n) return;               // (the last of several blockIdx.z may not be full)
+  const int64_t col = strip * (16 * E) + c * E;
   const int64_t r_beg = (int64_t)blockIdx.y * g.chunk;
   const int64_t r_end = r_beg + g.chunk < g.m ? r_beg + g.chunk : g.m;
   const bool on = col < g.n;
@@ -174,7 +176,7 @@ __global__ __launch_bounds__(64 * LB_WAVES) void linear_backward_kernel(LinBackA
     }
     __syncthreads();
   }
-  float* out = g.part + (int64_t)blockIdx.y * (1 + 16 * RB) * g.n_pad + (int64_t)blockIdx.x * (16 * E);
+  float* out = g.part + (int64_t)blockIdx.y * (1 + 16 * RB) * g.n_pad + strip * (16 * E);
   for (int i = threadIdx.x; i < (1 + 16 * RB) * 16 * E; i += 64 * LB_WAVES)
     out[(int64_t)(i / (16 * E)) * g.n_pad + i % (16 * E)] = red[i / (16 * E)][i % (16 * E)];
 }
@@ -223,8 +225,8 @@ template <typename T>
 static int launch_linear_backward(hipStream_t s, LinBackArgs g, const LinBackPlan& p, bool vec, float scale, float* db, float* dB) {
   g.chunk = p.chunk;
   g.n_pad = p.n_pad;
-  const dim3 grid((unsigned)p.strips, (unsigned)p.chunks);
-  if (grid.y > 65535) return LORACT_ERR_UNSUPPORTED;
+  const int64_t x = std::min<int64_t>(p.strips, 1 << 23);               // (fewer than 2^32 threads in a direction)
+  const dim3 grid((unsigned)x, (unsigned)p.chunks, (unsigned)ceil_div64(p.strips, x));
 #define LB_LAUNCH(V, RB) LORACT_LAUNCH("linear_backward", s, (linear_backward_kernel<T, V, RB>), grid, dim3(64 * LB_WAVES), 0, g)
 #define LB_RB(RB) { if (vec) LB_LAUNCH(true, RB); else LB_LAUNCH(false, RB); break; }
   switch (p.rb) {

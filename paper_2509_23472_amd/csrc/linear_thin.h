@@ -304,7 +304,7 @@ __global__ __launch_bounds__(64 * LN_WAVES) void linear_thin_t_kernel(LinearArgs
 // lies in whole pieces: at 2 bytes the general tiles are faster (one token through 4095 -> 11007 44 us against 31, 8192 x 4095 -> 16 31
 // against 21), at 8 they are not (one token through 4092 -> 11008 20 against 27); W as it lies at 8 bytes 53 against 32.
 static int linear_thin_form(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw, bool w_kc, bool bf16) {
-  if (k < 8 || m > (1 << 27) || n > (1 << 27)) return 0;    // (2^32 threads to a grid)
+  if (k < 8 || m > (1 << 27) - 16 || n > (1 << 27) - 16) return 0;    // (fewer than 2^32 threads to a launch, 512 for 16 rows)
   const int e = bf16 ? 8 : 4;
   if ((bf16 && (ldx % 2 || (w_kc && ldw % 2))) || (!w_kc && (ldw % e || n % e))) return 0;
   if (m <= 32) return w_kc ? 1 : 3;

@@ -29,6 +29,7 @@ struct LinearArgs {
   float* part;           // [split][m][n_pad] when the K range is split
   int64_t n_pad;
   int64_t k_per_split;
+  int splits;            // of K (general tiles)
   LinEpilogue e;
 };
 
@@ -149,7 +150,9 @@ __device__ inline void lin_multiply(const f32x4 (&w)[NT], const f32x4 (&x)[MT], 
 }
 
 // TINY: K, or the rows of W stored n_in x n_out, are shorter than a piece (the low-rank term's always may be).
-// WKC: W is n_out x n_in (rows along K), else n_in x n_out.  BM x BN tile, four waves of BM/2 x BN/2; blockIdx.z: split of K.
+// WKC: W is n_out x n_in (rows along K), else n_in x n_out.  BM x BN tile, four waves of BM/2 x BN/2.  blockIdx.x: row of tiles, blockIdx.y: column,
+// blockIdx.z: split of K, or where K is whole what the number of columns has beyond LT_MAX_Y.
+#define LT_MAX_Y 65535
 template <typename T, bool WKC, int BM, int BN, bool TINY>
 __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
   typedef LinOperand<T, true, BM, TINY> OpX;
@@ -164,8 +167,10 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
   __shared__ __attribute__((aligned(16))) unsigned char smem[2 * STAGE > OUT ? 2 * STAGE : OUT];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int wm = wave >> 1, wn = wave & 1;
-  const int64_t row0 = (int64_t)blockIdx.x * BM, col0 = (int64_t)blockIdx.y * BN;
-  const int kbeg = (int)(blockIdx.z * g.k_per_split);
+  const int split = g.splits > 1 ? blockIdx.z : 0;
+  const int64_t row0 = (int64_t)blockIdx.x * BM, col0 = ((g.splits > 1 ? 0 : (int64_t)blockIdx.z * gridDim.y) + blockIdx.y) * BN;
+  if (col0 >= g.n) return;                           // (the last of several blockIdx.z may not be full)
+  const int kbeg = (int)(split * g.k_per_split);
   const int kend = (int)(kbeg + g.k_per_split < g.k ? kbeg + g.k_per_split : g.k);
   const int nslab = (kend - kbeg + BK - 1) / BK;
   int x_off[MT], w_off[NT];
@@ -180,7 +185,7 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-  if (g.T && blockIdx.z == 0) {
+  if (g.T && split == 0) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) w_off[j] = OpX::BYTES + OpB::frag_off(wn * (BN / 2) + 32 * j, lane);
     OpT ot;
@@ -261,7 +266,7 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
   for (int i = 0; i < MT; ++i) {
     const int64_t row = row0 + wm * (BM / 2) + 32 * i + r0;
     f32x4 res[N4];
-    if (gridDim.z == 1) {
+    if (g.splits == 1) {
 #pragma unroll
       for (int q = 0; q < N4; ++q) res[q] = lin_load4<T>(g.e, row + ROWS * q, col);
     }
@@ -276,8 +281,8 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
     for (int q = 0; q < N4; ++q) {
       const f32x4 v = *(const f32x4*)(cs + (r0 + ROWS * q) * LDC + c4);
       const int64_t at = row + ROWS * q;
-      if (gridDim.z == 1) lin_store4<T>(g.e, at, col, v, res[q]);
-      else if (at < g.m && col < g.n_pad) *(f32x4*)(g.part + ((int64_t)blockIdx.z * g.m + at) * g.n_pad + col) = v;
+      if (g.splits == 1) lin_store4<T>(g.e, at, col, v, res[q]);
+      else if (at < g.m && col < g.n_pad) *(f32x4*)(g.part + ((int64_t)split * g.m + at) * g.n_pad + col) = v;
     }
     sb_wave_sync();
   }
@@ -302,6 +307,14 @@ static inline TilePlan linear_tile_plan(int64_t m, int64_t n, int64_t k, bool bf
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(s, 64));
   return p;
 }
+static inline bool linear_tile_tiny(int64_t n, int64_t k, bool w_kc, bool bf16) {
+  const int e = bf16 ? 8 : 4;
+  return k < e || (!w_kc && n < e);
+}
+// A launch takes fewer than 2^32 threads in a direction.  (More than LT_MAX_Y columns leave K whole.)
+static inline bool linear_tile_launches(int64_t m, int64_t n, int64_t k, bool w_kc, bool bf16) {
+  return ceil_div64(m, linear_tile_tiny(n, k, w_kc, bf16) ? 64 : linear_tile_plan(m, n, k, bf16).bm) < 1 << 24;
+}
 static inline size_t linear_tile_part_bytes(int64_t m, int64_t n, int64_t k, bool bf16) {
   const int s = linear_tile_plan(m, n, k, bf16).splits;
   return s > 1 ? (size_t)s * m * align_up((size_t)n, 4) * 4 : 0;
@@ -319,8 +332,7 @@ template <typename T>
 static int launch_linear_tile(hipStream_t s, LinearArgs g, bool w_kc) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int BK = LinOperand<T, true, 64, false>::BK;
-  constexpr int E = 16 / (int)sizeof(T);
-  const bool tiny = g.k < E || (!w_kc && g.n < E);
+  const bool tiny = linear_tile_tiny(g.n, g.k, w_kc, BF);
   TilePlan p = linear_tile_plan(g.m, g.n, g.k, BF);
   if (tiny) p.bm = p.bn = 64;
   const int bm = p.bm, bn = p.bn;
@@ -328,8 +340,9 @@ static int launch_linear_tile(hipStream_t s, LinearArgs g, bool w_kc) {
   g.k_per_split = ceil_div64(ceil_div64(g.k, splits), BK) * BK;
   splits = (int)ceil_div64(g.k, g.k_per_split);
   g.n_pad = (int64_t)align_up((size_t)g.n, 4);
-  const dim3 grid((unsigned)ceil_div64(g.m, bm), (unsigned)ceil_div64(g.n, bn), (unsigned)splits);
-  if (grid.y > 65535) return LORACT_ERR_UNSUPPORTED;
+  g.splits = splits;
+  const int64_t columns = ceil_div64(g.n, bn), y = std::min<int64_t>(columns, LT_MAX_Y);
+  const dim3 grid((unsigned)ceil_div64(g.m, bm), (unsigned)y, splits > 1 ? (unsigned)splits : (unsigned)ceil_div64(columns, y));
 #define LT_LAUNCH(WKC, BM, BN, TINY) LORACT_LAUNCH("linear_tile", s, (linear_tile_kernel<T, WKC, BM, BN, TINY>), grid, dim3(256), 0, g)
   if (w_kc) {
     if (tiny) LT_LAUNCH(true, 64, 64, true);

@@ -32,6 +32,7 @@ static int check_linear_forward(const loract_linear_params* p) {
   if (p->n_in < 1 || !dtype_ok(p->out_dtype)) return LORACT_ERR_INVALID_ARG;
   if (p->w_layout != LORACT_W_OUT_IN && p->w_layout != LORACT_W_IN_OUT) return LORACT_ERR_INVALID_ARG;
   if (!extent_ok(p->n_in) || (p->dtype == LORACT_F32 && p->out_dtype != LORACT_F32)) return LORACT_ERR_UNSUPPORTED;
+  if (!linear_tile_launches(p->m, p->n_out, p->n_in, p->w_layout == LORACT_W_OUT_IN, p->dtype == LORACT_BF16)) return LORACT_ERR_UNSUPPORTED;
   return LORACT_OK;
 }
 
@@ -112,7 +113,7 @@ int loract_linear(const void* X_dev, const void* W_dev, const float* bias_dev, c
   LinearArgs g;
   g.X = X_dev; g.ldx = p->ldx; g.W = W_dev; g.ldw = p->ldw; g.r = p->r_lora; g.lora_scale = p->lora_scale;
   g.T = p->r_lora ? T_dev : nullptr; g.B = p->r_lora ? Blora_dev : nullptr;
-  g.m = p->m; g.n = p->n_out; g.k = p->n_in; g.part = (float*)ws_dev; g.n_pad = 0; g.k_per_split = 0;
+  g.m = p->m; g.n = p->n_out; g.k = p->n_in; g.part = (float*)ws_dev; g.n_pad = 0; g.k_per_split = 0; g.splits = 1;
   LinEpilogue& e = g.e;
   e.bias = bias_dev; e.R = R_dev; e.ldr = R_dev ? p->ldr : 0; e.Y = Y_dev; e.ldy = p->ldy; e.Z = Z_dev; e.ldz = Z_dev ? p->ldz : 0;
   e.m = p->m; e.n = p->n_out; e.act = p->act; e.y_f32 = p->out_dtype == LORACT_F32;
@@ -171,12 +172,11 @@ int loract_rope_table(float* table_dev, int64_t n_pos, int32_t rot, double theta
   return LORACT_OK;
 }
 
-static int check_qk(const loract_qk_params* p, bool bwd) {
+static int check_qk(const loract_qk_params* p) {
   if (!p) return LORACT_ERR_INVALID_ARG;
   if (p->m < 1 || p->heads_q < 1 || p->heads_k < 0 || p->d < 1 || p->rot < 0 || p->rot % 2 || p->rot > p->d) return LORACT_ERR_INVALID_ARG;
   if (!dtype_ok(p->dtype) || !(p->eps >= 0.0f) || (p->rot && p->n_pos < 1)) return LORACT_ERR_INVALID_ARG;
   if (!extent_ok(p->m) || p->d > LORACT_MAX_HEAD || p->heads_q > 65536 || p->heads_k > 65536) return LORACT_ERR_UNSUPPORTED;
-  (void)bwd;
   return LORACT_OK;
 }
 static Extent qk_extent(const loract_qk_params* p, const void* at, int heads, int64_t token, int64_t head) {
@@ -207,7 +207,7 @@ static bool qk_strides(const void* p, int64_t token, int64_t head, int elems, si
 
 int loract_qknorm_rope_workspace_bytes(const loract_qk_params* p, size_t* bytes) {
   if (!bytes) return LORACT_ERR_INVALID_ARG;
-  LORACT_TRY(check_qk(p, true));
+  LORACT_TRY(check_qk(p));
   size_t most = 0;                                   // whatever alignment the call turns out to have
   const bool bf16 = p->dtype == LORACT_BF16, inter = p->interleaved != 0;
   for (int a = 0; a < 3; ++a)
@@ -219,7 +219,7 @@ int loract_qknorm_rope_workspace_bytes(const loract_qk_params* p, size_t* bytes)
 int loract_qknorm_rope_forward(const void* q_dev, const void* k_dev, const loract_qk_params* p, const float* gamma_q_dev,
                                const float* gamma_k_dev, const float* table_dev, const int32_t* pos_dev, void* q_out_dev,
                                void* k_out_dev, void* stream) {
-  LORACT_TRY(check_qk(p, false));
+  LORACT_TRY(check_qk(p));
   const bool keys = p->heads_k > 0;
   if (!q_dev || !q_out_dev || (keys && (!k_dev || !k_out_dev)) || (p->rot && !table_dev)) return LORACT_ERR_INVALID_ARG;
   const QkOperands in = {qk_extent(p, q_dev, p->heads_q, p->q_token, p->q_head), qk_extent(p, k_dev, p->heads_k, p->k_token, p->k_head), {}, {},
@@ -246,7 +246,7 @@ int loract_qknorm_rope_backward(const void* q_dev, const void* k_dev, const lora
                                 const float* gamma_k_dev, const float* table_dev, const int32_t* pos_dev,
                                 const void* dq_out_dev, const void* dk_out_dev, void* dq_dev, void* dk_dev,
                                 float* dgamma_q_dev, float* dgamma_k_dev, void* ws_dev, size_t ws_bytes, void* stream) {
-  LORACT_TRY(check_qk(p, true));
+  LORACT_TRY(check_qk(p));
   const bool keys = p->heads_k > 0;
   if (!q_dev || !dq_out_dev || !dq_dev || (keys && (!k_dev || !dk_out_dev || !dk_dev)) || (p->rot && !table_dev) ||
       (dgamma_k_dev && !keys))
