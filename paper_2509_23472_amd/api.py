@@ -38,12 +38,14 @@ def _check(code: int, where: str) -> None:
         raise LoractError(code, where)
 
 
+_DTYPE_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 def _dtype_code(dt: torch.dtype) -> int:
-    if dt == torch.float32:
-        return F32
-    if dt == torch.bfloat16:
-        return BF16
-    raise TypeError("unsupported dtype %s (float32 or bfloat16)" % dt)
+    code = _DTYPE_CODES.get(dt)
+    if code is None:
+        raise TypeError("unsupported dtype %s (float32 or bfloat16)" % dt)
+    return code
 
 
 def _torch_dtype(code: int) -> torch.dtype:
@@ -361,9 +363,9 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def _enqueue(call, args: tuple, query, params: bytes, t: torch.Tensor, where: str) -> None:
     """call(*args, workspace, its bytes, stream) on the stream's cached workspace, or where that is too small (which a call says before it
-    enqueues anything) or the stream is being captured on one of the size that `query` gives."""
+    enqueues anything) or the stream is being captured on one of the size that `query` gives (None: the call needs none)."""
     stream = _stream_ptr()
-    held = None if torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((t.get_device(), stream))
+    held = None if query is None or torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((t.get_device(), stream))
     code = call(*args, None, 0, stream) if held is None else call(*args, held.data_ptr(), held.numel(), stream)
     if code == _WORKSPACE_TOO_SMALL:
         nbytes = ctypes.c_size_t()
@@ -432,7 +434,7 @@ def loract_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor]
     ldr, r_ptr = (0, None) if residual is None else (_rows(residual, m, n_out, dt, "residual"), residual.data_ptr())
     bias_ptr = None if bias is None else _floats(bias, n_out, "bias")
     if out is None:
-        out, ldy = x.new_empty((m, n_out), dtype=odt), n_out
+        out, ldy = x.new_empty((m, n_out)) if odt is dt else x.new_empty((m, n_out), dtype=odt), n_out
     else:
         ldy = _rows(out, m, n_out, odt, "out")
     z = x.new_empty((m, n_out)) if save_preact else None
@@ -478,7 +480,7 @@ def loract_linear_backward(dy: torch.Tensor, z: Optional[torch.Tensor] = None, *
     params = _LINEAR_PARAMS.pack(m, 1, n, 0, 0, 0, ldy, ldz, ldp, _dtype_code(dt), 0, 0, act_code, r, lora_scale, p_drop, seed & _SEED)
     lib = _lib.load()
     _enqueue(lib.loract_linear_backward, (dy.data_ptr(), z_ptr, t_ptr, params, out.data_ptr(), _ptr(db), _ptr(d_b)),
-             lib.loract_linear_backward_workspace_bytes, params, dy, "loract_linear_backward")
+             lib.loract_linear_backward_workspace_bytes if bias_grad or r else None, params, dy, "loract_linear_backward")
     return out, db, d_b
 
 
@@ -571,7 +573,7 @@ def loract_qknorm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], gamm
     lib = _lib.load()
     _enqueue(lib.loract_qknorm_rope_backward, (q.data_ptr(), _ptr(k), params, gq, gk, _ptr(table), _ptr(positions), dq_out.data_ptr(),
                                                _ptr(dk_out), dq.data_ptr(), _ptr(dk), _ptr(dgq), _ptr(dgk)),
-             lib.loract_qknorm_rope_workspace_bytes, params, q, "loract_qknorm_rope_backward")
+             lib.loract_qknorm_rope_workspace_bytes if dgq is not None or dgk is not None else None, params, q, "loract_qknorm_rope_backward")
     return dq, dk, dgq, dgk
 
 
