@@ -335,10 +335,17 @@ _SEED = 2 ** 64 - 1
 _WORKSPACE_TOO_SMALL = -2
 
 
-def _rows(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str) -> int:
-    """Leading dimension of a GPU matrix of that shape and type with unit column stride."""
-    if t.shape != (rows, cols) or t.dtype is not dtype or not t.is_cuda:
-        raise ValueError("%s must be a %d x %d GPU tensor of %s" % (what, rows, cols, dtype))
+def _stream_on(device: int) -> int:
+    """The current stream of the GPU that a call's tensors live on, which must be the current one: there the kernels run."""
+    if torch._C._cuda_getDevice() != device:
+        raise ValueError("the tensors live on GPU %d, which is not the current one" % device)
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _rows(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str, device: int) -> int:
+    """Leading dimension of a matrix of that shape and type with unit column stride on that GPU (negative: none)."""
+    if t.shape != (rows, cols) or t.dtype is not dtype or t.get_device() != device or device < 0:
+        raise ValueError("%s must be a %d x %d tensor of %s on one GPU with the others" % (what, rows, cols, dtype))
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("%s must have unit column stride" % what)
@@ -349,11 +356,11 @@ def _rows(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str) 
     return ld
 
 
-def _floats(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+def _floats(t: Optional[torch.Tensor], n: int, what: str, device: int) -> Optional[int]:
     if t is None:
         return None
-    if t.shape != (n,) or t.dtype is not torch.float32 or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError("%s must be a contiguous float32 GPU tensor of length %d" % (what, n))
+    if t.shape != (n,) or t.dtype is not torch.float32 or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError("%s must be a contiguous float32 tensor of length %d on one GPU with the others" % (what, n))
     return t.data_ptr()
 
 
@@ -361,16 +368,16 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _enqueue(call, args: tuple, query, params: bytes, t: torch.Tensor, where: str) -> None:
+def _enqueue(call, args: tuple, query, params: bytes, device: int, where: str) -> None:
     """call(*args, workspace, its bytes, stream) on the stream's cached workspace, or where that is too small (which a call says before it
     enqueues anything) or the stream is being captured on one of the size that `query` gives (None: the call needs none)."""
-    stream = _stream_ptr()
-    held = None if query is None or torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((t.get_device(), stream))
+    stream = _stream_on(device)
+    held = None if query is None or torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((device, stream))
     code = call(*args, None, 0, stream) if held is None else call(*args, held.data_ptr(), held.numel(), stream)
     if code == _WORKSPACE_TOO_SMALL:
         nbytes = ctypes.c_size_t()
         _check(query(params, ctypes.byref(nbytes)), where + "_workspace_bytes")
-        held = _workspace(nbytes.value, t.device)
+        held = _workspace(nbytes.value, torch.device("cuda", device))
         code = call(*args, held.data_ptr(), held.numel(), stream)
     if code:
         raise LoractError(code, where)
@@ -390,17 +397,17 @@ def loract_dropout(x: torch.Tensor, p_drop: float, seed: int, residual: Optional
     if x.dim() != 2:
         raise ValueError("x must be a matrix")
     m, n = x.shape
-    dt = x.dtype
-    ldx = _rows(x, m, n, dt, "x")
-    ldr = 0 if residual is None else _rows(residual, m, n, dt, "residual")
+    dt, dev = x.dtype, x.get_device()
+    ldx = _rows(x, m, n, dt, "x", dev)
+    ldr = 0 if residual is None else _rows(residual, m, n, dt, "residual", dev)
     if out is None:
         out, ldy = x.new_empty((m, n)), n
     else:
-        ldy = _rows(out, m, n, dt, "out")
+        ldy = _rows(out, m, n, dt, "out", dev)
     if m == 0 or n == 0:
         return out
     code = _lib.load().loract_dropout(x.data_ptr(), ldx, _ptr(residual), ldr, m, n, _dtype_code(dt), p_drop, seed & _SEED,
-                                      out.data_ptr(), ldy, _stream_ptr())
+                                      out.data_ptr(), ldy, _stream_on(dev))
     if code:
         raise LoractError(code, "loract_dropout")
     return out
@@ -419,31 +426,31 @@ def loract_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor]
         raise ValueError("x and w must be matrices")
     m, n_in = x.shape
     n_out = w.shape[1 if w_transposed else 0]
-    dt = x.dtype
+    dt, dev = x.dtype, x.get_device()
     odt = dt if out_dtype is None else out_dtype
-    ldx = _rows(x, m, n_in, dt, "x")
-    ldw = _rows(w, n_in, n_out, dt, "w") if w_transposed else _rows(w, n_out, n_in, dt, "w")
+    ldx = _rows(x, m, n_in, dt, "x", dev)
+    ldw = _rows(w, n_in, n_out, dt, "w", dev) if w_transposed else _rows(w, n_out, n_in, dt, "w", dev)
     r, t_ptr, b_ptr = 0, None, None
     if lora_t is not None or lora_b is not None:
         if lora_t is None or lora_b is None:
             raise ValueError("lora_t and lora_b go together")
         r = lora_b.shape[0]
-        if _rows(lora_t, m, r, dt, "lora_t") != r or _rows(lora_b, r, n_out, dt, "lora_b") != n_out:
+        if _rows(lora_t, m, r, dt, "lora_t", dev) != r or _rows(lora_b, r, n_out, dt, "lora_b", dev) != n_out:
             raise ValueError("lora_t and lora_b must be contiguous")
         t_ptr, b_ptr = lora_t.data_ptr(), lora_b.data_ptr()
-    ldr, r_ptr = (0, None) if residual is None else (_rows(residual, m, n_out, dt, "residual"), residual.data_ptr())
-    bias_ptr = None if bias is None else _floats(bias, n_out, "bias")
+    ldr, r_ptr = (0, None) if residual is None else (_rows(residual, m, n_out, dt, "residual", dev), residual.data_ptr())
+    bias_ptr = None if bias is None else _floats(bias, n_out, "bias", dev)
     if out is None:
         out, ldy = x.new_empty((m, n_out)) if odt is dt else x.new_empty((m, n_out), dtype=odt), n_out
     else:
-        ldy = _rows(out, m, n_out, odt, "out")
+        ldy = _rows(out, m, n_out, odt, "out", dev)
     z = x.new_empty((m, n_out)) if save_preact else None
     if m:
         params = _LINEAR_PARAMS.pack(m, n_in, n_out, ldx, ldw, ldr, ldy, n_out, 0, _dtype_code(dt), _dtype_code(odt),
                                      W_IN_OUT if w_transposed else W_OUT_IN, _act_code(act), r, lora_scale, p_drop, seed & _SEED)
         lib = _lib.load()
         _enqueue(lib.loract_linear, (x.data_ptr(), w.data_ptr(), bias_ptr, t_ptr, b_ptr, r_ptr, params, out.data_ptr(), _ptr(z)),
-                 lib.loract_linear_workspace_bytes, params, x, "loract_linear")
+                 lib.loract_linear_workspace_bytes, params, dev, "loract_linear")
     return (out, z) if save_preact else out
 
 
@@ -457,22 +464,22 @@ def loract_linear_backward(dy: torch.Tensor, z: Optional[torch.Tensor] = None, *
     if dy.dim() != 2:
         raise ValueError("dy must be a matrix")
     m, n = dy.shape
-    dt = dy.dtype
-    ldy = _rows(dy, m, n, dt, "dy")
+    dt, dev = dy.dtype, dy.get_device()
+    ldy = _rows(dy, m, n, dt, "dy", dev)
     act_code, ldz, z_ptr = _act_code(act), 0, None
     if act_code:
         if z is None:
             raise ValueError("the slope of an activation needs z")
-        ldz, z_ptr = _rows(z, m, n, dt, "z"), z.data_ptr()
+        ldz, z_ptr = _rows(z, m, n, dt, "z", dev), z.data_ptr()
     if out is None:
         out, ldp = dy.new_empty((m, n)), n
     else:
-        ldp = _rows(out, m, n, dt, "out")
+        ldp = _rows(out, m, n, dt, "out", dev)
     db = dy.new_empty((n,), dtype=torch.float32) if bias_grad else None
     r, t_ptr, d_b = 0, None, None
     if lora_t is not None:
         r = lora_t.shape[1] if lora_t.dim() == 2 else 0
-        if _rows(lora_t, m, r, dt, "lora_t") != r:
+        if _rows(lora_t, m, r, dt, "lora_t", dev) != r:
             raise ValueError("lora_t must be contiguous")
         t_ptr, d_b = lora_t.data_ptr(), dy.new_empty((r, n), dtype=torch.float32)
     if m == 0:
@@ -480,7 +487,7 @@ def loract_linear_backward(dy: torch.Tensor, z: Optional[torch.Tensor] = None, *
     params = _LINEAR_PARAMS.pack(m, 1, n, 0, 0, 0, ldy, ldz, ldp, _dtype_code(dt), 0, 0, act_code, r, lora_scale, p_drop, seed & _SEED)
     lib = _lib.load()
     _enqueue(lib.loract_linear_backward, (dy.data_ptr(), z_ptr, t_ptr, params, out.data_ptr(), _ptr(db), _ptr(d_b)),
-             lib.loract_linear_backward_workspace_bytes if bias_grad or r else None, params, dy, "loract_linear_backward")
+             lib.loract_linear_backward_workspace_bytes if bias_grad or r else None, params, dev, "loract_linear_backward")
     return out, db, d_b
 
 
@@ -489,14 +496,14 @@ def loract_rope_table(n_pos: int, rot: int, theta: float = 10000.0, first: int =
     """Cosines and sines of positions first .. first + n_pos - 1: n_pos x 2 x rot / 2 float32, angles in float64."""
     device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
     table = torch.empty((n_pos, 2, rot // 2), dtype=torch.float32, device=device)
-    _check(_lib.load().loract_rope_table(table.data_ptr(), n_pos, rot, float(theta), first, _stream_ptr()), "loract_rope_table")
+    _check(_lib.load().loract_rope_table(table.data_ptr(), n_pos, rot, float(theta), first, _stream_on(table.get_device())), "loract_rope_table")
     return table
 
 
-def _heads(t: torch.Tensor, m: int, heads: int, d: int, dtype: torch.dtype, what: str, written: bool = False) -> Tuple[int, int]:
-    """Token and head strides of a GPU tensor tokens x heads x d with contiguous heads, which must not overlap if `written`."""
-    if t.shape != (m, heads, d) or t.dtype is not dtype or not t.is_cuda:
-        raise ValueError("%s must be a GPU tensor of %d tokens x %d heads x %d of %s" % (what, m, heads, d, dtype))
+def _heads(t: torch.Tensor, m: int, heads: int, d: int, dtype: torch.dtype, what: str, device: int, written: bool = False) -> Tuple[int, int]:
+    """Token and head strides of a tensor tokens x heads x d on that GPU with contiguous heads, which must not overlap if `written`."""
+    if t.shape != (m, heads, d) or t.dtype is not dtype or t.get_device() != device or device < 0:
+        raise ValueError("%s must be a tensor of %d tokens x %d heads x %d of %s on one GPU with the others" % (what, m, heads, d, dtype))
     token, head, step = t.stride()
     if step != 1 and d > 1:
         raise ValueError("the heads of %s must be contiguous" % what)
@@ -510,24 +517,24 @@ def _qk_call(q, k, gamma_q, gamma_k, table, positions, eps, interleaved, q_out, 
     if q.dim() != 3 or (k is not None and k.dim() != 3):
         raise ValueError("q and k must be tokens x heads x head size")
     m, hq, d = q.shape
-    dt = q.dtype
+    dt, dev = q.dtype, q.get_device()
     hk = 0 if k is None else k.shape[1]
     n_pos, rot = 0, 0
     if table is not None:
-        if table.dim() != 3 or table.shape[1] != 2 or table.dtype is not torch.float32 or not table.is_contiguous() or not table.is_cuda:
-            raise ValueError("table must come from loract_rope_table (positions x 2 x rot / 2, float32)")
+        if table.dim() != 3 or table.shape[1] != 2 or table.dtype is not torch.float32 or not table.is_contiguous() or table.get_device() != dev:
+            raise ValueError("table must come from loract_rope_table (positions x 2 x rot / 2, float32) and live with q")
         n_pos, rot = table.shape[0], 2 * table.shape[2]
     if positions is not None and (positions.shape != (m,) or positions.dtype is not torch.int32 or
-                                  not positions.is_contiguous() or not positions.is_cuda):
-        raise ValueError("positions must be a contiguous int32 GPU tensor with one entry per token")
-    strides = _heads(q, m, hq, d, dt, "q")
-    strides += (0, 0) if k is None else _heads(k, m, hk, d, dt, "k")
-    strides += (hq * d, d) if q_out is None else _heads(q_out, m, hq, d, dt, "out", True)
-    strides += (hk * d, d) if k_out is None else _heads(k_out, m, hk, d, dt, "out", True)
-    strides += (0, 0) if dq is None else _heads(dq, m, hq, d, dt, "dq_out")
-    strides += (0, 0) if dk is None else _heads(dk, m, hk, d, dt, "dk_out")
+                                  not positions.is_contiguous() or positions.get_device() != dev):
+        raise ValueError("positions must be a contiguous int32 tensor with one entry per token and live with q")
+    strides = _heads(q, m, hq, d, dt, "q", dev)
+    strides += (0, 0) if k is None else _heads(k, m, hk, d, dt, "k", dev)
+    strides += (hq * d, d) if q_out is None else _heads(q_out, m, hq, d, dt, "out", dev, True)
+    strides += (hk * d, d) if k_out is None else _heads(k_out, m, hk, d, dt, "out", dev, True)
+    strides += (0, 0) if dq is None else _heads(dq, m, hq, d, dt, "dq_out", dev)
+    strides += (0, 0) if dk is None else _heads(dk, m, hk, d, dt, "dk_out", dev)
     params = _QK_PARAMS.pack(m, hq, hk, d, rot, 1 if interleaved else 0, _dtype_code(dt), n_pos, eps, *strides)
-    return params, _floats(gamma_q, d, "gamma_q"), None if k is None else _floats(gamma_k, d, "gamma_k")
+    return params, _floats(gamma_q, d, "gamma_q", dev), None if k is None else _floats(gamma_k, d, "gamma_k", dev)
 
 
 def loract_qknorm_rope_forward(q: torch.Tensor, k: Optional[torch.Tensor], gamma_q: Optional[torch.Tensor],
@@ -546,7 +553,7 @@ def loract_qknorm_rope_forward(q: torch.Tensor, k: Optional[torch.Tensor], gamma
         qo, ko = q.new_empty(q.shape), None if k is None else q.new_empty(k.shape)
     if q.shape[0]:
         code = _lib.load().loract_qknorm_rope_forward(q.data_ptr(), _ptr(k), params, gq, gk, _ptr(table), _ptr(positions),
-                                                      qo.data_ptr(), _ptr(ko), _stream_ptr())
+                                                      qo.data_ptr(), _ptr(ko), _stream_on(q.get_device()))
         if code:
             raise LoractError(code, "loract_qknorm_rope_forward")
     return qo, ko
@@ -573,7 +580,7 @@ def loract_qknorm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], gamm
     lib = _lib.load()
     _enqueue(lib.loract_qknorm_rope_backward, (q.data_ptr(), _ptr(k), params, gq, gk, _ptr(table), _ptr(positions), dq_out.data_ptr(),
                                                _ptr(dk_out), dq.data_ptr(), _ptr(dk), _ptr(dgq), _ptr(dgk)),
-             lib.loract_qknorm_rope_workspace_bytes if dgq is not None or dgk is not None else None, params, q, "loract_qknorm_rope_backward")
+             lib.loract_qknorm_rope_workspace_bytes if dgq is not None or dgk is not None else None, params, q.get_device(), "loract_qknorm_rope_backward")
     return dq, dk, dgq, dgk
 
 
