@@ -577,10 +577,14 @@ def loract_qknorm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], gamm
     dgk = None if gk is None else q.new_empty((d,), dtype=torch.float32)
     if q.shape[0] == 0:
         return dq, dk, dgq if dgq is None else dgq.zero_(), dgk if dgk is None else dgk.zero_()
+    dgk_ptr = _ptr(dgk)
+    if dgk is not None and k.shape[1] == 0:            # (the library knows no gradient of keys that are not there)
+        dgk_ptr = None
+        dgk.zero_()
     lib = _lib.load()
     _enqueue(lib.loract_qknorm_rope_backward, (q.data_ptr(), _ptr(k), params, gq, gk, _ptr(table), _ptr(positions), dq_out.data_ptr(),
-                                               _ptr(dk_out), dq.data_ptr(), _ptr(dk), _ptr(dgq), _ptr(dgk)),
-             lib.loract_qknorm_rope_workspace_bytes if dgq is not None or dgk is not None else None, params, q.get_device(), "loract_qknorm_rope_backward")
+                                               _ptr(dk_out), dq.data_ptr(), _ptr(dk), _ptr(dgq), dgk_ptr),
+             lib.loract_qknorm_rope_workspace_bytes if dgq is not None or dgk_ptr else None, params, q.get_device(), "loract_qknorm_rope_backward")
     return dq, dk, dgq, dgk
 
 
