@@ -421,7 +421,7 @@ def loract_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor]
 
     x m x n_in; w n_out x n_in, or n_in x n_out with `w_transposed` (the forward's weights, for the input gradient);
     bias n_out floats; lora_t m x r and lora_b r x n_out; act none, relu, gelu or silu.  Returns Y, or (Y, Z) with
-    `save_preact`: Z = P rounded to x's type, for loract_linear_backward."""
+    `save_preact`: Z = P rounded to x's type, for loract_linear_backward.  `out` may be residual, but share no memory with the others."""
     if x.dim() != 2 or w.dim() != 2:
         raise ValueError("x and w must be matrices")
     m, n_in = x.shape
@@ -460,7 +460,7 @@ def loract_linear_backward(dy: torch.Tensor, z: Optional[torch.Tensor] = None, *
                            ) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
     """dP = act'(z) D(dy), the bias gradient (n_out floats; None without `bias_grad`) and lora_scale lora_t^T dP
     (r x n_out floats; None without `lora_t`), in one pass.  z is what loract_linear kept with `save_preact`; it may
-    be None without an activation.  `out` (dP) may be dy."""
+    be None without an activation.  `out` (dP) may be dy or z."""
     if dy.dim() != 2:
         raise ValueError("dy must be a matrix")
     m, n = dy.shape

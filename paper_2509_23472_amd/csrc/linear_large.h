@@ -10,8 +10,8 @@
 // of W per row: 8192 x 8192 -> 2048 203 us against 194), products of 16 x 16 x 32 rather than 32 x 32 x 16, which move half the
 // accumulators (218 against 205 of W as it lies).  Four waves of 128 x 128 with all accumulators in 256 accumulation registers
 // read a third less from LDS and were no faster (225): alone on its matrix unit, a wave that waits for the issue of a copy leaves it idle.
-// 8192 x 4096 -> 4096 201 us (1367 TFLOP/s), 8192 x 4096 -> 11008 646 (1143: 1376 tiles are 5.4 rounds), 8192 x 11008 -> 4096 of W as it
-// lies 555 (1331); a library's plain products take 184 to 192, 640 and 540 to 630 us.
+// 8192 x 4096 -> 4096 199 us (1384 TFLOP/s), 8192 x 4096 -> 11008 605 (1221: 1376 tiles are 5.4 rounds), 8192 x 11008 -> 4096 of W as it
+// lies 556 (1329); a library's plain products take 177, 636 and 537 us.  Many in a row lower the clock further: the first then takes 214.
 #pragma once
 #include "linear_tile.h"
 
@@ -370,7 +370,8 @@ __global__ __launch_bounds__(64 * ll_waves(TILE), TILE == 256 ? 1 : 2) void line
 // 35.  Measured (256 / 128 x 128): 2048 x 2048 -> 2048 46 / 26 us, 8192 x 4096 -> 1024 92 / 70, 6000 x 4096 -> 3000 177 / 165, 2048 x
 // 4096 -> 11008 195 / 195, 5000 x 2048 -> 2048 48 / 52, 4096 x 4096 -> 4096 123 / 155, 8192 x 4096 -> 11008 619 / 725.
 // Where even the smaller tiles leave CUs without work, K is split in parts of at least 512: 256 x 4096 -> 4096 36 -> 24 us, 128 x
-// 11008 -> 4096 124 -> 33; more than one workgroup per CU loses to the join (2048 x 2048 -> 2048 26 -> 39).
+// 11008 -> 4096 124 -> 33; more than one workgroup per CU loses to the join (2048 x 2048 -> 2048 26 -> 39).  What this leaves: 256 x 4096 ->
+// 4096 is at 3.5 times its floor of bytes (a library's product 22 us), 128 x 11008 -> 4096 at 1.7 (56), 1024 x 4096 -> 4096 50 us (41).
 struct LargePlan {
   int tile, splits;
 };

@@ -5,11 +5,11 @@
 // holds eight consecutive k of one row (float32: four, one for each of four v_mfma_f32_16x16x4_f32).  The eight waves of a workgroup
 // share its rows and split K, so that 16 rows are enough to keep a CU's share of the memory system busy; their sums are added in LDS
 // in a fixed order, then comes the epilogue.
-// One token through 4096 -> 11008 22 us (4.1 TB/s; a copy 5.1), 8192 x 4096 -> 16 17 us (3.9), 65536 x 4096 -> 16 105 us (5.1): what a
-// short pass loses is its start.  A second trip's loads ahead of the products gave fewer waves and 31 us instead of 24.
-// float32 (the general tiles before): one token through 4096 -> 11008 34 us (64; 5.4 TB/s), 8192 x 4096 -> 16 30 us (61), 8 tokens
-// through 11008 -> 11008 114 (168); with 17 to 32 rows on both sides its products weigh as much as its reads: 32 tokens through
-// 8192 -> 8192 75 (99), 12096 x 9920 -> 30 142 (161; 170 with twice the steps in flight, at half the waves).
+// One token through 4096 -> 11008 17.6 us (5.1 TB/s; a copy 5.1), with bias, 16 columns of B and SiLU 22, 8192 x 4096 -> 16 16 us (4.2), 65536 x
+// 4096 -> 16 100 us (5.4): what a short pass loses is its start, and with 17 to 32 tokens half of a wave's loads are X (32 us).  A second trip's loads ahead of the products gave fewer waves and 31 us instead of 24.
+// float32 (the general tiles before): one token through 4096 -> 11008 33 us (64; 5.4 TB/s), 8192 x 4096 -> 16 29 us (61), 8 tokens
+// through 11008 -> 11008 112 (168); with 17 to 32 rows on both sides its products weigh as much as its reads: 32 tokens through
+// 8192 -> 8192 74 (99), 12096 x 9920 -> 30 142 (161; 170 with twice the steps in flight, at half the waves).
 // Accumulators start with the low-rank term (the first waves, one step of its rank each), scaled in float32.
 #pragma once
 #include "linear_large.h"

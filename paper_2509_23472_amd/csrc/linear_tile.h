@@ -9,8 +9,8 @@
 // bf16 runs on v_mfma_f32_32x32x16_bf16, float32 on v_mfma_f32_32x32x2_f32 (a sixteenth of the rate): there a lane
 // reads four consecutive k at once and the four products take one of them each, the same one for both operands.
 //
-// float32 is bound by its matrix instructions: 8192 x 1024 -> 4096 568 us, 121 TFLOP/s where a library's plain product reaches 144.
-// bf16 comes here with rows that are no pieces or with sizes that are too small for copies to pay: 700 x 1030 -> 700 16 us.
+// float32 is bound by its matrix instructions: 8192 x 1024 -> 4096 563 us, 122 TFLOP/s where a library's plain product reaches 144.
+// bf16 comes here with rows that are no pieces or with sizes that are too small for copies to pay: 700 x 1030 -> 700 15 us.
 #pragma once
 #include "gemm_bf16.h"
 #include "linear_epilogue.h"
@@ -304,8 +304,8 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
 
 // Tiles: 128 x 128 (64 in a direction that has no more), but 64 x 64 for float32 where the large ones leave CUs without work or
 // need a second round for less than half of the card: a float32 tile of 128 x 128 is matrix instructions for 55 us per 1024 of K
-// whatever feeds it, so small ones lose nothing but traffic and balance better (1024 x 256 -> 256 20 -> 13 us, 500 x 500 -> 500 26 -> 15,
-// 12608 x 768 -> 768 210 -> 190; 4096 x 1024 -> 4096, which they do not take, 305 -> 339).
+// whatever feeds it, so small ones lose nothing but traffic and balance better (1024 x 256 -> 256 26 -> 10 us, 500 x 500 -> 500 44 -> 16,
+// 12608 x 768 -> 768 168 -> 146; 4096 x 1024 -> 4096, which they do not take, 284 -> 293).
 // K splits: as many as make 512 workgroups (1024 of the small float32 tiles), of at least 256 of K each, at most 64.
 struct TilePlan {
   int bm, bn, splits;

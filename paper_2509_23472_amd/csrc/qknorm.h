@@ -11,8 +11,8 @@
 // lane it comes by a lane exchange.  A wave keeps to one token while it walks over the heads, so that cos, sin and gamma
 // stay in registers: the table is 2 to 4 times the bytes of a bf16 head, and would otherwise pass through L1 for each.
 // gamma's gradients are summed in registers over the rows of a wave, then over the waves in LDS and over the
-// workgroups through partial sums, in a fixed order.  8192 tokens of 32 + 8 heads of 128 bf16: forward 39 us (4.3 TB/s; a copy 5.1),
-// backward 57 us with its join (4.4).
+// workgroups through partial sums, in a fixed order.  8192 tokens of 32 + 8 heads of 128 bf16: forward 38 us (4.4 TB/s; a copy 5.1),
+// backward 52 us with its join (4.8); float32 62 and 104.
 #pragma once
 #include "common.h"
 
