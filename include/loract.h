@@ -271,7 +271,8 @@ typedef struct {
  *           T = X A (itself a call with W = A), as B_lora of loract_lora_grad; not read if r_lora is 0.
  * R_dev     m x n_out, or NULL.   Y_dev out, m x n_out of out_dtype; Y may be R where their types and ld are the same.
  * Z_dev     out, m x n_out of dtype, or NULL: P rounded to dtype, what the backward pass reads.
- * m, n_in, n_out up to 2^30 (n_in below 8, or n_out below 8 with LORACT_W_IN_OUT: m up to 2^30 - 64), else LORACT_ERR_UNSUPPORTED, of the query too.
+ * m, n_in, n_out up to 2^30 (n_in below 8, or n_out below 8 with LORACT_W_IN_OUT: m up to 2^30 - 64), else LORACT_ERR_UNSUPPORTED, from
+ * the workspace query too.
  * Sums are float32.  Workspace: loract_linear_workspace_bytes.  NaN and infinities of X and W reach the outputs they belong to.
  */
 int loract_linear_workspace_bytes(const loract_linear_params* p, size_t* bytes);
@@ -283,8 +284,8 @@ int loract_linear(const void* X_dev, const void* W_dev, const float* bias_dev, c
  * Backward of loract_linear up to the products, one pass over dY and Z:
  *   dP = act'(Z) D(dY),   dbias_j = sum_i dP_ij,   dB_lora = lora_scale T^T dP
  * Z_dev     what the forward call kept; not read (may be NULL) without an activation.
- * dP_dev    out, m x n_out of dtype; may be dY or Z with the same ld.   dbias_dev out, n_out floats, or NULL.   dB_dev out, r_lora x n_out floats, or NULL
- *           (then T_dev is not read).  The sums are of the unrounded float32 dP.
+ * dP_dev    out, m x n_out of dtype; may be dY or Z with the same ld.   dbias_dev out, n_out floats, or NULL.
+ * dB_dev    out, r_lora x n_out floats, or NULL (then T_dev is not read).  The sums are of the unrounded float32 dP.
  * The rest of the backward pass are calls on dP: dT = lora_scale dP B_lora^T and dX = dP W + dT A^T by loract_linear,
  * dA by loract_lora_grad.  Workspace: loract_linear_backward_workspace_bytes.
  */
@@ -321,6 +322,7 @@ typedef struct {
  * forward   q_out may be q, k_out may be k (with the same strides).
  * backward  from the inputs and the gradients of the outputs: dq, dk and, where not NULL, dgamma_q, dgamma_k (d floats).
  *           dq may be dq_out or q, dk dk_out or k (with the same strides).
+ * The heads of an output lie apart: its larger stride is at least what all heads (or tokens) of the smaller one span.
  * No workspace in the forward direction; loract_qknorm_rope_workspace_bytes in the backward one.
  */
 int loract_qknorm_rope_workspace_bytes(const loract_qk_params* p, size_t* bytes);

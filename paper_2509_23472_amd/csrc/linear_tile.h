@@ -150,8 +150,8 @@ __device__ inline void lin_multiply(const f32x4 (&w)[NT], const f32x4 (&x)[MT], 
 }
 
 // TINY: K, or the rows of W stored n_in x n_out, are shorter than a piece (the low-rank term's always may be).
-// WKC: W is n_out x n_in (rows along K), else n_in x n_out.  BM x BN tile, four waves of BM/2 x BN/2.  blockIdx.x: row of tiles, blockIdx.y: column,
-// blockIdx.z: split of K, or where K is whole what the number of columns has beyond LT_MAX_Y.
+// WKC: W is n_out x n_in (rows along K), else n_in x n_out.  BM x BN tile, four waves of BM/2 x BN/2.  blockIdx.x: row of tiles, blockIdx.y: column;
+// blockIdx.z: split of K, or where K is whole and there are more than LT_MAX_Y columns, further columns.
 #define LT_MAX_Y 65535
 template <typename T, bool WKC, int BM, int BN, bool TINY>
 __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
@@ -177,9 +177,9 @@ __global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g) {
 #pragma unroll
   for (int i = 0; i < MT; ++i) x_off[i] = OpX::frag_off(wm * (BM / 2) + 32 * i, lane);
 
-  // TWO: odd and even steps of K have an accumulator each, which shortens the chain of roundings.  Where the tile leaves the registers for it: 3001 x
-  // 1030 -> 770 is 6.9 units of 2^-24 off (rms) instead of 9.7 in the same time; W as it lies 1024 x 256 -> 256 11.0 -> 11.6 us, tiles of 128 x 128
-  // 565 -> 633.
+  // TWO: odd and even steps of K have an accumulator each, which shortens the chain of roundings, where that costs nothing: 3001 x 1030 ->
+  // 770 is 6.9 units of 2^-24 off (rms) instead of 9.7 in the same time; W as it lies 1024 x 256 -> 256 would take 11.6 us instead of 11.0, tiles of
+  // 128 x 128 (8192 x 1024 -> 4096) 633 instead of 565.
   constexpr bool TWO = sizeof(T) == 4 && WKC && BM == 64 && BN == 64;
   f32x16 acc[MT][NT], odd[TWO ? MT : 1][TWO ? NT : 1];
 #pragma unroll

@@ -190,8 +190,8 @@ struct QkOperands {
 };
 static bool qk_outputs_meet(const loract_qk_params* p, const QkOperands& in, const Extent& oq, const Extent& ok, const Extent& scratch, const float* dgq,
                             const float* dgk) {
-  const Extent read[] = {extent_bytes(in.gamma_q, p->d * 4), extent_bytes(in.gamma_k, p->d * 4), extent_bytes(p->rot ? in.table : nullptr, (wide_t)p->n_pos * p->rot * 4),
-                         extent_bytes(in.pos, p->m * 4), scratch};
+  const Extent read[] = {extent_bytes(in.gamma_q, p->d * 4), extent_bytes(in.gamma_k, p->d * 4), extent_bytes(in.pos, p->m * 4), scratch,
+                         extent_bytes(p->rot ? in.table : nullptr, (wide_t)p->n_pos * p->rot * 4)};
   const Extent g[] = {extent_bytes(dgq, p->d * 4), extent_bytes(dgk, p->d * 4)};
   for (const Extent& e : read)
     if (extents_meet(oq, e) || extents_meet(ok, e) || extents_meet(g[0], e) || extents_meet(g[1], e)) return true;
