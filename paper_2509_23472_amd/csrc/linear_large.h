@@ -10,8 +10,8 @@
 // of W per row: 8192 x 8192 -> 2048 203 us against 194), products of 16 x 16 x 32 rather than 32 x 32 x 16, which move half the
 // accumulators (218 against 205 of W as it lies).  Four waves of 128 x 128 with all accumulators in 256 accumulation registers
 // read a third less from LDS and were no faster (225): alone on its matrix unit, a wave that waits for the issue of a copy leaves it idle.
-// 8192 x 4096 -> 4096 199 us (1384 TFLOP/s), 8192 x 4096 -> 11008 605 (1221: 1376 tiles are 5.4 rounds), 8192 x 11008 -> 4096 of W as it
-// lies 556 (1329); a library's plain products take 177, 636 and 537 us.  Many in a row lower the clock further: the first then takes 214.
+// 8192 x 4096 -> 4096 199 to 214 us from one program to another (1384 to 1284 TFLOP/s), 8192 x 4096 -> 11008 605 (1221: 1376 tiles are 5.4 rounds), 8192 x 11008 -> 4096 of W as it
+// lies 556 (1329); a library's plain products take 177, 636 and 537 us beside 199, 605 and 556.
 #pragma once
 #include "linear_tile.h"
 
