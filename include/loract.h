@@ -335,6 +335,45 @@ int loract_qknorm_rope_backward(const void* q_dev, const void* k_dev, const lora
                                 float* dgamma_q_dev, float* dgamma_k_dev, void* ws_dev, size_t ws_bytes, void* stream);
 
 /*
+ * What a step ends with and what its adapters are for: their update, the loss, and the adapters of many requests.
+ * Outputs that share memory with each other, with the workspace or with what the call reads are refused as above.
+ */
+
+#define LORACT_ADAMW_BLOCK 256   /* elements of a state in 8 bits that share an exponent; tensors begin at multiples of it */
+
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;   /* lr, eps, weight_decay >= 0; 0 <= beta < 1 */
+  int64_t step;          /* t, from 1 on */
+  uint64_t seed;         /* of the random roundings */
+  int32_t p_dtype, g_dtype;      /* loract_dtype of the parameters and of the gradients */
+  int32_t state_bits;    /* 32 or 8 */
+} loract_adamw_params;
+
+/*
+ * One step of AdamW over `count` tensors at once; every operation in float32 and in this order:
+ *   g = grad_scale g,  m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) (g g),  r' = sqrt(v')
+ *   p' = (1 - lr weight_decay) p - (lr / (1 - beta1^t)) (m' / (r' / sqrt(1 - beta2^t) + eps))
+ * p, g, copy, n    arrays of `count` in host memory, read before the call returns: the tensors' device pointers (contiguous; p of
+ *                  p_dtype, updated in place; g of g_dtype) and their sizes (0: a tensor without elements).  copy, or any entry of it, may be
+ *                  NULL: else p' rounded to bf16 is written there too (float32 parameters only).
+ * m_dev, v_dev     the states of all tensors one after the other, each tensor padded to a multiple of LORACT_ADAMW_BLOCK elements, 16-byte
+ *                  aligned; all zero before the first step.  state_bits 32: m and v, floats; exps_dev is not read.
+ *                  state_bits 8: bytes, e4m3 numbers that stand for m and r = sqrt(v) in units of 2^(exps[block][0] - 127)
+ *                  and 2^(exps[block][1] - 127), the unit that takes a block's largest finite magnitude to 320/3 or more and below
+ *                  640/3, but exponents of 1 at least.  What is not finite is NaN from then on; a root that is not zero stays above zero.
+ * Roundings to fewer bits than 32 are random (nearest ones would hold a moment or a weight where a step's change is less than half a
+ * spacing), from a counter: element e of the state takes the lower (e even) or upper half of output floor(e / 2) + 1 of the splitmix64
+ * stream that starts at output t of `seed`: bits 0-9 for m, 10-19 for r, 20-31 for a bf16 parameter.  A magnitude goes up to its upper
+ * neighbour where its place between the two plus (bits + 1/2) / 2^10 (2^12) is at least 1.
+ * lr_dev, step_dev, grad_scale_dev   a float, an int64 and a float in device memory, read when the step runs, or NULL: p->lr, p->step, 1.  A
+ *                  captured step that is replayed takes what changes from these.  A step below 1 there gives NaN or infinities.
+ * n up to 2^33 each.  No workspace.
+ */
+int loract_adamw(void* const* p, const void* const* g, void* const* copy, const int64_t* n, int64_t count,
+                 const loract_adamw_params* params, void* m_dev, void* v_dev, uint8_t* exps_dev, const float* lr_dev,
+                 const int64_t* step_dev, const float* grad_scale_dev, void* stream);
+
+/*
  * Per-kernel timing with HIP events on the stream the kernels are launched on.
  * begin: start bracketing every kernel launch of this library with event records.
  * end:   stop, wait for the recorded events, and aggregate by kernel name.

@@ -1,5 +1,6 @@
 """LoRAct activation compression for AMD MI355X: Python binding of the libloract C ABI."""
-from .api import (ACTIVATIONS, BF16, F32, MAX_HEAD, MAX_LORA_RANK, MAX_RANK, STATUS_RANK_DEFICIENT, LoractError, loract_compress,
+from .api import (ACTIVATIONS, BF16, F32, MAX_HEAD, MAX_LORA_RANK, MAX_RANK, STATUS_RANK_DEFICIENT, LoractError,
+                  AdamwState, loract_adamw, loract_adamw_state, loract_compress,
                   loract_compress_adaptive, loract_dropout,
                   loract_gaussian_omega_t, loract_linear, loract_linear_backward, loract_lora_grad, loract_lora_grad_static,
                   loract_static_scratch_bytes, loract_prenorm_backward,
@@ -10,6 +11,7 @@ from .api import (ACTIVATIONS, BF16, F32, MAX_HEAD, MAX_LORA_RANK, MAX_RANK, STA
 
 __all__ = [
     "ACTIVATIONS", "BF16", "F32", "MAX_HEAD", "MAX_LORA_RANK", "MAX_RANK", "STATUS_RANK_DEFICIENT", "LoractError",
+    "AdamwState", "loract_adamw", "loract_adamw_state",
     "loract_compress", "loract_compress_adaptive", "loract_dropout",
     "loract_gaussian_omega_t", "loract_linear", "loract_linear_backward", "loract_lora_grad", "loract_lora_grad_static",
     "loract_static_scratch_bytes", "loract_prenorm_backward", "loract_prenorm_forward",

@@ -39,6 +39,13 @@ class LoractQkParams(ctypes.Structure):
                                               "ko_head", "dq_token", "dq_head", "dk_token", "dk_head")]
 
 
+class LoractAdamwParams(ctypes.Structure):
+    """Mirror of `loract_adamw_params` in include/loract.h (api.py packs the same bytes)."""
+    _fields_ = [(f, ctypes.c_double) for f in ("lr", "beta1", "beta2", "eps", "weight_decay")] + \
+               [("step", ctypes.c_int64), ("seed", ctypes.c_uint64)] + \
+               [(f, ctypes.c_int32) for f in ("p_dtype", "g_dtype", "state_bits")]
+
+
 _P = ctypes.POINTER
 _vp, _i32, _i64, _u64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
 
@@ -75,6 +82,7 @@ SIGNATURES = {
     "loract_qknorm_rope_forward": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "loract_qknorm_rope_backward": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                                    _vp, _vp, _vp, _sz, _vp]),
+    "loract_adamw": (ctypes.c_int, [_vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "loract_profile_begin": (ctypes.c_int, []),
     "loract_profile_end": (ctypes.c_int, []),
     "loract_profile_count": (ctypes.c_int, []),

@@ -7,6 +7,7 @@ library.  Names match the C entry points.  No step of the method runs in Python.
 from __future__ import annotations
 
 import ctypes
+import operator
 import struct
 from typing import Dict, Optional, Sequence, Tuple
 
@@ -332,6 +333,7 @@ def loract_prenorm_backward(a: torch.Tensor, rms: torch.Tensor, gamma: torch.Ten
 _LINEAR_PARAMS = struct.Struct("9q5ifdQ")
 _QK_PARAMS = struct.Struct("q6iqf4x12q")
 _SEED = 2 ** 64 - 1
+_DTYPE_OF = operator.attrgetter("dtype")
 _WORKSPACE_TOO_SMALL = -2
 
 
@@ -586,6 +588,100 @@ def loract_qknorm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], gamm
                                                _ptr(dk_out), dq.data_ptr(), _ptr(dk), _ptr(dgq), dgk_ptr),
              lib.loract_qknorm_rope_workspace_bytes if dgq is not None or dgk_ptr else None, params, q.get_device(), "loract_qknorm_rope_backward")
     return dq, dk, dgq, dgk
+
+
+ADAMW_BLOCK = 256
+_ADAMW_PARAMS = struct.Struct("5dqQ3i4x")
+
+
+class AdamwState:
+    """The moments of a list of tensors, for loract_adamw: one flat tensor each, every tensor's part padded to a multiple of ADAMW_BLOCK.
+
+    bits = 32: `m` and `v` are float32 and `exps` is None.  bits = 8: `m` and `v` are float8_e4m3fn and stand for m and sqrt(v) in units of
+    2^(exps - 127), `exps` (blocks x 2, uint8) one for each block of ADAMW_BLOCK elements and moment.  All are plain tensors, to be saved and
+    copied into as such."""
+
+    def __init__(self, sizes: Sequence[int], bits: int, device: torch.device):
+        if bits not in (8, 32):
+            raise ValueError("states are held in 32 or 8 bits")
+        self.sizes, self.bits = list(sizes), bits
+        padded = sum(-(-n // ADAMW_BLOCK) * ADAMW_BLOCK for n in self.sizes)
+        dtype = torch.float32 if bits == 32 else torch.uint8
+        self.m, self.v = (torch.zeros(padded, dtype=dtype, device=device) for _ in range(2))
+        self.exps = None
+        if bits == 8:
+            self.m, self.v = self.m.view(torch.float8_e4m3fn), self.v.view(torch.float8_e4m3fn)
+            self.exps = torch.zeros((padded // ADAMW_BLOCK, 2), dtype=torch.uint8, device=device)
+
+
+def loract_adamw_state(params: Sequence[torch.Tensor], bits: int = 32) -> AdamwState:
+    """The state before the first step (zeros) of loract_adamw on these tensors, in their order."""
+    params = list(params)
+    if not params:
+        raise ValueError("no tensors")
+    _require_cuda(*params)
+    return AdamwState([p.numel() for p in params], bits, params[0].device)
+
+
+def _tensor_list(ts: Sequence[torch.Tensor], sizes: list, dtype: torch.dtype, device: int, what: str) -> bytes:
+    """The addresses of contiguous tensors of those sizes and that type on that GPU, as an array."""
+    T = torch.Tensor
+    if len(ts) != len(sizes) or list(map(T.numel, ts)) != sizes:
+        raise ValueError("%s must be the state's %d tensors, with its sizes" % (what, len(sizes)))
+    if set(map(_DTYPE_OF, ts)) != {dtype} or set(map(T.get_device, ts)) != {device} or device < 0 or not all(map(T.is_contiguous, ts)):
+        raise ValueError("%s must be contiguous tensors of %s on one GPU with the others" % (what, dtype))
+    return struct.pack("%dQ" % len(ts), *map(T.data_ptr, ts))
+
+
+def _scalar(v, dtype: torch.dtype, device: int, what: str):
+    """(number, address): one of a number and a tensor of one element."""
+    if not isinstance(v, torch.Tensor):
+        return v, None
+    if v.numel() != 1 or v.dtype is not dtype or v.get_device() != device:
+        raise ValueError("%s must be a number or one %s on one GPU with the others" % (what, dtype))
+    return 0, v.data_ptr()
+
+
+def loract_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], state: AdamwState, *, step, lr, betas: Tuple[float, float] = (0.9, 0.999),
+                 eps: float = 1e-8, weight_decay: float = 0.01, seed: int = 0, grad_scale: Optional[torch.Tensor] = None,
+                 copies: Optional[Sequence[torch.Tensor]] = None) -> None:
+    """One step of AdamW on all of `params` (float32 or bfloat16, in place) and `state`.
+
+    `grads` are float32 or bfloat16.  `copies` of float32 parameters get them rounded to bfloat16.  step (from 1 on) and lr are numbers, or
+    tensors of one element (int64, float32) that are read when the step runs, as `grad_scale` (float32, multiplies the gradients) always is:
+    a captured step takes what changes from replay to replay from these.  What is held in fewer than 32 bits is rounded at random by
+    (seed, step), so that small changes are kept on average."""
+    params, grads = list(params), list(grads)
+    if not params or not grads:
+        raise ValueError("no tensors")
+    sizes, dev, dt, gdt = state.sizes, params[0].get_device(), params[0].dtype, grads[0].dtype
+    p_ptr = _tensor_list(params, sizes, dt, dev, "params")
+    g_ptr = _tensor_list(grads, sizes, gdt, dev, "grads")
+    c_ptr = None
+    if copies is not None:
+        if dt is not torch.float32:
+            raise ValueError("only float32 parameters have copies")
+        c_ptr = _tensor_list(list(copies), sizes, torch.bfloat16, dev, "copies")
+    padded = sum((n + ADAMW_BLOCK - 1) // ADAMW_BLOCK for n in sizes) * ADAMW_BLOCK
+    held = torch.float32 if state.bits == 32 else torch.float8_e4m3fn
+    for t in (state.m, state.v):
+        if t.shape != (padded,) or t.dtype is not held or not t.is_contiguous() or t.get_device() != dev:
+            raise ValueError("the state's moments must be contiguous tensors of %d %s on one GPU with the parameters" % (padded, held))
+    if state.bits == 8 and (state.exps.shape != (padded // ADAMW_BLOCK, 2) or state.exps.dtype is not torch.uint8 or not state.exps.is_contiguous() or
+                            state.exps.get_device() != dev):
+        raise ValueError("the state's exponents must be a contiguous blocks x 2 uint8 tensor on one GPU with the parameters")
+    lr, lr_ptr = _scalar(lr, torch.float32, dev, "lr")
+    step, step_ptr = _scalar(step, torch.int64, dev, "step")
+    scale_ptr = None
+    if grad_scale is not None:
+        if not isinstance(grad_scale, torch.Tensor):
+            raise ValueError("grad_scale must be a tensor")
+        scale_ptr = _scalar(grad_scale, torch.float32, dev, "grad_scale")[1]
+    args = _ADAMW_PARAMS.pack(lr, betas[0], betas[1], eps, weight_decay, step, seed & _SEED, _dtype_code(dt), _dtype_code(gdt), state.bits)
+    code = _lib.load().loract_adamw(p_ptr, g_ptr, c_ptr, struct.pack("%dq" % len(sizes), *sizes), len(sizes), args, state.m.data_ptr(),
+                                    state.v.data_ptr(), _ptr(state.exps), lr_ptr, step_ptr, scale_ptr, _stream_on(dev))
+    if code:
+        raise LoractError(code, "loract_adamw")
 
 
 def loract_profile_begin() -> None:

@@ -1,0 +1,221 @@
+// One step of AdamW over many tensors at once, states in float32 or in 8 bits.
+//
+//   m' = b1 m + (1 - b1) g,  v' = b2 v + (1 - b2) g^2,  p' = (1 - lr wd) p - rate (m' / (sqrt(v') inv + eps)),
+//   rate = lr / (1 - b1^t),  inv = 1 / sqrt(1 - b2^t)
+//
+// Every operation is rounded by itself, in this order (no fused multiply-adds): the codes of the 8-bit states are then a function
+// of the definition alone, whoever computes them.
+//
+// States in 8 bits.  Of 256 elements m and r = sqrt(v) are held as e4m3 numbers times a power of two each.  A power of two costs no digit of a
+// floating-point code, only range (17 binades below the largest element), and scaling by it is exact.  The root, not v, because its range is
+// half of v's.  Roundings are random, from a counter: with b2 = 0.999 a step moves v by a thousandth of it at most, which a nearest rounding
+// to three digits would undo for ever; the root stays above zero where it is (a zero root below a moment that is not zero would make a step of m / eps).
+// bf16 parameters are rounded at random for the same reason.
+//
+// Bound by memory: p read and written, g read, the states read and written.
+#pragma once
+#include "common.h"
+
+#include <cmath>
+
+#define ADAMW_CHUNK 2048                             // elements per workgroup: eight per thread, 32 threads to a block of 256
+#define ADAMW_TENSORS 80                             // per launch: the table is a kernel argument (4 KB at most)
+
+struct AdamwTable {
+  void* p[ADAMW_TENSORS];
+  const void* g[ADAMW_TENSORS];
+  bf16_t* copy[ADAMW_TENSORS];
+  int64_t n[ADAMW_TENSORS], first[ADAMW_TENSORS];    // elements; the tensor's place in the state
+  uint32_t chunk[ADAMW_TENSORS + 1];                 // first workgroup of each tensor, and their number
+};
+struct AdamwArgs {
+  int count;
+  void *m, *v;
+  uint8_t* exps;
+  const float *lr_dev, *grad_scale_dev;
+  const int64_t* step_dev;
+  double lr, log2_beta1, log2_beta2, weight_decay;   // (where lr or step are read on the device)
+  float beta1, one_beta1, beta2, one_beta2, eps, decay, rate, inv;
+  uint64_t seed;
+  int64_t step;
+};
+static_assert(sizeof(AdamwTable) + sizeof(AdamwArgs) <= 4096, "the arguments of a launch");
+
+// rate, inv and decay of a step (host and device).
+__host__ __device__ inline void adamw_rates(AdamwArgs& a, double lr, double pow1, double pow2) {
+  a.rate = (float)(lr / (1.0 - pow1));
+  a.inv = (float)(1.0 / sqrt(1.0 - pow2));
+  a.decay = (float)(1.0 - lr * a.weight_decay);
+}
+
+template <typename T>
+struct Adamw8 {
+  typedef T vec __attribute__((ext_vector_type(8)));
+  typedef vec any __attribute__((aligned(sizeof(T))));      // parameters and gradients begin at any element
+};
+template <typename T>
+__device__ inline void adamw_load(const T* at, int64_t left, float (&x)[8]) {
+  if (left >= 8) {
+    const typename Adamw8<T>::vec v = *(const typename Adamw8<T>::any*)at;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = e < left ? (float)at[e] : 0.0f;
+  }
+}
+template <typename T>
+__device__ inline void adamw_store(T* at, int64_t left, const T (&x)[8]) {
+  if (left >= 8) {
+    typename Adamw8<T>::vec v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = x[e];
+    *(typename Adamw8<T>::any*)at = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) at[e] = x[e];
+  }
+}
+
+typedef unsigned adamw_codes __attribute__((ext_vector_type(2)));
+// Eight e4m3 numbers (bytes).
+__device__ inline void adamw_decode(adamw_codes c, float unit, float (&x)[8]) {
+#pragma clang fp contract(off)
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(c[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c[h], true);
+    x[4 * h] = lo[0] * unit;
+    x[4 * h + 1] = lo[1] * unit;
+    x[4 * h + 2] = hi[0] * unit;
+    x[4 * h + 3] = hi[1] * unit;
+  }
+}
+// The byte of a block's exponent from the 32 lanes that hold its elements.
+__device__ inline unsigned adamw_exponent(const float (&x)[8]) {
+  unsigned top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const unsigned b = __float_as_uint(x[e]) & 0x7fffffffu;
+    top = max(top, b < 0x7f800000u ? b : 0u);
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d));
+  return max((top + 0x2aaaabu) >> 23, 8u) - 7u;
+}
+// Rounds x 2^(127 - byte) to e4m3 at random: below 2^-6, where codes are 2^-9 apart, 2^-6 is added, whose binade has that spacing.
+__device__ inline unsigned adamw_code(float x, float scale, unsigned bits, bool above_zero) {
+#pragma clang fp contract(off)
+  const float size = fabsf(x) * scale;
+  const bool small = size < 0x1p-6f;
+  const float y = small ? size + 0x1p-6f : size;
+  unsigned code = ((__float_as_uint(y) + bits * 1024u + 512u) >> 20) - (small ? 968u : 960u);
+  if (above_zero && code == 0 && size > 0.0f) code = 1;
+  if (!(size < __builtin_inff())) code = 0x7f;
+  return x < 0.0f ? code | 0x80u : code;
+}
+// bf16 from float32 at random; infinities stay, and so does what is no number.
+__device__ inline bf16_t adamw_bf16(float x, unsigned bits) {
+  if (x != x) return (bf16_t)x;
+  return __builtin_bit_cast(bf16_t, (unsigned short)((__float_as_uint(x) + bits * 16u + 8u) >> 16));
+}
+
+template <typename P, typename G, bool NARROW>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamwTable t, AdamwArgs a) {
+#pragma clang fp contract(off)
+  int lo = 0, hi = a.count;                          // the tensor whose workgroups this one is among
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (t.chunk[mid] <= blockIdx.x) lo = mid;
+    else hi = mid;
+  }
+  const int64_t at = (int64_t)(blockIdx.x - t.chunk[lo]) * ADAMW_CHUNK + threadIdx.x * 8;
+  const int64_t e0 = t.first[lo] + at, left = t.n[lo] - at;
+  if ((at & ~(int64_t)255) >= t.n[lo]) return;       // (a whole block of 256: the lanes of the others stay together)
+  if (a.lr_dev || a.step_dev) {
+    const double lr = a.lr_dev ? (double)*a.lr_dev : a.lr;
+    if (a.step_dev) a.step = *a.step_dev;
+    adamw_rates(a, lr, exp2((double)a.step * a.log2_beta1), exp2((double)a.step * a.log2_beta2));
+  }
+  P* const pp = (P*)t.p[lo] + at;
+  float p[8], g[8], m[8], v[8], r[8];
+  adamw_load<P>(pp, left, p);
+  adamw_load<G>((const G*)t.g[lo] + at, left, g);
+  if constexpr (NARROW) {
+    const uint8_t* const exps = a.exps + (e0 >> 8) * 2;
+    const adamw_codes cm = *(const adamw_codes*)((const uint8_t*)a.m + e0), cv = *(const adamw_codes*)((const uint8_t*)a.v + e0);
+    adamw_decode(cm, __uint_as_float((unsigned)exps[0] << 23), m);
+    adamw_decode(cv, __uint_as_float((unsigned)exps[1] << 23), v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = v[e] * v[e];
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 x = *(const f32x4*)((const float*)a.m + e0 + 4 * h), y = *(const f32x4*)((const float*)a.v + e0 + 4 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { m[4 * h + e] = x[e]; v[4 * h + e] = y[e]; }
+    }
+  }
+  if (a.grad_scale_dev) {
+    const float scale = *a.grad_scale_dev;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) g[e] = g[e] * scale;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    m[e] = m[e] * a.beta1 + g[e] * a.one_beta1;
+    v[e] = v[e] * a.beta2 + (g[e] * g[e]) * a.one_beta2;
+    r[e] = sqrtf(v[e]);
+    p[e] = p[e] * a.decay - m[e] / (r[e] * a.inv + a.eps) * a.rate;
+  }
+  unsigned bits[8];
+  if (NARROW || sizeof(P) == 2) {
+    const uint64_t start = splitmix64_mix(a.seed + (uint64_t)a.step * SPLITMIX_GOLDEN);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint64_t word = splitmix64_mix(start + ((uint64_t)(e0 >> 1) + w + 1) * SPLITMIX_GOLDEN);
+      bits[2 * w] = (unsigned)word;
+      bits[2 * w + 1] = (unsigned)(word >> 32);
+    }
+  }
+  if constexpr (NARROW) {
+    const unsigned bm = adamw_exponent(m), br = adamw_exponent(r);
+    const float sm = __uint_as_float((254u - bm) << 23), sr = __uint_as_float((254u - br) << 23);
+    adamw_codes cm = {0, 0}, cr = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      cm[e / 4] |= adamw_code(m[e], sm, bits[e] & 1023u, false) << (8 * (e & 3));
+      cr[e / 4] |= adamw_code(r[e], sr, (bits[e] >> 10) & 1023u, true) << (8 * (e & 3));
+    }
+    *(adamw_codes*)((uint8_t*)a.m + e0) = cm;
+    *(adamw_codes*)((uint8_t*)a.v + e0) = cr;
+    if ((threadIdx.x & 31) == 0) *(uint16_t*)(a.exps + (e0 >> 8) * 2) = (uint16_t)(bm | br << 8);
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      *(f32x4*)((float*)a.m + e0 + 4 * h) = (f32x4){m[4 * h], m[4 * h + 1], m[4 * h + 2], m[4 * h + 3]};
+      *(f32x4*)((float*)a.v + e0 + 4 * h) = (f32x4){v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+    }
+  }
+  P out[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (sizeof(P) == 2) out[e] = adamw_bf16(p[e], bits[e] >> 20);
+    else out[e] = p[e];
+  }
+  adamw_store<P>(pp, left, out);
+  if (sizeof(P) == 4 && t.copy[lo]) {
+    bf16_t c[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = (bf16_t)p[e];
+    adamw_store<bf16_t>(t.copy[lo] + at, left, c);
+  }
+}
+
+template <typename P, typename G>
+static int launch_adamw(hipStream_t s, const AdamwTable& t, const AdamwArgs& a, bool narrow) {
+  const dim3 grid(t.chunk[a.count]), block(256);
+  if (narrow) LORACT_LAUNCH("adamw", s, (adamw_kernel<P, G, true>), grid, block, 0, t, a);
+  else LORACT_LAUNCH("adamw", s, (adamw_kernel<P, G, false>), grid, block, 0, t, a);
+  return LORACT_OK;
+}

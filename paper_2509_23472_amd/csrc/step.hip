@@ -1,0 +1,116 @@
+// libloract: what a fine-tuning step ends with -- the update of its parameters.  See include/loract.h.
+#include "common.h"
+#include "adamw.h"
+#include "overlap.h"
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+// ---------------------------------------------------------------------------------------------
+// AdamW.
+
+struct Span {                                        // bytes that a call writes, or reads
+  uintptr_t lo, hi;
+  bool operator<(const Span& o) const { return lo < o.lo; }
+};
+static int64_t adamw_padded(int64_t n) { return (int64_t)align_up((size_t)n, LORACT_ADAMW_BLOCK); }
+
+// Whether what the step writes (parameters, copies, states) shares memory with itself or with what it reads.  Sorted intervals: a parameter that
+// is in the list twice is found among a thousand tensors too.  -1: no host memory for them.
+static int adamw_meets(void* const* p, const void* const* g, void* const* copy, const int64_t* n, int64_t count, int p_size, int g_size,
+                       const Span (&state)[3], const Span (&scalars)[3]) {
+  Span* const out = new (std::nothrow) Span[(size_t)(2 * count + 3)];
+  if (!out) return -1;
+  size_t k = 0;
+  for (const Span& s : state)
+    if (s.hi > s.lo) out[k++] = s;
+  for (int64_t i = 0; i < count; ++i) {
+    if (n[i] < 1) continue;
+    out[k++] = {(uintptr_t)p[i], (uintptr_t)p[i] + (uintptr_t)n[i] * p_size};
+    if (copy && copy[i]) out[k++] = {(uintptr_t)copy[i], (uintptr_t)copy[i] + (uintptr_t)n[i] * 2};
+  }
+  std::sort(out, out + k);
+  int meets = 0;
+  for (size_t i = 1; i < k; ++i) meets |= out[i].lo < out[i - 1].hi;
+  auto met = [&](Span s) {                            // (the written intervals are apart here: the last one that begins before s ends)
+    const Span* at = std::lower_bound(out, out + k, Span{s.hi, s.hi});
+    return s.hi > s.lo && at != out && (at - 1)->hi > s.lo;
+  };
+  for (int64_t i = 0; i < count && !meets; ++i)
+    if (n[i] > 0) meets = met({(uintptr_t)g[i], (uintptr_t)g[i] + (uintptr_t)n[i] * g_size});
+  for (const Span& s : scalars) meets |= !meets && met(s);
+  delete[] out;
+  return meets;
+}
+
+static bool in_unit(double v) { return v >= 0.0 && v < 1.0; }
+static bool at_least_zero(double v) { return v >= 0.0 && v <= 1.7e308; }
+
+extern "C" {
+
+int loract_adamw(void* const* p, const void* const* g, void* const* copy, const int64_t* n, int64_t count,
+                 const loract_adamw_params* params, void* m_dev, void* v_dev, uint8_t* exps_dev, const float* lr_dev,
+                 const int64_t* step_dev, const float* grad_scale_dev, void* stream) {
+  if (!params || count < 0 || (count && (!p || !g || !n))) return LORACT_ERR_INVALID_ARG;
+  if (!dtype_ok(params->p_dtype) || !dtype_ok(params->g_dtype) || (params->state_bits != 32 && params->state_bits != 8)) return LORACT_ERR_INVALID_ARG;
+  if (!in_unit(params->beta1) || !in_unit(params->beta2) || !at_least_zero(params->eps) || !at_least_zero(params->weight_decay)) return LORACT_ERR_INVALID_ARG;
+  if ((!lr_dev && !at_least_zero(params->lr)) || (!step_dev && params->step < 1)) return LORACT_ERR_INVALID_ARG;
+  if (count > (1 << 24)) return LORACT_ERR_UNSUPPORTED;
+  const bool narrow = params->state_bits == 8, p_bf16 = params->p_dtype == LORACT_BF16, g_bf16 = params->g_dtype == LORACT_BF16;
+  int64_t total = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    if (n[i] < 0 || (n[i] && (!p[i] || !g[i])) || (p_bf16 && copy && copy[i])) return LORACT_ERR_INVALID_ARG;
+    if (n[i] && ((uintptr_t)p[i] % (p_bf16 ? 2 : 4) || (uintptr_t)g[i] % (g_bf16 ? 2 : 4) || (copy && (uintptr_t)copy[i] % 2))) return LORACT_ERR_INVALID_ARG;
+    if (n[i] > (1ll << 33)) return LORACT_ERR_UNSUPPORTED;
+    total += adamw_padded(n[i]);
+  }
+  if (!total) return LORACT_OK;
+  if (!m_dev || !v_dev || (narrow && !exps_dev)) return LORACT_ERR_INVALID_ARG;
+  if ((uintptr_t)m_dev % 16 || (uintptr_t)v_dev % 16 || (narrow && (uintptr_t)exps_dev % 2)) return LORACT_ERR_INVALID_ARG;
+  if ((uintptr_t)lr_dev % 4 || (uintptr_t)step_dev % 8 || (uintptr_t)grad_scale_dev % 4) return LORACT_ERR_INVALID_ARG;
+  const uintptr_t m0 = (uintptr_t)m_dev, v0 = (uintptr_t)v_dev, e0 = (uintptr_t)exps_dev;
+  const uintptr_t state_bytes = (uintptr_t)total * (narrow ? 1 : 4);
+  const Span state[3] = {{m0, m0 + state_bytes}, {v0, v0 + state_bytes}, {e0, narrow ? e0 + (uintptr_t)total / LORACT_ADAMW_BLOCK * 2 : e0}};
+  const Span scalars[3] = {{(uintptr_t)lr_dev, (uintptr_t)lr_dev + (lr_dev ? 4 : 0)}, {(uintptr_t)step_dev, (uintptr_t)step_dev + (step_dev ? 8 : 0)},
+                           {(uintptr_t)grad_scale_dev, (uintptr_t)grad_scale_dev + (grad_scale_dev ? 4 : 0)}};
+  const int meets = adamw_meets(p, g, copy, n, count, p_bf16 ? 2 : 4, g_bf16 ? 2 : 4, state, scalars);
+  if (meets < 0) {
+    g_host.last_hip_error = "no host memory to look the tensors over";
+    return LORACT_ERR_HIP;
+  }
+  if (meets) return LORACT_ERR_INVALID_ARG;
+  AdamwArgs a;
+  a.m = m_dev; a.v = v_dev; a.exps = exps_dev; a.lr_dev = lr_dev; a.step_dev = step_dev; a.grad_scale_dev = grad_scale_dev;
+  a.lr = params->lr; a.log2_beta1 = log2(params->beta1); a.log2_beta2 = log2(params->beta2); a.weight_decay = params->weight_decay;
+  a.beta1 = (float)params->beta1; a.one_beta1 = (float)(1.0 - params->beta1);
+  a.beta2 = (float)params->beta2; a.one_beta2 = (float)(1.0 - params->beta2);
+  a.eps = (float)params->eps; a.seed = params->seed; a.step = params->step; a.rate = a.inv = a.decay = 0.0f;
+  if (!lr_dev && !step_dev) adamw_rates(a, params->lr, pow(params->beta1, (double)params->step), pow(params->beta2, (double)params->step));
+  AdamwTable t;
+  a.count = 0;
+  t.chunk[0] = 0;
+  int64_t first = 0;
+  for (int64_t i = 0; i <= count; ++i) {
+    const int64_t chunks = i < count ? ceil_div64(n[i], ADAMW_CHUNK) : 0;
+    // (fewer than 2^32 threads to a launch)
+    if (a.count && (i == count || a.count == ADAMW_TENSORS || t.chunk[a.count] + chunks >= (1 << 24))) {
+      const hipStream_t s = (hipStream_t)stream;
+      LORACT_TRY(p_bf16 ? (g_bf16 ? launch_adamw<bf16_t, bf16_t>(s, t, a, narrow) : launch_adamw<bf16_t, float>(s, t, a, narrow))
+                        : (g_bf16 ? launch_adamw<float, bf16_t>(s, t, a, narrow) : launch_adamw<float, float>(s, t, a, narrow)));
+      a.count = 0;
+    }
+    if (!chunks) continue;
+    t.p[a.count] = p[i];
+    t.g[a.count] = g[i];
+    t.copy[a.count] = copy ? (bf16_t*)copy[i] : nullptr;
+    t.n[a.count] = n[i];
+    t.first[a.count] = first;
+    t.chunk[a.count + 1] = t.chunk[a.count] + (uint32_t)chunks;
+    ++a.count;
+    first += adamw_padded(n[i]);
+  }
+  return LORACT_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,64 @@
+"""Plain implementations in 64 bits of what a step ends with and of the adapters of many requests."""
+from __future__ import annotations
+
+import numpy as np
+import torch
+
+from sublayer_ref import splitmix64
+
+BLOCK = 256
+
+
+def padded(n):
+    return -(-n // BLOCK) * BLOCK
+
+
+def places(sizes):
+    """Where the elements of the tensors stand in the state."""
+    at, out = 0, []
+    for n in sizes:
+        out.append(np.arange(n) + at)
+        at += padded(n)
+    return np.concatenate(out) if out else np.zeros(0, dtype=np.int64)
+
+
+def halves(seed, step, count):
+    """32 random bits for every element of the state."""
+    start = splitmix64(seed, step)
+    words = [splitmix64(start, i + 1) for i in range(count // 2)]
+    return np.array(words, dtype=np.uint64).view(np.uint32).astype(np.int64)
+
+
+def unit_byte(top):
+    """The byte of the exponent that takes `top` to 320/3 or more and below 640/3."""
+    if not top > 0:
+        return 1
+    power = int(np.floor(np.log2(top * 3 / 320)))
+    while top / 2.0 ** power >= 640 / 3:
+        power += 1
+    while top / 2.0 ** power < 320 / 3:
+        power -= 1
+    return max(power, -126) + 127
+
+
+def rounded(x, bits, count, digits, lowest):
+    """|x| to `digits` digits after the point (2^(lowest - digits) apart below 2^lowest), up where the place between two
+    neighbours plus (bits + 1/2) / 2^count is at least 1."""
+    x = np.abs(np.asarray(x, dtype=np.float64))
+    low = np.maximum(np.frexp(np.maximum(x, 2.0 ** lowest))[1] - 1, lowest).astype(np.float64)
+    gap = np.exp2(low - digits)
+    return np.floor(x / gap + (bits + 0.5) / 2 ** count) * gap
+
+
+def adamw(p, g, m, v, step, lr, betas, eps, decay):
+    """(p, m, v, size of what p's last sum is made of) in 64 bits."""
+    b1, b2 = betas
+    m = b1 * m + (1 - b1) * g
+    v = b2 * v + (1 - b2) * g * g
+    move = lr / (1 - b1 ** step) * m / (np.sqrt(v) / np.sqrt(1 - b2 ** step) + eps)
+    return p * (1 - lr * decay) - move, m, v, np.abs(p) + np.abs(move)
+
+
+def e4m3(codes):
+    """The numbers that bytes stand for."""
+    return torch.from_numpy(np.asarray(codes, dtype=np.uint8)).view(torch.float8_e4m3fn).double().numpy()
