@@ -373,6 +373,51 @@ int loract_adamw(void* const* p, const void* const* g, void* const* copy, const 
                  const loract_adamw_params* params, void* m_dev, void* v_dev, uint8_t* exps_dev, const float* lr_dev,
                  const int64_t* step_dev, const float* grad_scale_dev, void* stream);
 
+#define LORACT_MAX_TOP 64        /* most alternatives of loract_token_logprobs */
+
+typedef struct {
+  int64_t m, n;          /* tokens, size of the vocabulary */
+  int64_t ld, ldg;       /* leading dimensions in elements of the logits and of the gradient (ldg unused without one) */
+  int32_t dtype;         /* loract_dtype of logits and gradient */
+  int32_t target_bits;   /* of the targets: 32 or 64 */
+  int32_t top;           /* alternatives, 0 to LORACT_MAX_TOP and at most n (only loract_token_logprobs reads it) */
+  int32_t reserved;      /* 0 */
+  double temperature;    /* T > 0 */
+} loract_logprob_params;
+
+/*
+ * Log probabilities of given tokens under p = softmax(x / T), rows of an m x n matrix of logits; statistics and sums in float32.
+ * x_dev          m x n (leading dimension ld).   targets_dev: m integers, or NULL.  A negative one is none (padding); one of n or more
+ *                gives NaN.
+ * logp_dev       out, m floats, or NULL: log p of the target, 0 without one.  Without targets_dev it must be NULL.
+ * stats_dev      out, 3 x m floats: the row's maximum of x / T, log of the sum of exp(x / T - maximum), entropy -sum p log p.
+ * top_logp_dev, top_ids_dev    out, m x top floats and int32 (NULL if top is 0): the log probabilities and indices of the largest logits, ties
+ *                in the order of their indices.  What is no number counts as -inf here.
+ * A row of nothing but -inf (a mask that leaves nothing) has the log probabilities -inf, the entropy 0 and the statistics -inf, 0, 0;
+ * one with NaN or +inf has NaN for all of them but, perhaps, the maximum.  m and n up to 2^30.
+ */
+int loract_token_logprobs_workspace_bytes(const loract_logprob_params* p, size_t* bytes);
+int loract_token_logprobs(const void* x_dev, const void* targets_dev, const loract_logprob_params* p, float* logp_dev,
+                          float* stats_dev, float* top_logp_dev, int32_t* top_ids_dev, void* ws_dev, size_t ws_bytes, void* stream);
+
+/*
+ * Its gradient, from the logits and stats_dev as the forward call (of the same x, temperature) left them:
+ *   grad_ij = (1 / T) [ d_logp_i (delta_j,target - p_ij) - d_entropy_i p_ij (log p_ij + H_i) ]
+ * d_logp_dev, d_entropy_dev: m floats each, or NULL (zeros; at least one is given); d_logp of a token without a target does not count, and a row
+ * whose two gradients are zero is zero whatever it holds, as is a row of nothing but -inf.  A target of n or more gives a row of NaN.
+ * grad_dev       out, m x n of dtype (ldg); may be x_dev with the same ld.  No workspace.
+ */
+int loract_token_logprobs_backward(const void* x_dev, const void* targets_dev, const loract_logprob_params* p, const float* stats_dev,
+                                   const float* d_logp_dev, const float* d_entropy_dev, void* grad_dev, void* stream);
+
+/*
+ * Both in one call, where the gradients of the outputs are known before them (a mean over tokens): rows that fit a workgroup's registers
+ * are read once.  grad_dev may be x_dev with the same ld.  Workspace: loract_token_logprobs_workspace_bytes with top = 0.
+ */
+int loract_token_logprobs_grad(const void* x_dev, const void* targets_dev, const loract_logprob_params* p, const float* d_logp_dev,
+                               const float* d_entropy_dev, float* logp_dev, float* stats_dev, void* grad_dev, void* ws_dev, size_t ws_bytes,
+                               void* stream);
+
 /*
  * Per-kernel timing with HIP events on the stream the kernels are launched on.
  * begin: start bracketing every kernel launch of this library with event records.

@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 import operator
 import struct
-from typing import Dict, Optional, Sequence, Tuple
+from typing import Dict, NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -682,6 +682,102 @@ def loract_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], 
                                     state.v.data_ptr(), _ptr(state.exps), lr_ptr, step_ptr, scale_ptr, _stream_on(dev))
     if code:
         raise LoractError(code, "loract_adamw")
+
+
+MAX_TOP = 64
+_LOGPROB_PARAMS = struct.Struct("4q4id")
+_TARGET_BITS = {torch.int32: 32, torch.int64: 64}
+
+
+class TokenLogprobs(NamedTuple):
+    """What loract_token_logprobs gives: `logp` of the targets (None without them), `entropy`, `stats` (3 x m: maximum, log sum, entropy) for the
+    backward pass, and `top_logp`, `top_ids` (m x top, None without any)."""
+    logp: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    stats: torch.Tensor
+    top_logp: Optional[torch.Tensor]
+    top_ids: Optional[torch.Tensor]
+
+
+def _logprob_call(logits, targets, temperature, top, ldg):
+    """(parameters, the targets' address) of a call."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be a matrix")
+    m, n = logits.shape
+    dev = logits.get_device()
+    ld = _rows(logits, m, n, logits.dtype, "logits", dev)
+    bits, t_ptr = 32, None
+    if targets is not None:
+        bits = _TARGET_BITS.get(targets.dtype)
+        if bits is None or targets.shape != (m,) or not targets.is_contiguous() or targets.get_device() != dev:
+            raise ValueError("targets must be a contiguous int32 or int64 tensor with one entry per token and live with the logits")
+        t_ptr = targets.data_ptr()
+    if n < 1:
+        raise ValueError("an empty vocabulary")
+    return _LOGPROB_PARAMS.pack(m, n, ld, ldg, _dtype_code(logits.dtype), bits, top, 0, temperature), t_ptr
+
+
+def loract_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, *, temperature: float = 1.0, top: int = 0) -> TokenLogprobs:
+    """Log probabilities of `targets` (int32 or int64, negative for none) under softmax(logits / temperature), the rows' entropy, and the `top` (at
+    most MAX_TOP) largest logits' log probabilities and indices, ties in the order of their indices.  All float32."""
+    params, t_ptr = _logprob_call(logits, targets, temperature, top, 0)
+    m, dev = logits.shape[0], logits.get_device()
+    logp = None if targets is None else logits.new_empty((m,), dtype=torch.float32)
+    stats = logits.new_empty((3, m), dtype=torch.float32)
+    top_logp, top_ids = (logits.new_empty((m, top), dtype=torch.float32), logits.new_empty((m, top), dtype=torch.int32)) if top > 0 else (None, None)
+    if m:
+        lib = _lib.load()
+        _enqueue(lib.loract_token_logprobs, (logits.data_ptr(), t_ptr, params, _ptr(logp), stats.data_ptr(), _ptr(top_logp), _ptr(top_ids)),
+                 lib.loract_token_logprobs_workspace_bytes, params, dev, "loract_token_logprobs")
+    return TokenLogprobs(logp, stats[2], stats, top_logp, top_ids)
+
+
+def _logprob_grads(logits, targets, d_logp, d_entropy, out):
+    if d_logp is None and d_entropy is None:
+        raise ValueError("a gradient of the log probabilities or of the entropy is needed")
+    if d_logp is not None and targets is None:
+        raise ValueError("d_logp needs targets")
+    if logits.dim() != 2:
+        raise ValueError("logits must be a matrix")
+    m, n = logits.shape
+    dev = logits.get_device()
+    pointers = _floats(d_logp, m, "d_logp", dev), _floats(d_entropy, m, "d_entropy", dev)
+    if out is None:
+        return logits.new_empty((m, n)), n, pointers
+    return out, _rows(out, m, n, logits.dtype, "out", dev), pointers
+
+
+def loract_token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.Tensor], stats: torch.Tensor, d_logp: Optional[torch.Tensor],
+                                   d_entropy: Optional[torch.Tensor] = None, *, temperature: float = 1.0,
+                                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The logits' gradient from those of logp and entropy (m floats each, or None) and the forward call's `stats`.  `out` may be logits."""
+    out, ldg, (lp_ptr, e_ptr) = _logprob_grads(logits, targets, d_logp, d_entropy, out)
+    params, t_ptr = _logprob_call(logits, targets, temperature, 0, ldg)
+    m, dev = logits.shape[0], logits.get_device()
+    if stats.shape != (3, m) or stats.dtype is not torch.float32 or not stats.is_contiguous() or stats.get_device() != dev:
+        raise ValueError("stats must come from loract_token_logprobs")
+    if m:
+        code = _lib.load().loract_token_logprobs_backward(logits.data_ptr(), t_ptr, params, stats.data_ptr(), lp_ptr, e_ptr, out.data_ptr(), _stream_on(dev))
+        if code:
+            raise LoractError(code, "loract_token_logprobs_backward")
+    return out
+
+
+def loract_token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor], d_logp: Optional[torch.Tensor],
+                               d_entropy: Optional[torch.Tensor] = None, *, temperature: float = 1.0, out: Optional[torch.Tensor] = None
+                               ) -> Tuple[Optional[torch.Tensor], torch.Tensor, torch.Tensor]:
+    """(logp, entropy, the logits' gradient) in one call, where the outputs' gradients are known before them: with d_logp = -1 / tokens it is the
+    cross-entropy loss, whose value is the mean of -logp.  `out` may be logits."""
+    out, ldg, (lp_ptr, e_ptr) = _logprob_grads(logits, targets, d_logp, d_entropy, out)
+    params, t_ptr = _logprob_call(logits, targets, temperature, 0, ldg)
+    m, dev = logits.shape[0], logits.get_device()
+    logp = None if targets is None else logits.new_empty((m,), dtype=torch.float32)
+    stats = logits.new_empty((3, m), dtype=torch.float32)
+    if m:
+        lib = _lib.load()
+        _enqueue(lib.loract_token_logprobs_grad, (logits.data_ptr(), t_ptr, params, lp_ptr, e_ptr, _ptr(logp), stats.data_ptr(), out.data_ptr()),
+                 lib.loract_token_logprobs_workspace_bytes, params, dev, "loract_token_logprobs_grad")
+    return logp, stats[2], out
 
 
 def loract_profile_begin() -> None:

@@ -1,0 +1,502 @@
+// Log probabilities of given tokens under logits (tokens x vocabulary), with the entropy and the largest alternatives, and their gradient.
+//
+//   z = x / T,  M = max z,  t_j = z_j - M,  S = sum e^t_j,  W = sum t_j e^t_j
+//   log p_j = t_j - log S,   H = log S - W / S      (no cancellation: log S >= 0, W <= 0)
+//   dx_j = (1 / T) [ g (delta_jt - p_j) - h p_j (log p_j + H) ]
+//
+// S and W are kept beside a running maximum in one pass: a new maximum M' takes S to S e^(M - M'), W to (W + (M - M') S) e^(M - M').
+// t is formed by one fused multiply-add and cut off at -200, where e^t is 0 in float32: an infinite t times 0 never occurs, and NaN stays.
+// The running maximum starts at the lowest finite number, so that a row of nothing but -inf ends with S = 0.
+//
+// The k largest: a workgroup first finds each thread's largest element; the k-th largest of those bounds the k-th largest element from below,
+// and few elements lie above it (k (1 + k / 512) of them in random order).  A second pass over the row, which is in L2, collects these in LDS, where they
+// are ranked by counting.  Elements are ordered by one 64-bit number, the value's order above the index's complement: no two are equal, so ties
+// go to the lowest index and the order of the atomic counter does not show.  Where too many lie above the bound (a row in descending
+// order), they are found one by one.
+//
+// Bound by memory: the logits are read once, the gradient written once.
+#pragma once
+#include "common.h"
+
+#include <algorithm>
+#include <cfloat>
+
+#define LP_THREADS 256
+#define LP_CANDIDATES 1024
+#define LP_SPLITS 64
+
+struct LpArgs {
+  const void* x;
+  int64_t ld, m, n;
+  const void* targets;   // int32 or int64, or null
+  int target_64;
+  float inv_t;
+  float *logp, *stats;   // m; 3 x m: M, log S, H
+  int top;
+  float* top_logp;       // m x top
+  int32_t* top_ids;
+  int64_t chunk;         // columns per workgroup
+  int splits;
+  float* part;           // m x splits x 4: M, S, W
+  uint64_t* part_top;    // m x splits x top
+  const float *d_logp, *d_entropy;
+  void* grad;
+  int64_t ldg;
+};
+
+struct LpSum {
+  float m, s, w;
+};
+__device__ inline LpSum lp_none() { return {-FLT_MAX, 0.0f, 0.0f}; }
+__device__ inline float lp_cut(float t) { return t < -200.0f ? -200.0f : t; }
+// e^t to a few units of the last place (REFINED), or to |t| 2^-23 of it.
+template <bool REFINED>
+__device__ inline float lp_exp(float t) {
+  const float u = t * 1.44269502f, e = __builtin_amdgcn_exp2f(u);
+  if (!REFINED) return e;
+  return fmaf(e, 0.693147181f * fmaf(t, 1.92596299e-8f, fmaf(t, 1.44269502f, -u)), e);
+}
+// (Each operation is rounded by itself: a fused one would take its two sides differently, and the lanes of a butterfly would differ.)
+__device__ inline LpSum lp_moved(const LpSum& a, float m) {
+#pragma clang fp contract(off)
+  const float d = lp_cut(a.m - m), f = lp_exp<true>(d);
+  return {m, a.s * f, (a.w + d * a.s) * f};
+}
+__device__ inline LpSum lp_merge(const LpSum& a, const LpSum& b) {
+#pragma clang fp contract(off)
+  const float m = fmaxf(a.m, b.m);
+  const LpSum x = lp_moved(a, m), y = lp_moved(b, m);
+  return {m, x.s + y.s, x.w + y.w};
+}
+__device__ inline LpSum lp_wave_merge(LpSum a) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    const LpSum b = {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.w, d)};
+    a = lp_merge(a, b);
+  }
+  return a;
+}
+// Log probability of an element of logit x (what is below nothing, a row without a distribution, gives -inf).
+__device__ inline float lp_log(float x, float inv_t, float m, float s, float log_s) {
+  return s == 0.0f ? -__builtin_inff() : fmaf(x, inv_t, -m) - log_s;
+}
+__device__ inline int64_t lp_target(const LpArgs& g, int64_t row) {
+  return g.target_64 ? ((const int64_t*)g.targets)[row] : (int64_t)((const int32_t*)g.targets)[row];
+}
+// What a row ends with, by one thread.
+template <typename T>
+__device__ inline void lp_finish(const LpArgs& g, int64_t row, const LpSum& a, float log_s) {
+  const bool none = a.s == 0.0f;
+  g.stats[row] = none ? -__builtin_inff() : a.m;
+  g.stats[g.m + row] = log_s;
+  g.stats[2 * g.m + row] = none ? 0.0f : log_s - a.w / a.s;
+  if (!g.logp) return;
+  const int64_t t = lp_target(g, row);
+  g.logp[row] = t < 0 ? 0.0f : (t >= g.n ? __builtin_nanf("") : lp_log((float)((const T*)g.x)[row * g.ld + t], g.inv_t, a.m, a.s, log_s));
+}
+__device__ inline float lp_log_sum(float s) { return s == 0.0f ? 0.0f : logf(s); }
+
+// Order of elements: larger values first, then lower indices; what is no number counts as -inf, and both zeros as one.
+__device__ inline uint64_t lp_key(float x, int64_t col) {
+  const unsigned b = x != x ? 0xff800000u : __float_as_uint(x + 0.0f);
+  return (uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (uint32_t)~(uint32_t)col;
+}
+__device__ inline float lp_value(uint64_t key) {
+  const unsigned b = (unsigned)(key >> 32);
+  return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
+}
+__device__ inline int32_t lp_index(uint64_t key) { return (int32_t)~(uint32_t)key; }
+
+template <typename T>
+struct LpPiece {
+  static constexpr int E = 16 / sizeof(T);
+  typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
+  typedef vec any __attribute__((aligned(sizeof(T))));
+};
+// Elements of a run before the first whole piece.
+template <typename T>
+__device__ inline int64_t lp_head(const T* at, int64_t n) {
+  const int64_t head = (int64_t)((16 - ((uintptr_t)at & 15)) & 15) / (int64_t)sizeof(T);
+  return head < n ? head : n;
+}
+// Calls f(values, column, how many) for the elements [c0, c1) of a row: whole pieces, then for thread i < 2 E one of the few around them.
+template <typename T, int U, typename F>
+__device__ inline void lp_each(const T* row, int64_t c0, int64_t c1, F f) {
+  constexpr int E = LpPiece<T>::E;
+  const int64_t head = lp_head(row + c0, c1 - c0), first = c0 + head, pieces = (c1 - first) / E;
+  for (int64_t v = threadIdx.x; v < pieces; v += LP_THREADS * U) {
+    typename LpPiece<T>::vec raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = v + u * LP_THREADS;
+      raw[u] = *(const typename LpPiece<T>::vec*)(row + first + (at < pieces ? at : v) * E);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float x[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = (float)raw[u][e];
+      if (v + u * LP_THREADS < pieces) f(x, first + (v + u * LP_THREADS) * E, E);
+    }
+  }
+  const int64_t tail = c1 - first - pieces * E, i = threadIdx.x;
+  const int64_t col = i < head ? c0 + i : (i >= E && i < E + tail ? first + pieces * E + i - E : -1);
+  if (col < 0) return;
+  float x[E];
+  x[0] = (float)row[col];
+#pragma unroll
+  for (int e = 1; e < E; ++e) x[e] = -__builtin_inff();
+  f(x, col, 1);
+}
+
+// Ranks the `count` candidates in LDS (all different, count at most LP_CANDIDATES): rank r < k goes to out(r, key).
+template <typename F>
+__device__ inline void lp_rank(const uint64_t* cand, int count, int k, F out) {
+  for (int i = threadIdx.x; i < count; i += LP_THREADS) {
+    const uint64_t mine = cand[i];
+    int above = 0;
+    for (int j = 0; j < count; ++j) above += cand[j] > mine;
+    if (above < k) out(above, mine);
+  }
+}
+
+template <typename T, bool TOP>
+__global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LpArgs g) {
+  constexpr int E = LpPiece<T>::E, WAVES = LP_THREADS / 64;
+  __shared__ LpSum sums[WAVES];
+  __shared__ uint64_t best_of[TOP ? LP_THREADS : 1], cand[TOP ? LP_CANDIDATES : 1], bound;
+  __shared__ int found;
+  const int tid = threadIdx.x, split = blockIdx.y;
+  const int64_t c0 = split * g.chunk, c1 = c0 + g.chunk < g.n ? c0 + g.chunk : g.n;
+  for (int64_t row = blockIdx.x; row < g.m; row += gridDim.x) {
+    const T* const x = (const T*)g.x + row * g.ld;
+    LpSum a = lp_none();
+    float best = -__builtin_inff();
+    int64_t best_col = -1;
+    lp_each<T, 4>(x, c0, c1, [&](const float (&v)[E], int64_t col, int count) {
+      float top = v[0];
+#pragma unroll
+      for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
+      const float z = top * g.inv_t;
+      if (z > a.m) a = lp_moved(a, z);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (e >= count) break;
+        const float t = lp_cut(fmaf(v[e], g.inv_t, -a.m)), p = lp_exp<sizeof(T) == 4>(t);
+        a.s += p;
+        a.w = fmaf(t, p, a.w);
+      }
+      if (TOP && (best_col < 0 || top > best)) {
+        best = top > best ? top : best;
+        int at = 0;
+#pragma unroll
+        for (int e = E - 1; e >= 0; --e)
+          if (v[e] == best) at = e;
+        best_col = col + (best == -__builtin_inff() ? 0 : at);
+      }
+    });
+    a = lp_wave_merge(a);
+    if ((tid & 63) == 0) sums[tid >> 6] = a;
+    if (TOP) best_of[tid] = best_col < 0 ? 0 : lp_key(best, best_col);
+    if (TOP && tid == 0) { bound = 0; found = 0; }
+    __syncthreads();
+    a = sums[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) a = lp_merge(a, sums[w]);
+    const float log_s = lp_log_sum(a.s);
+    if (tid == 0) {
+      if (g.splits == 1) lp_finish<T>(g, row, a, log_s);
+      else *(f32x4*)(g.part + (row * g.splits + split) * 4) = (f32x4){a.m, a.s, a.w, 0.0f};
+    }
+    if constexpr (TOP) {
+      const uint64_t mine = best_of[tid];
+      int above = 0;
+      for (int i = 0; i < LP_THREADS; ++i) above += best_of[i] > mine;
+      if (above == g.top - 1 && mine) bound = mine;        // (all different but for threads without elements)
+      __syncthreads();
+      const uint64_t least = bound;
+      const float least_value = least ? lp_value(least) : -__builtin_inff();
+      lp_each<T, 4>(x, c0, c1, [&](const float (&v)[E], int64_t col, int count) {
+        float top = v[0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
+        if (top < least_value) return;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          if (e >= count) break;
+          const uint64_t key = lp_key(v[e], col + e);
+          if (key >= least) {
+            const int at = atomicAdd(&found, 1);
+            if (at < LP_CANDIDATES) cand[at] = key;
+          }
+        }
+      });
+      __syncthreads();
+      const int count = found;
+      auto put = [&](int r, uint64_t key) {
+        if (g.splits > 1) {
+          g.part_top[(row * g.splits + split) * g.top + r] = key;
+        } else {
+          g.top_ids[row * g.top + r] = lp_index(key);
+          g.top_logp[row * g.top + r] = lp_log(lp_value(key), g.inv_t, a.m, a.s, log_s);
+        }
+      };
+      if (count <= LP_CANDIDATES) {
+        lp_rank(cand, count, g.top, put);
+        if (g.splits > 1)
+          for (int r = count + tid; r < g.top; r += LP_THREADS) put(r, 0);
+      } else {                                       // one by one, each below the one before
+        uint64_t last = ~0ull;
+        for (int r = 0; r < g.top; ++r) {
+          uint64_t next = 0;
+          lp_each<T, 4>(x, c0, c1, [&](const float (&v)[E], int64_t col, int cnt) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              if (e >= cnt) break;
+              const uint64_t key = lp_key(v[e], col + e);
+              if (key < last && key > next) next = key;
+            }
+          });
+#pragma unroll
+          for (int d = 32; d; d >>= 1) {
+            const uint64_t other = __shfl_xor((unsigned long long)next, d);
+            next = other > next ? other : next;
+          }
+          __syncthreads();
+          if ((tid & 63) == 0) best_of[tid >> 6] = next;
+          __syncthreads();
+          last = best_of[0];
+#pragma unroll
+          for (int w = 1; w < WAVES; ++w) last = best_of[w] > last ? best_of[w] : last;
+          if (tid == 0) put(r, last);
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the parts of split rows: their sums in a fixed tree, and the rank of every candidate by a search in each part's sorted list.
+template <typename T>
+__global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LpArgs g) {
+  extern __shared__ uint64_t lists[];                // splits x top
+  const int tid = threadIdx.x, lane = tid & 63;
+  for (int64_t row = blockIdx.x; row < g.m; row += gridDim.x) {
+    LpSum a = lp_none();
+    if (lane < g.splits) {
+      const f32x4 p = *(const f32x4*)(g.part + (row * g.splits + lane) * 4);
+      a = {p[0], p[1], p[2]};
+    }
+    a = lp_wave_merge(a);
+    const float log_s = lp_log_sum(a.s);
+    if (tid == 0) lp_finish<T>(g, row, a, log_s);
+    if (g.top) {
+      const int total = g.splits * g.top;
+      for (int i = tid; i < total; i += LP_THREADS) lists[i] = g.part_top[row * total + i];
+      __syncthreads();
+      for (int i = tid; i < total; i += LP_THREADS) {
+        const uint64_t key = lists[i];
+        int above = i % g.top;
+        for (int s = 0; s < g.splits && above < g.top; ++s) {
+          if (s == i / g.top) continue;
+          int lo = 0, hi = g.top;                    // how many of list s are larger
+          while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (lists[s * g.top + mid] > key) lo = mid + 1;
+            else hi = mid;
+          }
+          above += lo;
+        }
+        if (key && above < g.top) {
+          g.top_ids[row * g.top + above] = lp_index(key);
+          g.top_logp[row * g.top + above] = lp_log(lp_value(key), g.inv_t, a.m, a.s, log_s);
+        }
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// What the gradient of a row needs.
+struct LpRow {
+  float m, inv_s, log_s, h, g, d;        // M, 1 / S, log S, H; gradients of log p (0 without a target) and of H, over T
+  int64_t target;
+  bool zero, bad;
+};
+__device__ inline LpRow lp_row(const LpArgs& g, int64_t row) {
+  LpRow r;
+  r.target = g.targets ? lp_target(g, row) : -1;
+  r.bad = r.target >= g.n;
+  r.g = r.target >= 0 && g.d_logp ? g.d_logp[row] * g.inv_t : 0.0f;
+  r.d = g.d_entropy ? g.d_entropy[row] * g.inv_t : 0.0f;
+  r.zero = r.g == 0.0f && r.d == 0.0f && !r.bad;
+  return r;
+}
+template <bool REFINED>
+__device__ inline float lp_slope(const LpRow& r, float inv_t, float x, int64_t col) {
+  const float t = lp_cut(fmaf(x, inv_t, -r.m)), p = lp_exp<REFINED>(t) * r.inv_s;
+  const float out = -p * (r.g + r.d * (t - r.log_s + r.h));
+  return (col == r.target ? r.g : 0.0f) + out;
+}
+
+// Gradient from the statistics: a chunk of a row per workgroup.
+template <typename T>
+__global__ __launch_bounds__(LP_THREADS) void logprob_backward_kernel(LpArgs g) {
+  constexpr int E = LpPiece<T>::E;
+  const int64_t c0 = blockIdx.y * g.chunk, c1 = c0 + g.chunk < g.n ? c0 + g.chunk : g.n;
+  for (int64_t row = blockIdx.x; row < g.m; row += gridDim.x) {
+    LpRow r = lp_row(g, row);
+    r.m = g.stats[row];
+    r.log_s = g.stats[g.m + row];
+    r.h = g.stats[2 * g.m + row];
+    r.inv_s = lp_exp<true>(-r.log_s);
+    if (r.m == -__builtin_inff()) r.zero = !r.bad;
+    const T* const x = (const T*)g.x + row * g.ld;
+    T* const y = (T*)g.grad + row * g.ldg;
+    auto slope = [&](float v, int64_t col) { return r.zero ? 0.0f : (r.bad ? __builtin_nanf("") : lp_slope<sizeof(T) == 4>(r, g.inv_t, v, col)); };
+    lp_each<T, 4>(x, c0, c1, [&](const float (&v)[E], int64_t col, int count) {
+      if (count == 1) {
+        y[col] = (T)slope(v[0], col);
+        return;
+      }
+      typename LpPiece<T>::vec out;
+#pragma unroll
+      for (int e = 0; e < E; ++e) out[e] = (T)slope(v[e], col + e);
+      *(typename LpPiece<T>::any*)(y + col) = out;
+    });
+  }
+}
+
+// Both in one call: a row stays in the registers of a workgroup between the sums and the gradient.  V pieces per thread.
+template <typename T, int THREADS, int V>
+__global__ __launch_bounds__(THREADS) void logprob_grad_kernel(LpArgs g) {
+  constexpr int E = LpPiece<T>::E, WAVES = THREADS / 64;
+  constexpr bool REFINED = sizeof(T) == 4;
+  __shared__ float tops[WAVES];
+  __shared__ float sums[2][WAVES];
+  const int tid = threadIdx.x;
+  for (int64_t row = blockIdx.x; row < g.m; row += gridDim.x) {
+    const T* const x = (const T*)g.x + row * g.ld;
+    const int64_t head = lp_head(x, g.n);
+    const int pieces = (int)((g.n - head) / E), tail = (int)(g.n - head - (int64_t)pieces * E);
+    typename LpPiece<T>::vec raw[V];
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+      const int at = tid + u * THREADS;
+      if (at < pieces) raw[u] = *(const typename LpPiece<T>::vec*)(x + head + (int64_t)at * E);
+    }
+    const int64_t lone = tid < head ? tid : (tid >= E && tid < E + tail ? head + (int64_t)pieces * E + tid - E : -1);
+    const float alone = lone >= 0 ? (float)x[lone] : -__builtin_inff();
+    float top = alone;
+#pragma unroll
+    for (int u = 0; u < V; ++u)
+      if (tid + u * THREADS < pieces) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) top = fmaxf(top, (float)raw[u][e]);
+      }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if ((tid & 63) == 0) tops[tid >> 6] = top;
+    __syncthreads();
+    top = tops[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, tops[w]);
+    LpSum a = {fmaxf(top * g.inv_t, -FLT_MAX), 0.0f, 0.0f};
+    auto add = [&](float v) {
+      const float t = lp_cut(fmaf(v, g.inv_t, -a.m)), p = lp_exp<REFINED>(t);
+      a.s += p;
+      a.w = fmaf(t, p, a.w);
+    };
+    if (lone >= 0) add(alone);
+#pragma unroll
+    for (int u = 0; u < V; ++u)
+      if (tid + u * THREADS < pieces) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) add((float)raw[u][e]);
+      }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+      a.s += __shfl_xor(a.s, d);
+      a.w += __shfl_xor(a.w, d);
+    }
+    if ((tid & 63) == 0) { sums[0][tid >> 6] = a.s; sums[1][tid >> 6] = a.w; }
+    __syncthreads();
+    a.s = sums[0][0];
+    a.w = sums[1][0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) { a.s += sums[0][w]; a.w += sums[1][w]; }
+    const float log_s = lp_log_sum(a.s);
+    LpRow r = lp_row(g, row);
+    r.m = a.m;
+    r.log_s = log_s;
+    r.inv_s = 1.0f / a.s;
+    r.h = log_s - a.w / a.s;
+    if (a.s == 0.0f) r.zero = !r.bad;
+    if (tid == 0) lp_finish<T>(g, row, a, log_s);
+    __syncthreads();                                 // (the target's logit is read before the gradient may take its place)
+    T* const y = (T*)g.grad + row * g.ldg;
+    auto slope = [&](float v, int64_t col) { return r.zero ? 0.0f : (r.bad ? __builtin_nanf("") : lp_slope<REFINED>(r, g.inv_t, v, col)); };
+    if (lone >= 0) y[lone] = (T)slope(alone, lone);
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+      const int at = tid + u * THREADS;
+      if (at < pieces) {
+        const int64_t col = head + (int64_t)at * E;
+        typename LpPiece<T>::vec out;
+#pragma unroll
+        for (int e = 0; e < E; ++e) out[e] = (T)slope((float)raw[u][e], col + e);
+        *(typename LpPiece<T>::any*)(y + col) = out;
+      }
+    }
+  }
+}
+
+// Splits of a row between workgroups: as many as make 512 of them, of at least 4096 columns.
+static int lp_splits(int64_t m, int64_t n) {
+  const int64_t want = std::max<int64_t>(1, 512 / m);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, n / 4096), LP_SPLITS));
+}
+static int64_t lp_chunk(int64_t n, int splits) { return (int64_t)align_up((size_t)ceil_div64(n, splits), 64); }
+static size_t lp_part_bytes(int64_t m, int64_t n, int top) {
+  const int s = lp_splits(m, n);
+  return s > 1 ? (size_t)m * s * (16 + 8 * (size_t)top) : 0;
+}
+// Pieces that a workgroup of the one-call kernel can hold in registers; rows of more, and few rows, take two passes.
+static bool lp_held(int64_t m, int64_t n, bool bf16) { return lp_splits(m, n) == 1 && n / (bf16 ? 8 : 4) <= 16 * 1024; }
+
+template <typename T>
+static int launch_logprobs(hipStream_t s, LpArgs g) {
+  g.splits = lp_splits(g.m, g.n);
+  g.chunk = lp_chunk(g.n, g.splits);
+  g.splits = (int)ceil_div64(g.n, g.chunk);
+  const dim3 grid((unsigned)std::min<int64_t>(g.m, 1 << 20), (unsigned)g.splits), block(LP_THREADS);
+  if (g.top) LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, true>), grid, block, 0, g);
+  else LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, false>), grid, block, 0, g);
+  if (g.splits > 1)
+    LORACT_LAUNCH("token_logprobs_join", s, logprob_join_kernel<T>, dim3(grid.x), block, (unsigned)(g.splits * g.top * 8), g);
+  return LORACT_OK;
+}
+template <typename T>
+static int launch_logprobs_backward(hipStream_t s, LpArgs g) {
+  const int64_t rows = std::min<int64_t>(g.m, 1 << 16);
+  g.chunk = std::max<int64_t>(LP_THREADS * 4 * LpPiece<T>::E, lp_chunk(g.n, 64));
+  LORACT_LAUNCH("token_logprobs_backward", s, logprob_backward_kernel<T>, dim3((unsigned)rows, (unsigned)ceil_div64(g.n, g.chunk)), dim3(LP_THREADS), 0, g);
+  return LORACT_OK;
+}
+template <typename T>
+static int launch_logprobs_grad(hipStream_t s, LpArgs g) {
+  if (!lp_held(g.m, g.n, sizeof(T) == 2)) {
+    LORACT_TRY(launch_logprobs<T>(s, g));
+    return launch_logprobs_backward<T>(s, g);
+  }
+  const int64_t pieces = g.n / LpPiece<T>::E;
+  const dim3 grid((unsigned)std::min<int64_t>(g.m, 1 << 20));
+#define LP_GRAD(THREADS, V) LORACT_LAUNCH("token_logprobs_grad", s, (logprob_grad_kernel<T, THREADS, V>), grid, dim3(THREADS), 0, g)
+  if (pieces <= 256 * 2) LP_GRAD(256, 2);
+  else if (pieces <= 256 * 8) LP_GRAD(256, 8);
+  else if (pieces <= 1024 * 4) LP_GRAD(1024, 4);
+  else if (pieces <= 1024 * 8) LP_GRAD(1024, 8);
+  else LP_GRAD(1024, 16);
+#undef LP_GRAD
+  return LORACT_OK;
+}

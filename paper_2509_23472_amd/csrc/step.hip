@@ -1,10 +1,12 @@
-// libloract: what a fine-tuning step ends with -- the update of its parameters.  See include/loract.h.
+// libloract: what a fine-tuning step ends with -- the loss and its gradient, the update of its parameters.  See include/loract.h.
 #include "common.h"
 #include "adamw.h"
+#include "logprobs.h"
 #include "overlap.h"
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <new>
 
 // ---------------------------------------------------------------------------------------------
@@ -111,6 +113,109 @@ int loract_adamw(void* const* p, const void* const* g, void* const* copy, const 
     first += adamw_padded(n[i]);
   }
   return LORACT_OK;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------------------------
+// Log probabilities.
+
+static int check_logprobs(const loract_logprob_params* p, bool top) {
+  if (!p || p->m < 1 || p->n < 1 || p->ld < p->n || !dtype_ok(p->dtype) || (p->target_bits != 32 && p->target_bits != 64)) return LORACT_ERR_INVALID_ARG;
+  if (!(p->temperature > 0.0) || !std::isfinite((float)p->temperature) || !std::isfinite((float)(1.0 / p->temperature)) || p->reserved) return LORACT_ERR_INVALID_ARG;
+  if (top && (p->top < 0 || p->top > p->n)) return LORACT_ERR_INVALID_ARG;
+  if (p->m > (1 << 30) || p->n > (1 << 30) || (top && p->top > LORACT_MAX_TOP)) return LORACT_ERR_UNSUPPORTED;
+  return LORACT_OK;
+}
+struct LpOperands {
+  Extent x, targets, d_logp, d_entropy, logp, stats, top_logp, top_ids, grad, ws;
+};
+// Whether what is written shares memory with what is read or written beside it, but the gradient in place of the logits.
+static bool logprobs_meet(const LpOperands& o) {
+  const Extent out[] = {o.logp, o.stats, o.top_logp, o.top_ids, o.ws, o.grad};
+  for (int i = 0; i < 6; ++i) {
+    for (int j = i + 1; j < 6; ++j)
+      if (extents_meet(out[i], out[j])) return true;
+    for (const Extent& e : {o.targets, o.d_logp, o.d_entropy})
+      if (extents_meet(out[i], e)) return true;
+    if (i < 5 ? extents_meet(out[i], o.x) : meets_but_in_place(out[i], o.x)) return true;
+  }
+  return false;
+}
+static LpArgs logprob_args(const void* x, const void* targets, const loract_logprob_params* p) {
+  LpArgs g{};
+  g.x = x; g.ld = p->ld; g.m = p->m; g.n = p->n; g.targets = targets; g.target_64 = p->target_bits == 64;
+  g.inv_t = (float)(1.0 / p->temperature); g.splits = 1;
+  return g;
+}
+static bool at_multiple(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
+static bool logprobs_aligned(const void* x, const void* targets, const loract_logprob_params* p, std::initializer_list<const void*> words) {
+  for (const void* w : words)
+    if (!at_multiple(w, 4)) return false;
+  return at_multiple(x, p->dtype == LORACT_BF16 ? 2 : 4) && at_multiple(targets, p->target_bits / 8);
+}
+
+extern "C" {
+
+int loract_token_logprobs_workspace_bytes(const loract_logprob_params* p, size_t* bytes) {
+  if (!bytes) return LORACT_ERR_INVALID_ARG;
+  LORACT_TRY(check_logprobs(p, true));
+  *bytes = align_up(lp_part_bytes(p->m, p->n, p->top), 256);
+  return LORACT_OK;
+}
+
+int loract_token_logprobs(const void* x_dev, const void* targets_dev, const loract_logprob_params* p, float* logp_dev,
+                          float* stats_dev, float* top_logp_dev, int32_t* top_ids_dev, void* ws_dev, size_t ws_bytes, void* stream) {
+  LORACT_TRY(check_logprobs(p, true));
+  if (!x_dev || !stats_dev || (logp_dev && !targets_dev) || (p->top && (!top_logp_dev || !top_ids_dev))) return LORACT_ERR_INVALID_ARG;
+  if (!logprobs_aligned(x_dev, targets_dev, p, {logp_dev, stats_dev, p->top ? top_logp_dev : nullptr, p->top ? top_ids_dev : nullptr})) return LORACT_ERR_INVALID_ARG;
+  const size_t need = lp_part_bytes(p->m, p->n, p->top);
+  if (need && (!ws_dev || ws_bytes < need)) return LORACT_ERR_WORKSPACE_TOO_SMALL;
+  if (need && !at_multiple(ws_dev, 16)) return LORACT_ERR_INVALID_ARG;
+  const int64_t size = p->dtype == LORACT_BF16 ? 2 : 4;
+  const LpOperands o = {extent_rows(x_dev, p->m, p->ld, p->n, size), extent_bytes(targets_dev, p->m * p->target_bits / 8), {}, {},
+                        extent_bytes(logp_dev, p->m * 4), extent_bytes(stats_dev, p->m * 12), extent_bytes(p->top ? top_logp_dev : nullptr, p->m * p->top * 4),
+                        extent_bytes(p->top ? top_ids_dev : nullptr, p->m * p->top * 4), {}, extent_bytes(need ? ws_dev : nullptr, need)};
+  if (logprobs_meet(o)) return LORACT_ERR_INVALID_ARG;
+  LpArgs g = logprob_args(x_dev, targets_dev, p);
+  g.logp = logp_dev; g.stats = stats_dev; g.top = p->top; g.top_logp = top_logp_dev; g.top_ids = top_ids_dev;
+  g.part = (float*)ws_dev;
+  g.part_top = need ? (uint64_t*)((char*)ws_dev + (size_t)p->m * lp_splits(p->m, p->n) * 16) : nullptr;
+  return size == 2 ? launch_logprobs<bf16_t>((hipStream_t)stream, g) : launch_logprobs<float>((hipStream_t)stream, g);
+}
+
+int loract_token_logprobs_backward(const void* x_dev, const void* targets_dev, const loract_logprob_params* p, const float* stats_dev,
+                                   const float* d_logp_dev, const float* d_entropy_dev, void* grad_dev, void* stream) {
+  LORACT_TRY(check_logprobs(p, false));
+  if (!x_dev || !stats_dev || !grad_dev || p->ldg < p->n || (!d_logp_dev && !d_entropy_dev) || (d_logp_dev && !targets_dev)) return LORACT_ERR_INVALID_ARG;
+  const int64_t size = p->dtype == LORACT_BF16 ? 2 : 4;
+  if (!logprobs_aligned(x_dev, targets_dev, p, {stats_dev, d_logp_dev, d_entropy_dev}) || !at_multiple(grad_dev, size)) return LORACT_ERR_INVALID_ARG;
+  LpOperands o = {extent_rows(x_dev, p->m, p->ld, p->n, size), extent_bytes(targets_dev, p->m * p->target_bits / 8), extent_bytes(d_logp_dev, p->m * 4),
+                  extent_bytes(d_entropy_dev, p->m * 4), {}, {}, {}, {}, extent_rows(grad_dev, p->m, p->ldg, p->n, size), {}};
+  if (logprobs_meet(o) || extents_meet(o.grad, extent_bytes(stats_dev, p->m * 12))) return LORACT_ERR_INVALID_ARG;
+  LpArgs g = logprob_args(x_dev, targets_dev, p);
+  g.stats = (float*)stats_dev; g.d_logp = d_logp_dev; g.d_entropy = d_entropy_dev; g.grad = grad_dev; g.ldg = p->ldg;
+  return size == 2 ? launch_logprobs_backward<bf16_t>((hipStream_t)stream, g) : launch_logprobs_backward<float>((hipStream_t)stream, g);
+}
+
+int loract_token_logprobs_grad(const void* x_dev, const void* targets_dev, const loract_logprob_params* p, const float* d_logp_dev,
+                               const float* d_entropy_dev, float* logp_dev, float* stats_dev, void* grad_dev, void* ws_dev, size_t ws_bytes,
+                               void* stream) {
+  LORACT_TRY(check_logprobs(p, false));
+  if (!x_dev || !stats_dev || !grad_dev || p->ldg < p->n || (!d_logp_dev && !d_entropy_dev)) return LORACT_ERR_INVALID_ARG;
+  if ((d_logp_dev || logp_dev) && !targets_dev) return LORACT_ERR_INVALID_ARG;
+  const int64_t size = p->dtype == LORACT_BF16 ? 2 : 4;
+  if (!logprobs_aligned(x_dev, targets_dev, p, {logp_dev, stats_dev, d_logp_dev, d_entropy_dev}) || !at_multiple(grad_dev, size)) return LORACT_ERR_INVALID_ARG;
+  const size_t need = lp_part_bytes(p->m, p->n, 0);
+  if (need && (!ws_dev || ws_bytes < need)) return LORACT_ERR_WORKSPACE_TOO_SMALL;
+  if (need && !at_multiple(ws_dev, 16)) return LORACT_ERR_INVALID_ARG;
+  const LpOperands o = {extent_rows(x_dev, p->m, p->ld, p->n, size), extent_bytes(targets_dev, p->m * p->target_bits / 8), extent_bytes(d_logp_dev, p->m * 4),
+                        extent_bytes(d_entropy_dev, p->m * 4), extent_bytes(logp_dev, p->m * 4), extent_bytes(stats_dev, p->m * 12), {}, {},
+                        extent_rows(grad_dev, p->m, p->ldg, p->n, size), extent_bytes(need ? ws_dev : nullptr, need)};
+  if (logprobs_meet(o)) return LORACT_ERR_INVALID_ARG;
+  LpArgs g = logprob_args(x_dev, targets_dev, p);
+  g.logp = logp_dev; g.stats = stats_dev; g.d_logp = d_logp_dev; g.d_entropy = d_entropy_dev; g.grad = grad_dev; g.ldg = p->ldg; g.part = (float*)ws_dev;
+  return size == 2 ? launch_logprobs_grad<bf16_t>((hipStream_t)stream, g) : launch_logprobs_grad<float>((hipStream_t)stream, g);
 }
 
 }  // extern "C"

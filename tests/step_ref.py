@@ -62,3 +62,47 @@ def adamw(p, g, m, v, step, lr, betas, eps, decay):
 def e4m3(codes):
     """The numbers that bytes stand for."""
     return torch.from_numpy(np.asarray(codes, dtype=np.uint8)).view(torch.float8_e4m3fn).double().numpy()
+
+
+# ---------------------------------------------------------------------------------------------
+# Log probabilities (torch, 64 bits, on the device of the logits).
+
+def logprobs(x, targets, temperature=1.0):
+    """(log p of all, entropy, logp of the targets); rows of nothing but -inf: -inf, 0, -inf."""
+    z = x.double() / temperature
+    top = z.max(1, keepdim=True)[0]
+    none = top[:, 0] == -float("inf")
+    low = z - torch.where(none[:, None], torch.zeros_like(top), top)
+    log_p = low - torch.where(none[:, None], torch.zeros_like(top), low.exp().sum(1, keepdim=True).log())
+    p = torch.where(none[:, None], torch.zeros_like(low), log_p.exp())
+    entropy = -torch.where(p > 0, p * log_p, torch.zeros_like(p)).sum(1)
+    if targets is None:
+        return log_p, p, entropy, None
+    at = targets.long().clamp(0, x.shape[1] - 1)
+    logp = log_p.gather(1, at[:, None])[:, 0]
+    logp = torch.where(targets < 0, torch.zeros_like(logp), logp)
+    return log_p, p, entropy, torch.where(targets >= x.shape[1], torch.full_like(logp, float("nan")), logp)
+
+
+def logprobs_grad(x, targets, d_logp, d_entropy, temperature=1.0):
+    log_p, p, entropy, _ = logprobs(x, targets, temperature)
+    grad, size = torch.zeros_like(p), torch.zeros_like(p)
+    none = x.max(1)[0] == -float("inf")
+    if d_logp is not None:
+        g = torch.where((targets < 0) | none, torch.zeros_like(d_logp), d_logp).double()[:, None]
+        hit = (torch.arange(x.shape[1], device=x.device) == targets[:, None]).double()
+        grad += g * (hit - p)
+        size += g.abs() * (hit + p)
+    if d_entropy is not None:
+        d = d_entropy.double()[:, None]
+        grad -= torch.where(p > 0, d * p * (log_p + entropy[:, None]), torch.zeros_like(p))
+        size += torch.where(p > 0, d.abs() * p * (log_p.abs() + entropy[:, None]), torch.zeros_like(p))
+    if targets is not None:
+        grad[targets >= x.shape[1]] = float("nan")
+    return grad / temperature, size / temperature
+
+
+def top(x, k):
+    """Indices of the k largest, ties in the order of their indices; what is no number counts as -inf."""
+    v = torch.where(x != x, torch.full_like(x, -float("inf")), x).float().cpu()
+    return torch.sort(v, dim=1, descending=True, stable=True)[1][:, :k].int().to(x.device)
