@@ -418,6 +418,33 @@ int loract_token_logprobs_grad(const void* x_dev, const void* targets_dev, const
                                const float* d_entropy_dev, float* logp_dev, float* stats_dev, void* grad_dev, void* ws_dev, size_t ws_bytes,
                                void* stream);
 
+typedef struct {
+  int64_t m;             /* tokens */
+  int64_t n_in, n_out;   /* sizes of the shared projection */
+  int64_t adapters;
+  int64_t ldx, ldr, ldy; /* leading dimensions in elements: X, R, Y */
+  int32_t dtype;         /* loract_dtype of X, A and B */
+  int32_t out_dtype;     /* of R and Y; float32 inputs require float32 */
+  int32_t r;             /* rank of all adapters, 1 to LORACT_MAX_LORA_RANK (smaller ones have columns of A or rows of B that are zero) */
+  int32_t reserved;      /* 0 */
+} loract_requests_params;
+
+/*
+ * The adapters of many requests beside a projection that they share (serving):
+ *   Y_i = R_i + scale_a (X_i A_a) B_a   with a = ids_i
+ * X_dev      m x n_in.   A_dev adapters x n_in x r and B_dev adapters x r x n_out, contiguous: each pair as in loract_linear's low-rank term.
+ * ids_dev    m int32: the token's adapter, in any order (neighbours that share one cost least); a negative one is none, Y_i = R_i; one that
+ *            is not there (adapters or more) gives a row of NaN.
+ * scales_dev adapters floats, or NULL (ones).   R_dev m x n_out, or NULL (zeros).
+ * Y_dev      out, m x n_out; may be R with the same ld: then rows without an adapter are left as they are.
+ * Sums are float32, X A is not rounded to less than 16 bits between the products.  What an adapter or a token holds reaches the tokens with that
+ * adapter and that token alone, be it infinite.  adapters, n_in up to 2^30; m up to 2^27, n_out up to 2^24, and less together where a launch could not
+ * hold them (LORACT_ERR_UNSUPPORTED, from the workspace query too).
+ */
+int loract_lora_requests_workspace_bytes(const loract_requests_params* p, size_t* bytes);
+int loract_lora_requests(const void* X_dev, const void* A_dev, const void* B_dev, const int32_t* ids_dev, const float* scales_dev,
+                         const void* R_dev, const loract_requests_params* p, void* Y_dev, void* ws_dev, size_t ws_bytes, void* stream);
+
 /*
  * Per-kernel timing with HIP events on the stream the kernels are launched on.
  * begin: start bracketing every kernel launch of this library with event records.

@@ -52,6 +52,12 @@ class LoractLogprobParams(ctypes.Structure):
                [(f, ctypes.c_int32) for f in ("dtype", "target_bits", "top", "reserved")] + [("temperature", ctypes.c_double)]
 
 
+class LoractRequestsParams(ctypes.Structure):
+    """Mirror of `loract_requests_params` in include/loract.h (api.py packs the same bytes)."""
+    _fields_ = [(f, ctypes.c_int64) for f in ("m", "n_in", "n_out", "adapters", "ldx", "ldr", "ldy")] + \
+               [(f, ctypes.c_int32) for f in ("dtype", "out_dtype", "r", "reserved")]
+
+
 _P = ctypes.POINTER
 _vp, _i32, _i64, _u64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
 
@@ -93,6 +99,8 @@ SIGNATURES = {
     "loract_token_logprobs": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "loract_token_logprobs_backward": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "loract_token_logprobs_grad": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "loract_lora_requests_workspace_bytes": (ctypes.c_int, [_vp, _P(_sz)]),
+    "loract_lora_requests": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "loract_profile_begin": (ctypes.c_int, []),
     "loract_profile_end": (ctypes.c_int, []),
     "loract_profile_count": (ctypes.c_int, []),

@@ -780,6 +780,43 @@ def loract_token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Ten
     return logp, stats[2], out
 
 
+_REQUESTS_PARAMS = struct.Struct("7q4i")
+
+
+def loract_lora_requests(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor, scales: Optional[torch.Tensor] = None, *,
+                         residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                         out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Y_i = residual_i + scales[ids_i] (x_i a[ids_i]) b[ids_i]: the adapters of many requests beside a shared projection, whose result is the residual.
+
+    x m x n_in; a adapters x n_in x r and b adapters x r x n_out, contiguous (adapters of smaller rank padded with zeros); ids m int32 in any order, negative
+    for none; scales float32.  residual and Y are of out_dtype (x's by default); `out` may be residual, whose rows without an adapter then stay."""
+    if x.dim() != 2 or a.dim() != 3 or b.dim() != 3:
+        raise ValueError("x must be a matrix, a and b adapters x n_in x r and adapters x r x n_out")
+    m, n_in = x.shape
+    count, _, r = a.shape
+    n_out = b.shape[2]
+    dt, dev = x.dtype, x.get_device()
+    odt = dt if out_dtype is None else out_dtype
+    ldx = _rows(x, m, n_in, dt, "x", dev)
+    for t, shape, what in ((a, (count, n_in, r), "a"), (b, (count, r, n_out), "b")):
+        if t.shape != shape or t.dtype is not dt or not t.is_contiguous() or t.get_device() != dev:
+            raise ValueError("%s must be a contiguous %d x %d x %d tensor of %s on one GPU with the others" % ((what,) + shape + (dt,)))
+    if ids.shape != (m,) or ids.dtype is not torch.int32 or not ids.is_contiguous() or ids.get_device() != dev:
+        raise ValueError("ids must be a contiguous int32 tensor with one entry per token on one GPU with the others")
+    s_ptr = _floats(scales, count, "scales", dev)
+    ldr, r_ptr = (0, None) if residual is None else (_rows(residual, m, n_out, odt, "residual", dev), residual.data_ptr())
+    if out is None:
+        out, ldy = x.new_empty((m, n_out), dtype=odt), n_out
+    else:
+        ldy = _rows(out, m, n_out, odt, "out", dev)
+    if m:
+        params = _REQUESTS_PARAMS.pack(m, n_in, n_out, count, ldx, ldr, ldy, _dtype_code(dt), _dtype_code(odt), r, 0)
+        lib = _lib.load()
+        _enqueue(lib.loract_lora_requests, (x.data_ptr(), a.data_ptr(), b.data_ptr(), ids.data_ptr(), s_ptr, r_ptr, params, out.data_ptr()),
+                 lib.loract_lora_requests_workspace_bytes, params, dev, "loract_lora_requests")
+    return out
+
+
 def loract_profile_begin() -> None:
     _check(_lib.load().loract_profile_begin(), "loract_profile_begin")
 

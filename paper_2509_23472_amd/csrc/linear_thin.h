@@ -12,22 +12,11 @@
 // 8192 -> 8192 74 (99), 12096 x 9920 -> 30 142 (161; 170 with twice the steps in flight, at half the waves).
 // Accumulators start with the low-rank term (the first waves, one step of its rank each), scaled in float32.
 #pragma once
+#include "frag.h"
 #include "linear_large.h"
 
 #define LN_WAVES 8
 
-template <typename T>
-struct Ln {
-  static constexpr int E = 16 / sizeof(T), STEP = 4 * E;     // k per lane and per step
-  typedef T frag __attribute__((ext_vector_type(E)));
-  typedef frag frag_any __attribute__((aligned(sizeof(T))));
-};
-__device__ inline f32x4 ln_mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ inline f32x4 ln_mfma(f32x4 a, f32x4 b, f32x4 c) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
-  return c;
-}
 // A lane's k of a row, zero past the end of K (of at least 8).  Rows along K may start at any multiple of 4 bytes.
 template <typename T>
 __device__ inline typename Ln<T>::frag ln_load(const T* row, int64_t k, int64_t k_len) {

@@ -1,7 +1,9 @@
-// libloract: what a fine-tuning step ends with -- the loss and its gradient, the update of its parameters.  See include/loract.h.
+// libloract: what a fine-tuning step ends with -- the loss and its gradient, the update of its parameters -- and
+// the adapters of many requests that it serves.  See include/loract.h.
 #include "common.h"
 #include "adamw.h"
 #include "logprobs.h"
+#include "lora_requests.h"
 #include "overlap.h"
 
 #include <algorithm>
@@ -216,6 +218,61 @@ int loract_token_logprobs_grad(const void* x_dev, const void* targets_dev, const
   LpArgs g = logprob_args(x_dev, targets_dev, p);
   g.logp = logp_dev; g.stats = stats_dev; g.d_logp = d_logp_dev; g.d_entropy = d_entropy_dev; g.grad = grad_dev; g.ldg = p->ldg; g.part = (float*)ws_dev;
   return size == 2 ? launch_logprobs_grad<bf16_t>((hipStream_t)stream, g) : launch_logprobs_grad<float>((hipStream_t)stream, g);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------------------------
+// Adapters of many requests.
+
+static int check_requests(const loract_requests_params* p, LqPlan* plan) {
+  if (!p || p->m < 1 || p->n_in < 1 || p->n_out < 1 || p->adapters < 1 || p->r < 1 || p->reserved) return LORACT_ERR_INVALID_ARG;
+  if (!dtype_ok(p->dtype) || !dtype_ok(p->out_dtype) || p->ldx < p->n_in || p->ldy < p->n_out) return LORACT_ERR_INVALID_ARG;
+  if (p->m > (1 << 27) || p->n_in > (1 << 30) || p->n_out > (1 << 24) || p->adapters > (1 << 30) || p->r > LORACT_MAX_LORA_RANK) return LORACT_ERR_UNSUPPORTED;
+  const bool bf16 = p->dtype == LORACT_BF16;
+  if (!bf16 && p->out_dtype == LORACT_BF16) return LORACT_ERR_UNSUPPORTED;
+  *plan = lora_requests_plan(p->m, p->n_in, p->n_out, p->r, p->adapters, bf16);
+  return lora_requests_launches(*plan, p->m, p->n_out, bf16) ? LORACT_OK : LORACT_ERR_UNSUPPORTED;
+}
+
+extern "C" {
+
+int loract_lora_requests_workspace_bytes(const loract_requests_params* p, size_t* bytes) {
+  LqPlan plan;
+  if (!bytes) return LORACT_ERR_INVALID_ARG;
+  LORACT_TRY(check_requests(p, &plan));
+  *bytes = align_up(lora_requests_part_bytes(plan, p->m), 256);
+  return LORACT_OK;
+}
+
+int loract_lora_requests(const void* X_dev, const void* A_dev, const void* B_dev, const int32_t* ids_dev, const float* scales_dev,
+                         const void* R_dev, const loract_requests_params* p, void* Y_dev, void* ws_dev, size_t ws_bytes, void* stream) {
+  LqPlan plan;
+  LORACT_TRY(check_requests(p, &plan));
+  if (!X_dev || !A_dev || !B_dev || !ids_dev || !Y_dev || (R_dev && p->ldr < p->n_out)) return LORACT_ERR_INVALID_ARG;
+  const int64_t size = p->dtype == LORACT_BF16 ? 2 : 4, y_size = p->out_dtype == LORACT_BF16 ? 2 : 4;
+  for (const void* at : {X_dev, A_dev, B_dev})
+    if (!at_multiple(at, size)) return LORACT_ERR_INVALID_ARG;
+  if (!at_multiple(ids_dev, 4) || !at_multiple(scales_dev, 4) || !at_multiple(R_dev, y_size) || !at_multiple(Y_dev, y_size)) return LORACT_ERR_INVALID_ARG;
+  const size_t need = lora_requests_part_bytes(plan, p->m);
+  if (!ws_dev || ws_bytes < need) return LORACT_ERR_WORKSPACE_TOO_SMALL;
+  if (!at_multiple(ws_dev, 16)) return LORACT_ERR_INVALID_ARG;
+  const Extent y = extent_rows(Y_dev, p->m, p->ldy, p->n_out, y_size), r = extent_rows(R_dev, p->m, p->ldr, p->n_out, y_size), ws = extent_bytes(ws_dev, need);
+  for (const Extent& e : {extent_rows(X_dev, p->m, p->ldx, p->n_in, size), extent_bytes(A_dev, (wide_t)p->adapters * p->n_in * p->r * size),
+                          extent_bytes(B_dev, (wide_t)p->adapters * p->n_out * p->r * size), extent_bytes(ids_dev, p->m * 4),
+                          extent_bytes(scales_dev, p->adapters * 4)})
+    if (extents_meet(y, e) || extents_meet(ws, e)) return LORACT_ERR_INVALID_ARG;
+  if (extents_meet(y, ws) || extents_meet(r, ws) || meets_but_in_place(y, r)) return LORACT_ERR_INVALID_ARG;
+  LqArgs g{};
+  g.X = X_dev; g.ldx = p->ldx; g.A = A_dev; g.B = B_dev; g.ids = ids_dev; g.scales = scales_dev; g.R = R_dev; g.ldr = R_dev ? p->ldr : 0;
+  g.Y = Y_dev; g.ldy = p->ldy; g.m = p->m; g.k = p->n_in; g.n = p->n_out; g.adapters = p->adapters; g.r = p->r; g.part = (float*)ws_dev;
+  const int64_t e = 16 / size;
+  g.a_pieces = p->r % e == 0 && at_multiple(A_dev, 16);
+  g.b_pieces = p->n_out % e == 0 && at_multiple(B_dev, 16);
+  g.in_place = R_dev == Y_dev;
+  const hipStream_t s = (hipStream_t)stream;
+  if (size == 4) return launch_lora_requests<float, float>(s, g, plan);
+  return y_size == 2 ? launch_lora_requests<bf16_t, bf16_t>(s, g, plan) : launch_lora_requests<bf16_t, float>(s, g, plan);
 }
 
 }  // extern "C"

@@ -106,3 +106,25 @@ def top(x, k):
     """Indices of the k largest, ties in the order of their indices; what is no number counts as -inf."""
     v = torch.where(x != x, torch.full_like(x, -float("inf")), x).float().cpu()
     return torch.sort(v, dim=1, descending=True, stable=True)[1][:, :k].int().to(x.device)
+
+
+# ---------------------------------------------------------------------------------------------
+# Adapters of many requests.
+
+def lora_requests(x, a, b, ids, scales, residual):
+    """(Y, bound without the output's rounding) in 64 bits: sums of K products stray by 6 sqrt(K) 2^-24 of their magnitudes, X A enters the second
+    product with 16 bits (of bf16 operands)."""
+    y = torch.zeros(x.shape[0], b.shape[2], dtype=torch.float64, device=x.device) if residual is None else residual.double().clone()
+    off = y.abs() * 2.0 ** -24
+    u, k, r = 2.0 ** -24, x.shape[1], a.shape[2]
+    held = 2.0 ** -16 if x.dtype is torch.bfloat16 else u
+    for i in range(a.shape[0]):
+        rows = (ids == i).nonzero()[:, 0]
+        s = 1.0 if scales is None else float(scales[i])
+        xi, ai, bi = x[rows].double(), a[i].double(), b[i].double()
+        t = xi @ ai
+        y[rows] += s * (t @ bi)
+        off_t = 6 * k ** 0.5 * u * (xi.abs() @ ai.abs()) + (held + 2 * u) * t.abs()
+        off[rows] += abs(s) * (off_t @ bi.abs() + (6 * (2 * r) ** 0.5 + 4) * u * (t.abs() @ bi.abs()))
+    y[ids >= a.shape[0]] = float("nan")
+    return y, off

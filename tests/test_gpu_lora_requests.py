@@ -1,0 +1,181 @@
+"""Adapters of many requests against the formula in 64 bits; the bound is derived beside the reference, and each output is rounded once."""
+import pytest
+import torch
+
+import paper_2509_23472_amd as L
+import step_ref as ref
+from sublayer_ref import U
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+NAN, INF = float("nan"), float("inf")
+
+
+def _make(m, n_in, n_out, r, count, dtype, seed=0, out_dtype=None, pad=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+    x = rand(m, n_in + pad).to(dtype)[:, :n_in]
+    a, b = (rand(count, n_in, r) * n_in ** -0.5).to(dtype), (rand(count, r, n_out) * r ** -0.5).to(dtype)
+    res = rand(m, n_out + pad).to(out_dtype or dtype)[:, :n_out]
+    return x, a, b, 0.5 + torch.rand(count, generator=gen, device="cuda"), res, gen
+
+
+def _ids(kind, m, count, gen):
+    if kind == "single":
+        ids = torch.arange(m, device="cuda") % count
+        return ids[torch.randperm(m, generator=gen, device="cuda")].int()
+    ids = torch.randint(-1, count, (m,), generator=gen, device="cuda")
+    if kind == "runs":
+        cuts = torch.randint(0, m + 1, (6,), generator=gen, device="cuda").sort()[0]
+        ids = torch.randint(-1, count, (7,), generator=gen, device="cuda")[torch.bucketize(torch.arange(m, device="cuda"), cuts, right=True)]
+    return ids.int()
+
+
+def _check(got, x, a, b, ids, scales, res):
+    want, off = ref.lora_requests(x, a, b, ids, scales, res)
+    bad = ~(((got.double() - want).abs() <= off + U[got.dtype] * (want.abs() + off)) | (torch.isnan(got) & torch.isnan(want)))
+    assert not bad.any(), (bad.nonzero()[:4].tolist(), got[bad][:4].tolist(), want[bad][:4].tolist(), off[bad][:4].tolist())
+
+
+SHAPES = [(1, 4096, 11008, 16, 8, "single"), (1, 1, 1, 1, 1, "single"), (2, 7, 5, 3, 2, "single"), (64, 4096, 4096, 16, 64, "single"), (17, 100, 130, 8, 5, "mixed"),
+          (100, 257, 129, 33, 30, "mixed"), (33, 64, 1000, 64, 3, "mixed"), (300, 1030, 770, 12, 5, "runs"), (1000, 512, 640, 48, 16, "runs"), (8200, 264, 136, 64, 7, "runs"),
+          (8200, 255, 1031, 5, 40, "mixed"), (5, 2050, 2048, 32, 100, "single"), (4100, 96, 11008, 17, 3, "runs")]
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF, BF), (F32, F32), (BF, F32)])
+@pytest.mark.parametrize("m,n_in,n_out,r,count,kind", SHAPES)
+def test_against_the_formula(m, n_in, n_out, r, count, kind, dtype, out_dtype):
+    x, a, b, scales, res, gen = _make(m, n_in, n_out, r, count, dtype, m + r, out_dtype)
+    ids = _ids(kind, m, count, gen)
+    _check(L.loract_lora_requests(x, a, b, ids, scales, residual=res, out_dtype=out_dtype), x, a, b, ids, scales, res)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("m,n_in,n_out,r,count,pad", [(50, 130, 72, 16, 4, 3), (50, 136, 72, 16, 4, 8), (300, 129, 71, 7, 9, 1)])
+def test_strides_no_residual_no_scales(m, n_in, n_out, r, count, pad, dtype):
+    x, a, b, scales, res, gen = _make(m, n_in, n_out, r, count, dtype, 3, pad=pad)
+    ids = _ids("mixed", m, count, gen)
+    _check(L.loract_lora_requests(x, a, b, ids), x, a, b, ids, None, None)
+    memory = torch.full((m + 2, n_out + 5), 7.0, dtype=dtype, device="cuda")
+    out = memory[1:m + 1, 2:n_out + 2]
+    L.loract_lora_requests(x, a, b, ids, scales, residual=res, out=out)
+    _check(out, x, a, b, ids, scales, res)
+    outside = torch.ones_like(memory, dtype=torch.bool)
+    outside[1:m + 1, 2:n_out + 2] = False
+    assert (memory[outside] == 7).all()
+
+
+def test_unaligned_operands():
+    for dtype in (BF, F32):
+        x, a, b, scales, res, gen = _make(70, 128, 256, 16, 6, dtype, 4)
+        ids = _ids("mixed", 70, 6, gen)
+
+        def moved(t):
+            flat = torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")[1:]
+            flat.copy_(t.reshape(-1))
+            return flat.view(t.shape)
+        _check(L.loract_lora_requests(moved(x), moved(a), moved(b), ids, scales, residual=moved(res)), x, a, b, ids, scales, res)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("m", [40, 9000])
+def test_in_place_leaves_other_rows(m, dtype):
+    x, a, b, scales, res, gen = _make(m, 96, 264, 16, 4, dtype, 5, pad=8)
+    ids = _ids("mixed", m, 4, gen)
+    ids[:3] = -1
+    ids[-2:] = -2 ** 31
+    res[0] = NAN
+    whole, before = res._base.clone(), res.clone()
+    out = whole[:, :264]
+    L.loract_lora_requests(x, a, b, ids, scales, residual=out, out=out)
+    none = ids < 0
+    assert torch.equal(out[none].view(torch.int16 if dtype is BF else torch.int32), before[none].view(torch.int16 if dtype is BF else torch.int32))
+    assert torch.equal(whole[:, 264:], res._base[:, 264:])
+    _check(out[~none], x[~none], a, b, ids[~none], scales, before[~none])
+
+
+def test_adapters_that_are_not_there():
+    x, a, b, scales, res, gen = _make(50, 64, 72, 8, 3, BF, 6)
+    ids = _ids("mixed", 50, 3, gen)
+    ids[[4, 20, 49]] = torch.tensor([3, 2 ** 31 - 1, 77], dtype=torch.int32, device="cuda")
+    got = L.loract_lora_requests(x, a, b, ids, scales, residual=res)
+    assert torch.isnan(got[[4, 20, 49]]).all()
+    _check(got, x, a, b, ids, scales, res)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_what_is_not_finite_stays_with_its_own(dtype):
+    x, a, b, scales, res, gen = _make(64, 200, 136, 16, 8, dtype, 7)
+    ids = (torch.arange(64, device="cuda") % 8).int()
+    clean = L.loract_lora_requests(x, a, b, ids, scales, residual=res)
+    a[2, 5, 3], b[3, 1, 7], x[9, 0], scales[6], res[12, 4] = NAN, INF, NAN, INF, NAN
+    got = L.loract_lora_requests(x, a, b, ids, scales, residual=res)
+    touched = (ids == 2) | (ids == 3) | (ids == 6)
+    touched[[9, 12]] = True
+    assert torch.equal(got[~touched], clean[~touched])
+    assert torch.isnan(got[ids == 2]).all() and torch.isnan(got[9]).all() and not torch.isfinite(got[ids == 6]).any()
+    row = (ids == 3) & (torch.arange(64, device="cuda") != 9)
+    assert not torch.isfinite(got[row][:, 7]).any() and torch.equal(got[row][:, :7], clean[row][:, :7]) and torch.equal(got[row][:, 8:], clean[row][:, 8:])
+    assert torch.isnan(got[12, 4]) and torch.equal(got[12, :4], clean[12, :4])
+
+
+def test_the_order_of_tokens_does_not_matter_and_equal_calls_give_equal_bits():
+    x, a, b, scales, res, gen = _make(96, 512, 256, 16, 12, BF, 8)
+    ids = _ids("mixed", 96, 12, gen)
+    got = L.loract_lora_requests(x, a, b, ids, scales, residual=res)
+    order = torch.randperm(96, generator=gen, device="cuda")
+    assert torch.equal(L.loract_lora_requests(x[order], a, b, ids[order], scales, residual=res[order]), got[order])
+    assert torch.equal(L.loract_lora_requests(x, a, b, ids, scales, residual=res), got)
+
+
+def test_no_tokens():
+    x, a, b, scales, res, _ = _make(4, 64, 72, 8, 3, BF, 9)
+    assert L.loract_lora_requests(x[:0], a, b, torch.zeros(0, dtype=torch.int32, device="cuda"), scales, residual=res[:0]).shape == (0, 72)
+
+
+def test_captured_calls_beside_eager_ones():
+    x, a, b, scales, res, gen = _make(32, 1024, 512, 16, 10, BF, 10)
+    more = _make(700, 1024, 512, 16, 10, BF, 11)
+    ids, more_ids = _ids("mixed", 32, 10, gen), _ids("runs", 700, 10, gen)
+    L.loract_lora_requests(x, a, b, ids, scales, residual=res)
+    torch.cuda.synchronize()
+    graphs = []
+    for args in ((x, a, b, ids, scales, res), (more[0], a, b, more_ids, scales, more[4])):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = L.loract_lora_requests(*args[:5], residual=args[5])
+        graphs.append((graph, out, args))
+    for _ in range(4):
+        x.copy_(torch.randn(x.shape, generator=gen, device="cuda"))
+        ids.copy_(_ids("mixed", 32, 10, gen))
+        more_ids.copy_(_ids("runs", 700, 10, gen))
+        for graph, _, _ in graphs:
+            graph.replay()
+        want = [L.loract_lora_requests(*args[:5], residual=args[5]) for _, _, args in graphs]
+        torch.cuda.synchronize()
+        assert all(torch.equal(out, w) for (_, out, _), w in zip(graphs, want))
+
+
+def test_another_stream():
+    x, a, b, scales, res, gen = _make(64, 1024, 512, 16, 10, BF, 12)
+    ids = _ids("single", 64, 10, gen)
+    want = L.loract_lora_requests(x, a, b, ids, scales, residual=res)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = L.loract_lora_requests(x, a, b, ids, scales, residual=res)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want)
+
+
+def test_one_adapter_is_the_low_rank_term_of_a_linear_map():
+    """Beside the projection it gives what the projection with its own low-rank term gives, but for the roundings of T, Y and the residual."""
+    x, a, b, scales, res, gen = _make(200, 256, 384, 16, 1, BF, 13)
+    w = (torch.randn(384, 256, generator=gen, device="cuda") / 16).bfloat16()
+    t = L.loract_linear(x, a[0], w_transposed=True)
+    want = L.loract_linear(x, w, lora_t=t, lora_b=b[0], lora_scale=0.75, out_dtype=F32)
+    got = L.loract_linear(x, w, out_dtype=F32)
+    L.loract_lora_requests(x, a, b, torch.zeros(200, dtype=torch.int32, device="cuda"), torch.full((1,), 0.75, device="cuda"), residual=got, out=got, out_dtype=F32)
+    # T rounded to bf16 moves the term by 2^-8 of its products' magnitudes
+    off = 0.75 * 2.0 ** -8 * (t.double().abs() @ b[0].double().abs()) + 1e-4
+    assert ((got.double() - want.double()).abs() <= off).all()
