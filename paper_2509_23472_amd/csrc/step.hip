@@ -241,7 +241,7 @@ int loract_lora_requests_workspace_bytes(const loract_requests_params* p, size_t
   LqPlan plan;
   if (!bytes) return LORACT_ERR_INVALID_ARG;
   LORACT_TRY(check_requests(p, &plan));
-  *bytes = align_up(lora_requests_part_bytes(plan, p->m), 256);
+  *bytes = align_up(plan.bytes, 256);
   return LORACT_OK;
 }
 
@@ -254,7 +254,7 @@ int loract_lora_requests(const void* X_dev, const void* A_dev, const void* B_dev
   for (const void* at : {X_dev, A_dev, B_dev})
     if (!at_multiple(at, size)) return LORACT_ERR_INVALID_ARG;
   if (!at_multiple(ids_dev, 4) || !at_multiple(scales_dev, 4) || !at_multiple(R_dev, y_size) || !at_multiple(Y_dev, y_size)) return LORACT_ERR_INVALID_ARG;
-  const size_t need = lora_requests_part_bytes(plan, p->m);
+  const size_t need = plan.bytes;
   if (!ws_dev || ws_bytes < need) return LORACT_ERR_WORKSPACE_TOO_SMALL;
   if (!at_multiple(ws_dev, 16)) return LORACT_ERR_INVALID_ARG;
   const Extent y = extent_rows(Y_dev, p->m, p->ldy, p->n_out, y_size), r = extent_rows(R_dev, p->m, p->ldr, p->n_out, y_size), ws = extent_bytes(ws_dev, need);
