@@ -390,7 +390,7 @@ typedef struct {
  * x_dev          m x n (leading dimension ld).   targets_dev: m integers, or NULL.  A negative one is none (padding); one of n or more
  *                gives NaN.
  * logp_dev       out, m floats, or NULL: log p of the target, 0 without one.  Without targets_dev it must be NULL.
- * stats_dev      out, 3 x m floats: the row's maximum of x / T, log of the sum of exp(x / T - maximum), entropy -sum p log p.
+ * stats_dev      out, 3 x m floats: the row's maximum M, log2 of the sum of exp((x - M) / T), the entropy -sum p log p.
  * top_logp_dev, top_ids_dev    out, m x top floats and int32 (NULL if top is 0): the log probabilities and indices of the largest logits, ties
  *                in the order of their indices.  What is no number counts as -inf here.
  * A row of nothing but -inf (a mask that leaves nothing) has the log probabilities -inf, the entropy 0 and the statistics -inf, 0, 0;

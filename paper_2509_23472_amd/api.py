@@ -690,8 +690,8 @@ _TARGET_BITS = {torch.int32: 32, torch.int64: 64}
 
 
 class TokenLogprobs(NamedTuple):
-    """What loract_token_logprobs gives: `logp` of the targets (None without them), `entropy`, `stats` (3 x m: maximum, log sum, entropy) for the
-    backward pass, and `top_logp`, `top_ids` (m x top, None without any)."""
+    """What loract_token_logprobs gives: `logp` of the targets (None without them), `entropy`, `stats` (3 x m: maximum, log2 of the sum, entropy)
+    for the backward pass, and `top_logp`, `top_ids` (m x top, None without any)."""
     logp: Optional[torch.Tensor]
     entropy: torch.Tensor
     stats: torch.Tensor

@@ -1,11 +1,14 @@
 // Log probabilities of given tokens under logits (tokens x vocabulary), with the entropy and the largest alternatives, and their gradient.
 //
-//   z = x / T,  M = max z,  t_j = z_j - M,  S = sum e^t_j,  W = sum t_j e^t_j
-//   log p_j = t_j - log S,   H = log S - W / S      (no cancellation: log S >= 0, W <= 0)
+//   c = 1 / (T ln 2),  M = max x,  u_j = (x_j - M) c,  S = sum 2^u_j,  W = sum u_j 2^u_j
+//   log p_j = ln 2 (u_j - log2 S),   H = ln 2 (log2 S - W / S)      (no cancellation: log2 S >= 0, W <= 0)
 //   dx_j = (1 / T) [ g (delta_jt - p_j) - h p_j (log p_j + H) ]
 //
-// S and W are kept beside a running maximum in one pass: a new maximum M' takes S to S e^(M - M'), W to (W + (M - M') S) e^(M - M').
-// t is formed by one fused multiply-add and cut off at -200, where e^t is 0 in float32: an infinite t times 0 never occurs, and NaN stays.
+// Exponents are binary logarithms, so that an element costs a difference, a product and the exponential: a CU has 30 vector operations for each bf16
+// that it reads and writes at the rate of a copy, and an exponential is four of them.  c is rounded once for all elements (a relative error of 2^-25 of
+// the temperature), u twice.  The maximum is one of x itself: a row of the type's lowest value, which x c may not hold, is as good as equal.
+// S and W are kept beside a running maximum in one pass: a new maximum M' takes S to S 2^((M - M') c), W to (W + (M - M') c S) 2^((M - M') c).
+// In W u is cut off at -300, where 2^u is 0: an infinite u times 0 never occurs; NaN stays in S.
 // The running maximum starts at the lowest finite number, so that a row of nothing but -inf ends with S = 0.
 //
 // The k largest: a workgroup first finds each thread's largest element; the k-th largest of those bounds the k-th largest element from below,
@@ -30,8 +33,8 @@ struct LpArgs {
   int64_t ld, m, n;
   const void* targets;   // int32 or int64, or null
   int target_64;
-  float inv_t;
-  float *logp, *stats;   // m; 3 x m: M, log S, H
+  float inv_t, c;        // 1 / T, 1 / (T ln 2)
+  float *logp, *stats;   // m; 3 x m: M, log2 S, H
   int top;
   float* top_logp;       // m x top
   int32_t* top_ids;
@@ -48,38 +51,34 @@ struct LpSum {
   float m, s, w;
 };
 __device__ inline LpSum lp_none() { return {-FLT_MAX, 0.0f, 0.0f}; }
-__device__ inline float lp_cut(float t) { return t < -200.0f ? -200.0f : t; }
-// e^t to a few units of the last place (REFINED), or to |t| 2^-23 of it.
-template <bool REFINED>
-__device__ inline float lp_exp(float t) {
-  const float u = t * 1.44269502f, e = __builtin_amdgcn_exp2f(u);
-  if (!REFINED) return e;
-  return fmaf(e, 0.693147181f * fmaf(t, 1.92596299e-8f, fmaf(t, 1.44269502f, -u)), e);
-}
+#define LP_LN2 0.693147181f
+__device__ inline float lp_cut(float u) { return fmaxf(u, -300.0f); }
 // (Each operation is rounded by itself: a fused one would take its two sides differently, and the lanes of a butterfly would differ.)
-__device__ inline LpSum lp_moved(const LpSum& a, float m) {
+__device__ inline LpSum lp_moved(const LpSum& a, float m, float c) {
 #pragma clang fp contract(off)
-  const float d = lp_cut(a.m - m), f = lp_exp<true>(d);
+  const float d = lp_cut((a.m - m) * c), f = __builtin_amdgcn_exp2f(d);
   return {m, a.s * f, (a.w + d * a.s) * f};
 }
-__device__ inline LpSum lp_merge(const LpSum& a, const LpSum& b) {
+__device__ inline LpSum lp_merge(const LpSum& a, const LpSum& b, float c) {
 #pragma clang fp contract(off)
   const float m = fmaxf(a.m, b.m);
-  const LpSum x = lp_moved(a, m), y = lp_moved(b, m);
+  const LpSum x = lp_moved(a, m, c), y = lp_moved(b, m, c);
   return {m, x.s + y.s, x.w + y.w};
 }
-__device__ inline LpSum lp_wave_merge(LpSum a) {
+__device__ inline LpSum lp_wave_merge(LpSum a, float c) {
 #pragma unroll
   for (int d = 32; d; d >>= 1) {
     const LpSum b = {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.w, d)};
-    a = lp_merge(a, b);
+    a = lp_merge(a, b, c);
   }
   return a;
 }
 // Log probability of an element of logit x (what is below nothing, a row without a distribution, gives -inf).
-__device__ inline float lp_log(float x, float inv_t, float m, float s, float log_s) {
-  return s == 0.0f ? -__builtin_inff() : fmaf(x, inv_t, -m) - log_s;
+__device__ inline float lp_log(const LpArgs& g, float x, const LpSum& a, float log_s) {
+  return a.s == 0.0f ? -__builtin_inff() : ((x - a.m) * g.c - log_s) * LP_LN2;
 }
+__device__ inline float lp_log_sum(float s) { return s == 0.0f ? 0.0f : log2f(s); }
+__device__ inline float lp_entropy(const LpSum& a, float log_s) { return a.s == 0.0f ? 0.0f : (log_s - a.w / a.s) * LP_LN2; }
 __device__ inline int64_t lp_target(const LpArgs& g, int64_t row) {
   return g.target_64 ? ((const int64_t*)g.targets)[row] : (int64_t)((const int32_t*)g.targets)[row];
 }
@@ -89,12 +88,11 @@ __device__ inline void lp_finish(const LpArgs& g, int64_t row, const LpSum& a, f
   const bool none = a.s == 0.0f;
   g.stats[row] = none ? -__builtin_inff() : a.m;
   g.stats[g.m + row] = log_s;
-  g.stats[2 * g.m + row] = none ? 0.0f : log_s - a.w / a.s;
+  g.stats[2 * g.m + row] = lp_entropy(a, log_s);
   if (!g.logp) return;
   const int64_t t = lp_target(g, row);
-  g.logp[row] = t < 0 ? 0.0f : (t >= g.n ? __builtin_nanf("") : lp_log((float)((const T*)g.x)[row * g.ld + t], g.inv_t, a.m, a.s, log_s));
+  g.logp[row] = t < 0 ? 0.0f : (t >= g.n ? __builtin_nanf("") : lp_log(g, (float)((const T*)g.x)[row * g.ld + t], a, log_s));
 }
-__device__ inline float lp_log_sum(float s) { return s == 0.0f ? 0.0f : logf(s); }
 
 // Order of elements: larger values first, then lower indices; what is no number counts as -inf, and both zeros as one.
 __device__ inline uint64_t lp_key(float x, int64_t col) {
@@ -149,12 +147,26 @@ __device__ inline void lp_each(const T* row, int64_t c0, int64_t c1, F f) {
   f(x, col, 1);
 }
 
+// Fills the elements [c0, c1) of a row.
+template <typename T>
+__device__ inline void lp_fill(T* row, int64_t c0, int64_t c1, T value) {
+  constexpr int E = LpPiece<T>::E;
+  const int64_t head = lp_head(row + c0, c1 - c0), first = c0 + head, pieces = (c1 - first) / E, tail = c1 - first - pieces * E;
+  typename LpPiece<T>::vec all;
+#pragma unroll
+  for (int e = 0; e < E; ++e) all[e] = value;
+  for (int64_t v = threadIdx.x; v < pieces; v += LP_THREADS) *(typename LpPiece<T>::vec*)(row + first + v * E) = all;
+  if (threadIdx.x < head) row[c0 + threadIdx.x] = value;
+  if (threadIdx.x < tail) row[first + pieces * E + threadIdx.x] = value;
+}
+
 // Ranks the `count` candidates in LDS (all different, count at most LP_CANDIDATES): rank r < k goes to out(r, key).
 template <typename F>
 __device__ inline void lp_rank(const uint64_t* cand, int count, int k, F out) {
   for (int i = threadIdx.x; i < count; i += LP_THREADS) {
     const uint64_t mine = cand[i];
     int above = 0;
+#pragma unroll 16
     for (int j = 0; j < count; ++j) above += cand[j] > mine;
     if (above < k) out(above, mine);
   }
@@ -177,14 +189,13 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LpArgs g) {
       float top = v[0];
 #pragma unroll
       for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
-      const float z = top * g.inv_t;
-      if (z > a.m) a = lp_moved(a, z);
+      if (top > a.m) a = lp_moved(a, top, g.c);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         if (e >= count) break;
-        const float t = lp_cut(fmaf(v[e], g.inv_t, -a.m)), p = lp_exp<sizeof(T) == 4>(t);
+        const float u = (v[e] - a.m) * g.c, p = __builtin_amdgcn_exp2f(u);
         a.s += p;
-        a.w = fmaf(t, p, a.w);
+        a.w = fmaf(lp_cut(u), p, a.w);
       }
       if (TOP && (best_col < 0 || top > best)) {
         best = top > best ? top : best;
@@ -195,14 +206,14 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LpArgs g) {
         best_col = col + (best == -__builtin_inff() ? 0 : at);
       }
     });
-    a = lp_wave_merge(a);
+    a = lp_wave_merge(a, g.c);
     if ((tid & 63) == 0) sums[tid >> 6] = a;
     if (TOP) best_of[tid] = best_col < 0 ? 0 : lp_key(best, best_col);
     if (TOP && tid == 0) { bound = 0; found = 0; }
     __syncthreads();
     a = sums[0];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) a = lp_merge(a, sums[w]);
+    for (int w = 1; w < WAVES; ++w) a = lp_merge(a, sums[w], g.c);
     const float log_s = lp_log_sum(a.s);
     if (tid == 0) {
       if (g.splits == 1) lp_finish<T>(g, row, a, log_s);
@@ -211,6 +222,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LpArgs g) {
     if constexpr (TOP) {
       const uint64_t mine = best_of[tid];
       int above = 0;
+#pragma unroll 16
       for (int i = 0; i < LP_THREADS; ++i) above += best_of[i] > mine;
       if (above == g.top - 1 && mine) bound = mine;        // (all different but for threads without elements)
       __syncthreads();
@@ -238,7 +250,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LpArgs g) {
           g.part_top[(row * g.splits + split) * g.top + r] = key;
         } else {
           g.top_ids[row * g.top + r] = lp_index(key);
-          g.top_logp[row * g.top + r] = lp_log(lp_value(key), g.inv_t, a.m, a.s, log_s);
+          g.top_logp[row * g.top + r] = lp_log(g, lp_value(key), a, log_s);
         }
       };
       if (count <= LP_CANDIDATES) {
@@ -276,42 +288,47 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LpArgs g) {
   }
 }
 
-// Joins the parts of split rows: their sums in a fixed tree, and the rank of every candidate by a search in each part's sorted list.
+// Joins the parts of split rows: their sums in a fixed tree, and the ranks of the candidates among those that are not below a bound of the k-th
+// largest: the largest of the lists' last entries, or the smallest of their (k / splits)-th ones.
 template <typename T>
 __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LpArgs g) {
-  extern __shared__ uint64_t lists[];                // splits x top
-  const int tid = threadIdx.x, lane = tid & 63;
+  extern __shared__ uint64_t cand[];                 // splits x top
+  __shared__ int found;
+  const int tid = threadIdx.x, lane = tid & 63, total = g.splits * g.top;
   for (int64_t row = blockIdx.x; row < g.m; row += gridDim.x) {
+    const uint64_t* const lists = g.part_top + row * total;
     LpSum a = lp_none();
+    uint64_t last = 0, early = ~0ull;
     if (lane < g.splits) {
       const f32x4 p = *(const f32x4*)(g.part + (row * g.splits + lane) * 4);
+      if (g.top) {
+        last = lists[lane * g.top + g.top - 1];
+        early = lists[lane * g.top + (g.top - 1) / g.splits];
+      }
       a = {p[0], p[1], p[2]};
     }
-    a = lp_wave_merge(a);
+    a = lp_wave_merge(a, g.c);
     const float log_s = lp_log_sum(a.s);
     if (tid == 0) lp_finish<T>(g, row, a, log_s);
     if (g.top) {
-      const int total = g.splits * g.top;
-      for (int i = tid; i < total; i += LP_THREADS) lists[i] = g.part_top[row * total + i];
+#pragma unroll
+      for (int d = 32; d; d >>= 1) {
+        const uint64_t l = __shfl_xor((unsigned long long)last, d), e = __shfl_xor((unsigned long long)early, d);
+        last = l > last ? l : last;
+        early = e < early ? e : early;
+      }
+      const uint64_t least = last > early ? last : early;
+      if (tid == 0) found = 0;
       __syncthreads();
       for (int i = tid; i < total; i += LP_THREADS) {
         const uint64_t key = lists[i];
-        int above = i % g.top;
-        for (int s = 0; s < g.splits && above < g.top; ++s) {
-          if (s == i / g.top) continue;
-          int lo = 0, hi = g.top;                    // how many of list s are larger
-          while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (lists[s * g.top + mid] > key) lo = mid + 1;
-            else hi = mid;
-          }
-          above += lo;
-        }
-        if (key && above < g.top) {
-          g.top_ids[row * g.top + above] = lp_index(key);
-          g.top_logp[row * g.top + above] = lp_log(lp_value(key), g.inv_t, a.m, a.s, log_s);
-        }
+        if (key && key >= least) cand[atomicAdd(&found, 1)] = key;
       }
+      __syncthreads();
+      lp_rank(cand, found, g.top, [&](int r, uint64_t key) {
+        g.top_ids[row * g.top + r] = lp_index(key);
+        g.top_logp[row * g.top + r] = lp_log(g, lp_value(key), a, log_s);
+      });
       __syncthreads();
     }
   }
@@ -319,73 +336,83 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LpArgs g) {
 
 // What the gradient of a row needs.
 struct LpRow {
-  float m, inv_s, log_s, h, g, d;        // M, 1 / S, log S, H; gradients of log p (0 without a target) and of H, over T
+  float m, inv_s;        // M, 1 / S
+  float by, by_u;        // dx_j = 2^u_j (by + by_u u_j) but at the target, which has g more
+  float g;
   int64_t target;
   bool zero, bad;
 };
-__device__ inline LpRow lp_row(const LpArgs& g, int64_t row) {
+__device__ inline LpRow lp_row(const LpArgs& g, int64_t row, float m, float s, float log_s, float entropy) {
   LpRow r;
   r.target = g.targets ? lp_target(g, row) : -1;
   r.bad = r.target >= g.n;
   r.g = r.target >= 0 && g.d_logp ? g.d_logp[row] * g.inv_t : 0.0f;
-  r.d = g.d_entropy ? g.d_entropy[row] * g.inv_t : 0.0f;
-  r.zero = r.g == 0.0f && r.d == 0.0f && !r.bad;
+  const float d = g.d_entropy ? g.d_entropy[row] * g.inv_t : 0.0f, inv_s = 1.0f / s;
+  r.zero = !r.bad && ((r.g == 0.0f && d == 0.0f) || s == 0.0f);
+  r.m = m;
+  r.by_u = -d * LP_LN2 * inv_s;
+  r.by = -(r.g + d * fmaf(-LP_LN2, log_s, entropy)) * inv_s;
   return r;
 }
-template <bool REFINED>
-__device__ inline float lp_slope(const LpRow& r, float inv_t, float x, int64_t col) {
-  const float t = lp_cut(fmaf(x, inv_t, -r.m)), p = lp_exp<REFINED>(t) * r.inv_s;
-  const float out = -p * (r.g + r.d * (t - r.log_s + r.h));
-  return (col == r.target ? r.g : 0.0f) + out;
-}
+template <bool ENTROPY>
+__device__ inline float lp_slope(const LpRow& r, float u, float p) { return ENTROPY ? p * fmaf(r.by_u, lp_cut(u), r.by) : p * r.by; }
 
 // Gradient from the statistics: a chunk of a row per workgroup.
-template <typename T>
+template <typename T, bool ENTROPY>
 __global__ __launch_bounds__(LP_THREADS) void logprob_backward_kernel(LpArgs g) {
   constexpr int E = LpPiece<T>::E;
   const int64_t c0 = blockIdx.y * g.chunk, c1 = c0 + g.chunk < g.n ? c0 + g.chunk : g.n;
   for (int64_t row = blockIdx.x; row < g.m; row += gridDim.x) {
-    LpRow r = lp_row(g, row);
-    r.m = g.stats[row];
-    r.log_s = g.stats[g.m + row];
-    r.h = g.stats[2 * g.m + row];
-    r.inv_s = lp_exp<true>(-r.log_s);
-    if (r.m == -__builtin_inff()) r.zero = !r.bad;
+    const float m = g.stats[row], log_s = g.stats[g.m + row];
+    const LpRow r = lp_row(g, row, m, m == -__builtin_inff() ? 0.0f : exp2f(log_s), log_s, g.stats[2 * g.m + row]);
     const T* const x = (const T*)g.x + row * g.ld;
     T* const y = (T*)g.grad + row * g.ldg;
-    auto slope = [&](float v, int64_t col) { return r.zero ? 0.0f : (r.bad ? __builtin_nanf("") : lp_slope<sizeof(T) == 4>(r, g.inv_t, v, col)); };
+    if (r.zero || r.bad) {
+      const T fill = (T)(r.bad ? __builtin_nanf("") : 0.0f);
+      lp_fill(y, c0, c1, fill);
+      continue;
+    }
     lp_each<T, 4>(x, c0, c1, [&](const float (&v)[E], int64_t col, int count) {
-      if (count == 1) {
-        y[col] = (T)slope(v[0], col);
-        return;
-      }
       typename LpPiece<T>::vec out;
 #pragma unroll
-      for (int e = 0; e < E; ++e) out[e] = (T)slope(v[e], col + e);
-      *(typename LpPiece<T>::any*)(y + col) = out;
+      for (int e = 0; e < E; ++e) {
+        if (e >= count) break;
+        const float u = (v[e] - r.m) * g.c;
+        out[e] = (T)lp_slope<ENTROPY>(r, u, __builtin_amdgcn_exp2f(u));
+      }
+      if (r.target >= col && r.target < col + count) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (col + e == r.target) {
+            const float u = (v[e] - r.m) * g.c;
+            out[e] = (T)(r.g + lp_slope<ENTROPY>(r, u, __builtin_amdgcn_exp2f(u)));
+          }
+      }
+      if (count == E) *(typename LpPiece<T>::any*)(y + col) = out;
+      else y[col] = out[0];
     });
   }
 }
 
-// Both in one call: a row stays in the registers of a workgroup between the sums and the gradient.  V pieces per thread.
-template <typename T, int THREADS, int V>
-__global__ __launch_bounds__(THREADS) void logprob_grad_kernel(LpArgs g) {
+// Both in one call: a row stays in the registers of a workgroup between the sums and the gradient.  V pieces per thread.  The exponentials are formed
+// again for the gradient: kept, they take twice the row's registers, and no second workgroup of the CU could work while one waits for memory.
+template <typename T, int THREADS, int V, bool ENTROPY>
+__global__ __launch_bounds__(THREADS, V < 8 || THREADS * V == 8192 ? 8 : (V == 8 ? 7 : 4)) void logprob_grad_kernel(LpArgs g) {
   constexpr int E = LpPiece<T>::E, WAVES = THREADS / 64;
-  constexpr bool REFINED = sizeof(T) == 4;
   __shared__ float tops[WAVES];
   __shared__ float sums[2][WAVES];
   const int tid = threadIdx.x;
   for (int64_t row = blockIdx.x; row < g.m; row += gridDim.x) {
     const T* const x = (const T*)g.x + row * g.ld;
-    const int64_t head = lp_head(x, g.n);
-    const int pieces = (int)((g.n - head) / E), tail = (int)(g.n - head - (int64_t)pieces * E);
+    const int n = (int)g.n, head = (int)lp_head(x, g.n), pieces = (n - head) / E, tail = n - head - pieces * E;      // (rows in registers are short)
+    const T* const body = x + head;
     typename LpPiece<T>::vec raw[V];
 #pragma unroll
     for (int u = 0; u < V; ++u) {
       const int at = tid + u * THREADS;
-      if (at < pieces) raw[u] = *(const typename LpPiece<T>::vec*)(x + head + (int64_t)at * E);
+      if (at < pieces) raw[u] = *(const typename LpPiece<T>::vec*)(body + (unsigned)at * E);
     }
-    const int64_t lone = tid < head ? tid : (tid >= E && tid < E + tail ? head + (int64_t)pieces * E + tid - E : -1);
+    const int lone = tid < head ? tid : (tid >= E && tid < E + tail ? head + pieces * E + tid - E : -1);
     const float alone = lone >= 0 ? (float)x[lone] : -__builtin_inff();
     float top = alone;
 #pragma unroll
@@ -401,11 +428,11 @@ __global__ __launch_bounds__(THREADS) void logprob_grad_kernel(LpArgs g) {
     top = tops[0];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) top = fmaxf(top, tops[w]);
-    LpSum a = {fmaxf(top * g.inv_t, -FLT_MAX), 0.0f, 0.0f};
+    LpSum a = {fmaxf(top, -FLT_MAX), 0.0f, 0.0f};
     auto add = [&](float v) {
-      const float t = lp_cut(fmaf(v, g.inv_t, -a.m)), p = lp_exp<REFINED>(t);
+      const float u = (v - a.m) * g.c, p = __builtin_amdgcn_exp2f(u);
       a.s += p;
-      a.w = fmaf(t, p, a.w);
+      a.w = fmaf(lp_cut(u), p, a.w);
     };
     if (lone >= 0) add(alone);
 #pragma unroll
@@ -426,34 +453,52 @@ __global__ __launch_bounds__(THREADS) void logprob_grad_kernel(LpArgs g) {
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) { a.s += sums[0][w]; a.w += sums[1][w]; }
     const float log_s = lp_log_sum(a.s);
-    LpRow r = lp_row(g, row);
-    r.m = a.m;
-    r.log_s = log_s;
-    r.inv_s = 1.0f / a.s;
-    r.h = log_s - a.w / a.s;
-    if (a.s == 0.0f) r.zero = !r.bad;
+    const LpRow r = lp_row(g, row, a.m, a.s, log_s, lp_entropy(a, log_s));
     if (tid == 0) lp_finish<T>(g, row, a, log_s);
+    const float asked = r.g != 0.0f && !r.bad && r.target >= 0 ? (float)x[r.target] : 0.0f;
     __syncthreads();                                 // (the target's logit is read before the gradient may take its place)
     T* const y = (T*)g.grad + row * g.ldg;
-    auto slope = [&](float v, int64_t col) { return r.zero ? 0.0f : (r.bad ? __builtin_nanf("") : lp_slope<REFINED>(r, g.inv_t, v, col)); };
-    if (lone >= 0) y[lone] = (T)slope(alone, lone);
+    if (r.zero || r.bad) {
+      const T fill = (T)(r.bad ? __builtin_nanf("") : 0.0f);
+      if (lone >= 0) y[lone] = fill;
+#pragma unroll
+      for (int u = 0; u < V; ++u)
+        if (tid + u * THREADS < pieces) {
+          typename LpPiece<T>::vec out;
+#pragma unroll
+          for (int e = 0; e < E; ++e) out[e] = fill;
+          *(typename LpPiece<T>::any*)(y + head + (unsigned)(tid + u * THREADS) * E) = out;
+        }
+      continue;
+    }
+    const int hit = r.g != 0.0f && r.target >= 0 ? (int)r.target : -1;
+    auto slope = [&](float v) {
+      const float u = (v - r.m) * g.c;
+      return lp_slope<ENTROPY>(r, u, __builtin_amdgcn_exp2f(u));
+    };
+    if (lone >= 0) y[lone] = (T)(slope(alone) + (lone == hit ? r.g : 0.0f));
 #pragma unroll
     for (int u = 0; u < V; ++u) {
       const int at = tid + u * THREADS;
       if (at < pieces) {
-        const int64_t col = head + (int64_t)at * E;
+        const int col = head + at * E;
         typename LpPiece<T>::vec out;
 #pragma unroll
-        for (int e = 0; e < E; ++e) out[e] = (T)slope((float)raw[u][e], col + e);
-        *(typename LpPiece<T>::any*)(y + col) = out;
+        for (int e = 0; e < E; ++e) out[e] = (T)slope((float)raw[u][e]);
+        if (hit >= col && hit < col + E) {
+          const T own = (T)(r.g + slope(asked));
+#pragma unroll
+          for (int e = 0; e < E; ++e) out[e] = col + e == hit ? own : out[e];
+        }
+        *(typename LpPiece<T>::any*)(y + head + (unsigned)at * E) = out;
       }
     }
   }
 }
 
-// Splits of a row between workgroups: as many as make 512 of them, of at least 4096 columns.
+// Splits of a row between workgroups: as many as make 1024 of them, of at least 4096 columns.
 static int lp_splits(int64_t m, int64_t n) {
-  const int64_t want = std::max<int64_t>(1, 512 / m);
+  const int64_t want = std::max<int64_t>(1, 1024 / m);
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, n / 4096), LP_SPLITS));
 }
 static int64_t lp_chunk(int64_t n, int splits) { return (int64_t)align_up((size_t)ceil_div64(n, splits), 64); }
@@ -480,7 +525,9 @@ template <typename T>
 static int launch_logprobs_backward(hipStream_t s, LpArgs g) {
   const int64_t rows = std::min<int64_t>(g.m, 1 << 16);
   g.chunk = std::max<int64_t>(LP_THREADS * 4 * LpPiece<T>::E, lp_chunk(g.n, 64));
-  LORACT_LAUNCH("token_logprobs_backward", s, logprob_backward_kernel<T>, dim3((unsigned)rows, (unsigned)ceil_div64(g.n, g.chunk)), dim3(LP_THREADS), 0, g);
+  const dim3 grid((unsigned)rows, (unsigned)ceil_div64(g.n, g.chunk));
+  if (g.d_entropy) LORACT_LAUNCH("token_logprobs_backward", s, (logprob_backward_kernel<T, true>), grid, dim3(LP_THREADS), 0, g);
+  else LORACT_LAUNCH("token_logprobs_backward", s, (logprob_backward_kernel<T, false>), grid, dim3(LP_THREADS), 0, g);
   return LORACT_OK;
 }
 template <typename T>
@@ -491,10 +538,14 @@ static int launch_logprobs_grad(hipStream_t s, LpArgs g) {
   }
   const int64_t pieces = g.n / LpPiece<T>::E;
   const dim3 grid((unsigned)std::min<int64_t>(g.m, 1 << 20));
-#define LP_GRAD(THREADS, V) LORACT_LAUNCH("token_logprobs_grad", s, (logprob_grad_kernel<T, THREADS, V>), grid, dim3(THREADS), 0, g)
+#define LP_GRAD(THREADS, V)                                                                                                       \
+  do {                                                                                                                             \
+    if (g.d_entropy) LORACT_LAUNCH("token_logprobs_grad", s, (logprob_grad_kernel<T, THREADS, V, true>), grid, dim3(THREADS), 0, g); \
+    else LORACT_LAUNCH("token_logprobs_grad", s, (logprob_grad_kernel<T, THREADS, V, false>), grid, dim3(THREADS), 0, g);          \
+  } while (0)
   if (pieces <= 256 * 2) LP_GRAD(256, 2);
   else if (pieces <= 256 * 8) LP_GRAD(256, 8);
-  else if (pieces <= 1024 * 4) LP_GRAD(1024, 4);
+  else if (pieces <= 512 * 8) LP_GRAD(512, 8);
   else if (pieces <= 1024 * 8) LP_GRAD(1024, 8);
   else LP_GRAD(1024, 16);
 #undef LP_GRAD

@@ -124,7 +124,7 @@ int loract_adamw(void* const* p, const void* const* g, void* const* copy, const 
 
 static int check_logprobs(const loract_logprob_params* p, bool top) {
   if (!p || p->m < 1 || p->n < 1 || p->ld < p->n || !dtype_ok(p->dtype) || (p->target_bits != 32 && p->target_bits != 64)) return LORACT_ERR_INVALID_ARG;
-  if (!(p->temperature > 0.0) || !std::isfinite((float)p->temperature) || !std::isfinite((float)(1.0 / p->temperature)) || p->reserved) return LORACT_ERR_INVALID_ARG;
+  if (!(p->temperature > 0.0) || !std::isfinite((float)p->temperature) || !std::isfinite((float)(1.5 / p->temperature)) || p->reserved) return LORACT_ERR_INVALID_ARG;
   if (top && (p->top < 0 || p->top > p->n)) return LORACT_ERR_INVALID_ARG;
   if (p->m > (1 << 30) || p->n > (1 << 30) || (top && p->top > LORACT_MAX_TOP)) return LORACT_ERR_UNSUPPORTED;
   return LORACT_OK;
@@ -147,7 +147,7 @@ static bool logprobs_meet(const LpOperands& o) {
 static LpArgs logprob_args(const void* x, const void* targets, const loract_logprob_params* p) {
   LpArgs g{};
   g.x = x; g.ld = p->ld; g.m = p->m; g.n = p->n; g.targets = targets; g.target_64 = p->target_bits == 64;
-  g.inv_t = (float)(1.0 / p->temperature); g.splits = 1;
+  g.inv_t = (float)(1.0 / p->temperature); g.c = (float)(1.4426950408889634 / p->temperature); g.splits = 1;
   return g;
 }
 static bool at_multiple(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
