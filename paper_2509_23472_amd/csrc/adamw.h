@@ -103,16 +103,13 @@ __device__ inline unsigned adamw_exponent(const float (&x)[8]) {
   for (int d = 16; d; d >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, d));
   return max((top + 0x2aaaabu) >> 23, 8u) - 7u;
 }
-// Rounds x 2^(127 - byte) to e4m3 at random: below 2^-6, where codes are 2^-9 apart, 2^-6 is added, whose binade has that spacing.
-__device__ inline unsigned adamw_code(float x, float scale, unsigned bits, bool above_zero) {
-#pragma clang fp contract(off)
-  const float size = fabsf(x) * scale;
-  const bool small = size < 0x1p-6f;
-  const float y = small ? size + 0x1p-6f : size;
-  unsigned code = ((__float_as_uint(y) + bits * 1024u + 512u) >> 20) - (small ? 968u : 960u);
-  if (above_zero && code == 0 && size > 0.0f) code = 1;
-  if (!(size < __builtin_inff())) code = 0x7f;
-  return x < 0.0f ? code | 0x80u : code;
+// Rounds x 2^(127 - byte) to e4m3 at random and puts it into byte B of `into`: the conversion adds the upper 20 bits of its seed to the 20 bits that
+// it cuts off (fewer where codes are 2^-9 apart).
+template <int B>
+__device__ inline unsigned adamw_code(float x, float scale, unsigned bits, bool above_zero, unsigned into) {
+  float y = x * scale;
+  if (above_zero) y = x > 0.0f ? fmaxf(y, 0x1p-9f) : y;                // (below 2^-9 it would be 0 or that)
+  return (unsigned)__builtin_amdgcn_cvt_sr_fp8_f32(y, (int)(bits << 22 | 1u << 21), (int)into, B);
 }
 // bf16 from float32 at random; infinities stay, and so does what is no number.
 __device__ inline bf16_t adamw_bf16(float x, unsigned bits) {
@@ -166,14 +163,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwTable t, AdamwArgs a) {
     m[e] = m[e] * a.beta1 + g[e] * a.one_beta1;
     v[e] = v[e] * a.beta2 + (g[e] * g[e]) * a.one_beta2;
     r[e] = sqrtf(v[e]);
-    p[e] = p[e] * a.decay - m[e] / (r[e] * a.inv + a.eps) * a.rate;
+    p[e] = p[e] * a.decay - m[e] * __builtin_amdgcn_rcpf(r[e] * a.inv + a.eps) * a.rate;
   }
   unsigned bits[8];
   if (NARROW || sizeof(P) == 2) {
-    const uint64_t start = splitmix64_mix(a.seed + (uint64_t)a.step * SPLITMIX_GOLDEN);
+    uint64_t at_word = splitmix64_mix(a.seed + (uint64_t)a.step * SPLITMIX_GOLDEN) + (uint64_t)(e0 >> 1) * SPLITMIX_GOLDEN;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const uint64_t word = splitmix64_mix(start + ((uint64_t)(e0 >> 1) + w + 1) * SPLITMIX_GOLDEN);
+      const uint64_t word = splitmix64_mix(at_word += SPLITMIX_GOLDEN);
       bits[2 * w] = (unsigned)word;
       bits[2 * w + 1] = (unsigned)(word >> 32);
     }
@@ -183,9 +180,16 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwTable t, AdamwArgs a) {
     const float sm = __uint_as_float((254u - bm) << 23), sr = __uint_as_float((254u - br) << 23);
     adamw_codes cm = {0, 0}, cr = {0, 0};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      cm[e / 4] |= adamw_code(m[e], sm, bits[e] & 1023u, false) << (8 * (e & 3));
-      cr[e / 4] |= adamw_code(r[e], sr, (bits[e] >> 10) & 1023u, true) << (8 * (e & 3));
+    for (int h = 0; h < 2; ++h) {
+      const unsigned* const b = bits + 4 * h;
+      cm[h] = adamw_code<0>(m[4 * h], sm, b[0], false, cm[h]);
+      cm[h] = adamw_code<1>(m[4 * h + 1], sm, b[1], false, cm[h]);
+      cm[h] = adamw_code<2>(m[4 * h + 2], sm, b[2], false, cm[h]);
+      cm[h] = adamw_code<3>(m[4 * h + 3], sm, b[3], false, cm[h]);
+      cr[h] = adamw_code<0>(r[4 * h], sr, b[0] >> 10, true, cr[h]);
+      cr[h] = adamw_code<1>(r[4 * h + 1], sr, b[1] >> 10, true, cr[h]);
+      cr[h] = adamw_code<2>(r[4 * h + 2], sr, b[2] >> 10, true, cr[h]);
+      cr[h] = adamw_code<3>(r[4 * h + 3], sr, b[3] >> 10, true, cr[h]);
     }
     *(adamw_codes*)((uint8_t*)a.m + e0) = cm;
     *(adamw_codes*)((uint8_t*)a.v + e0) = cr;
