@@ -367,7 +367,7 @@ typedef struct {
  * neighbour where its place between the two plus (bits + 1/2) / 2^10 (2^12) is at least 1.
  * lr_dev, step_dev, grad_scale_dev   a float, an int64 and a float in device memory, read when the step runs, or NULL: p->lr, p->step, 1.  A
  *                  captured step that is replayed takes what changes from these.  A step below 1 there gives NaN or infinities.
- * n up to 2^33 each.  No workspace.
+ * n up to 2^33 each, 2^39 together.  No workspace.
  */
 int loract_adamw(void* const* p, const void* const* g, void* const* copy, const int64_t* n, int64_t count,
                  const loract_adamw_params* params, void* m_dev, void* v_dev, uint8_t* exps_dev, const float* lr_dev,

@@ -19,14 +19,17 @@
 #include <cmath>
 
 #define ADAMW_CHUNK 2048                             // elements per workgroup: eight per thread, 32 threads to a block of 256
-#define ADAMW_TENSORS 80                             // per launch: the table is a kernel argument (4 KB at most)
 
+// The tensors of a launch, a kernel argument (4 KB at most with the rest): 98 of them, 122 without copies.
+template <bool COPY>
 struct AdamwTable {
-  void* p[ADAMW_TENSORS];
-  const void* g[ADAMW_TENSORS];
-  bf16_t* copy[ADAMW_TENSORS];
-  int64_t n[ADAMW_TENSORS], first[ADAMW_TENSORS];    // elements; the tensor's place in the state
-  uint32_t chunk[ADAMW_TENSORS + 1];                 // first workgroup of each tensor, and their number
+  static constexpr int MOST = COPY ? 98 : 122;
+  void* p[MOST];
+  const void* g[MOST];
+  bf16_t* copy[COPY ? MOST : 1];
+  int64_t n[MOST];                                   // elements
+  uint32_t first[MOST];                              // the tensor's place in the state, in blocks of 256
+  uint32_t chunk[MOST + 1];                          // first workgroup of each tensor, and their number
 };
 struct AdamwArgs {
   int count;
@@ -39,7 +42,7 @@ struct AdamwArgs {
   uint64_t seed;
   int64_t step;
 };
-static_assert(sizeof(AdamwTable) + sizeof(AdamwArgs) <= 4096, "the arguments of a launch");
+static_assert(sizeof(AdamwTable<true>) + sizeof(AdamwArgs) <= 4096 && sizeof(AdamwTable<false>) + sizeof(AdamwArgs) <= 4096, "the arguments of a launch");
 
 // rate, inv and decay of a step (host and device).
 __host__ __device__ inline void adamw_rates(AdamwArgs& a, double lr, double pow1, double pow2) {
@@ -117,8 +120,8 @@ __device__ inline bf16_t adamw_bf16(float x, unsigned bits) {
   return __builtin_bit_cast(bf16_t, (unsigned short)((__float_as_uint(x) + bits * 16u + 8u) >> 16));
 }
 
-template <typename P, typename G, bool NARROW>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamwTable t, AdamwArgs a) {
+template <typename P, typename G, bool NARROW, bool COPY>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamwTable<COPY> t, AdamwArgs a) {
 #pragma clang fp contract(off)
   int lo = 0, hi = a.count;                          // the tensor whose workgroups this one is among
   while (hi - lo > 1) {
@@ -127,7 +130,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwTable t, AdamwArgs a) {
     else hi = mid;
   }
   const int64_t at = (int64_t)(blockIdx.x - t.chunk[lo]) * ADAMW_CHUNK + threadIdx.x * 8;
-  const int64_t e0 = t.first[lo] + at, left = t.n[lo] - at;
+  const int64_t e0 = (int64_t)t.first[lo] * LORACT_ADAMW_BLOCK + at, left = t.n[lo] - at;
   if ((at & ~(int64_t)255) >= t.n[lo]) return;       // (a whole block of 256: the lanes of the others stay together)
   if (a.lr_dev || a.step_dev) {
     const double lr = a.lr_dev ? (double)*a.lr_dev : a.lr;
@@ -208,7 +211,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwTable t, AdamwArgs a) {
     else out[e] = p[e];
   }
   adamw_store<P>(pp, left, out);
-  if (sizeof(P) == 4 && t.copy[lo]) {
+  if (COPY && t.copy[lo]) {
     bf16_t c[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) c[e] = (bf16_t)p[e];
@@ -216,10 +219,31 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwTable t, AdamwArgs a) {
   }
 }
 
-template <typename P, typename G>
-static int launch_adamw(hipStream_t s, const AdamwTable& t, const AdamwArgs& a, bool narrow) {
-  const dim3 grid(t.chunk[a.count]), block(256);
-  if (narrow) LORACT_LAUNCH("adamw", s, (adamw_kernel<P, G, true>), grid, block, 0, t, a);
-  else LORACT_LAUNCH("adamw", s, (adamw_kernel<P, G, false>), grid, block, 0, t, a);
+// Launches as many tables as the tensors need.
+template <typename P, typename G, bool COPY>
+static int launch_adamw(hipStream_t s, AdamwArgs& a, bool narrow, void* const* p, const void* const* g, void* const* copy, const int64_t* n, int64_t count) {
+  AdamwTable<COPY> t;
+  a.count = 0;
+  t.chunk[0] = 0;
+  int64_t first = 0;
+  for (int64_t i = 0; i <= count; ++i) {
+    const int64_t chunks = i < count ? ceil_div64(n[i], ADAMW_CHUNK) : 0;
+    // (fewer than 2^32 threads to a launch)
+    if (a.count && (i == count || a.count == t.MOST || t.chunk[a.count] + chunks >= (1 << 24))) {
+      const dim3 grid(t.chunk[a.count]), block(256);
+      if (narrow) LORACT_LAUNCH("adamw", s, (adamw_kernel<P, G, true, COPY>), grid, block, 0, t, a);
+      else LORACT_LAUNCH("adamw", s, (adamw_kernel<P, G, false, COPY>), grid, block, 0, t, a);
+      a.count = 0;
+    }
+    if (!chunks) continue;
+    t.p[a.count] = p[i];
+    t.g[a.count] = g[i];
+    if (COPY) t.copy[a.count] = (bf16_t*)copy[i];
+    t.n[a.count] = n[i];
+    t.first[a.count] = (uint32_t)(first / LORACT_ADAMW_BLOCK);
+    t.chunk[a.count + 1] = t.chunk[a.count] + (uint32_t)chunks;
+    ++a.count;
+    first += (int64_t)align_up((size_t)n[i], LORACT_ADAMW_BLOCK);
+  }
   return LORACT_OK;
 }

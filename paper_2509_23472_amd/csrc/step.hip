@@ -29,11 +29,10 @@ static int adamw_meets(void* const* p, const void* const* g, void* const* copy, 
   size_t k = 0;
   for (const Span& s : state)
     if (s.hi > s.lo) out[k++] = s;
-  for (int64_t i = 0; i < count; ++i) {
-    if (n[i] < 1) continue;
-    out[k++] = {(uintptr_t)p[i], (uintptr_t)p[i] + (uintptr_t)n[i] * p_size};
-    if (copy && copy[i]) out[k++] = {(uintptr_t)copy[i], (uintptr_t)copy[i] + (uintptr_t)n[i] * 2};
-  }
+  for (int64_t i = 0; i < count; ++i)
+    if (n[i] > 0) out[k++] = {(uintptr_t)p[i], (uintptr_t)p[i] + (uintptr_t)n[i] * p_size};
+  for (int64_t i = 0; copy && i < count; ++i)
+    if (n[i] > 0 && copy[i]) out[k++] = {(uintptr_t)copy[i], (uintptr_t)copy[i] + (uintptr_t)n[i] * 2};
   std::sort(out, out + k);
   int meets = 0;
   for (size_t i = 1; i < k; ++i) meets |= out[i].lo < out[i - 1].hi;
@@ -68,6 +67,7 @@ int loract_adamw(void* const* p, const void* const* g, void* const* copy, const 
     if (n[i] && ((uintptr_t)p[i] % (p_bf16 ? 2 : 4) || (uintptr_t)g[i] % (g_bf16 ? 2 : 4) || (copy && (uintptr_t)copy[i] % 2))) return LORACT_ERR_INVALID_ARG;
     if (n[i] > (1ll << 33)) return LORACT_ERR_UNSUPPORTED;
     total += adamw_padded(n[i]);
+    if (total > (1ll << 39)) return LORACT_ERR_UNSUPPORTED;
   }
   if (!total) return LORACT_OK;
   if (!m_dev || !v_dev || (narrow && !exps_dev)) return LORACT_ERR_INVALID_ARG;
@@ -91,30 +91,12 @@ int loract_adamw(void* const* p, const void* const* g, void* const* copy, const 
   a.beta2 = (float)params->beta2; a.one_beta2 = (float)(1.0 - params->beta2);
   a.eps = (float)params->eps; a.seed = params->seed; a.step = params->step; a.rate = a.inv = a.decay = 0.0f;
   if (!lr_dev && !step_dev) adamw_rates(a, params->lr, pow(params->beta1, (double)params->step), pow(params->beta2, (double)params->step));
-  AdamwTable t;
-  a.count = 0;
-  t.chunk[0] = 0;
-  int64_t first = 0;
-  for (int64_t i = 0; i <= count; ++i) {
-    const int64_t chunks = i < count ? ceil_div64(n[i], ADAMW_CHUNK) : 0;
-    // (fewer than 2^32 threads to a launch)
-    if (a.count && (i == count || a.count == ADAMW_TENSORS || t.chunk[a.count] + chunks >= (1 << 24))) {
-      const hipStream_t s = (hipStream_t)stream;
-      LORACT_TRY(p_bf16 ? (g_bf16 ? launch_adamw<bf16_t, bf16_t>(s, t, a, narrow) : launch_adamw<bf16_t, float>(s, t, a, narrow))
-                        : (g_bf16 ? launch_adamw<float, bf16_t>(s, t, a, narrow) : launch_adamw<float, float>(s, t, a, narrow)));
-      a.count = 0;
-    }
-    if (!chunks) continue;
-    t.p[a.count] = p[i];
-    t.g[a.count] = g[i];
-    t.copy[a.count] = copy ? (bf16_t*)copy[i] : nullptr;
-    t.n[a.count] = n[i];
-    t.first[a.count] = first;
-    t.chunk[a.count + 1] = t.chunk[a.count] + (uint32_t)chunks;
-    ++a.count;
-    first += adamw_padded(n[i]);
-  }
-  return LORACT_OK;
+  const hipStream_t s = (hipStream_t)stream;
+#define LORACT_ADAMW(P, G, COPY) launch_adamw<P, G, COPY>(s, a, narrow, p, g, copy, n, count)
+  if (p_bf16) return g_bf16 ? LORACT_ADAMW(bf16_t, bf16_t, false) : LORACT_ADAMW(bf16_t, float, false);
+  if (copy) return g_bf16 ? LORACT_ADAMW(float, bf16_t, true) : LORACT_ADAMW(float, float, true);
+  return g_bf16 ? LORACT_ADAMW(float, bf16_t, false) : LORACT_ADAMW(float, float, false);
+#undef LORACT_ADAMW
 }
 
 }  // extern "C"
