@@ -40,6 +40,7 @@ struct LqArgs {
   float* part;           // splits x m x ldt
   int ldt, splits, shares;           // shares: workgroups (z) that share the adapters of a tile
   int64_t k_per_split;
+  int trips, groups;                 // ordered tokens, second launch: times 16 E columns per workgroup, workgroups to a tile
   int *tiles, *order;                // ordered tokens: their number, then group and size of each tile; the tokens, 64 to a tile
 };
 #define LQ_TILE 64
@@ -135,73 +136,70 @@ __device__ inline typename Ln<T>::frag lq_load(const T* at, int64_t left) {
   return v;
 }
 
-// TB: blocks of 16 tokens per tile.  SB: blocks of 16 columns of A.  SORTED: halves of the ordered tiles.
-template <typename T, int TB, int SB, bool SORTED>
+// The transposed fragment of 16 columns of A: k from E q on, column c, of rows `pitch` bytes apart that start at `at`.
+template <typename T>
+__device__ inline typename Ln<T>::frag lq_turned(const unsigned char* at, int pitch, int c, int q) {
+  constexpr int E = Ln<T>::E;
+  typename Ln<T>::frag f;
+  if constexpr (sizeof(T) == 2) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    at += (8 * q + (c >> 2)) * pitch + (c & 3) * 8;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * pitch));
+    f = __builtin_bit_cast(typename Ln<T>::frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) f[e] = *(const T*)(at + (E * q + e) * pitch + c * 4);
+  }
+  return f;
+}
+// A piece of a row of A: columns col .. col + E - 1 of row k, zeros where there is none.
+template <typename T>
+__device__ inline typename Ln<T>::frag lq_piece(const LqArgs& g, const T* a, int64_t k, int64_t k_end, int col) {
+  const bool here = k < k_end && col < g.r;
+  if (!g.a_pieces) return lq_load<T>(a + k * g.r + col, here ? g.r - col : 0);
+  typename Ln<T>::frag v = {};
+  if (here) v = *(const typename Ln<T>::frag*)(a + k * g.r + col);
+  return v;
+}
+
+// Few tokens: tiles of 16 in the order they come.  SB: blocks of 16 columns of A.
+template <typename T, int SB>
 __global__ __launch_bounds__(64 * LQ_WAVES) void lora_down_kernel(LqArgs g) {
-  constexpr int E = Ln<T>::E, STEP = Ln<T>::STEP, U = SB == 1 ? 4 : 2, QUADS = TB * SB * 64, PER = 16 / E;
+  constexpr int E = Ln<T>::E, STEP = Ln<T>::STEP, U = SB == 1 ? 4 : 2, QUADS = SB * 64, PER = 16 / E;
   typedef typename Ln<T>::frag frag;
   constexpr int TURN_BYTES = LQ_WAVES * U * SB * 1024, PART_BYTES = LQ_WAVES * QUADS * 16;
   __shared__ __attribute__((aligned(16))) unsigned char smem[TURN_BYTES > PART_BYTES ? TURN_BYTES : PART_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
-  int64_t token[TB];                                 // token c of each block
-  int id = -1, blocks = TB;
-  bool live = false;
-  uint64_t done = 0;                                 // tokens whose T is written
-  if constexpr (SORTED) {
-    const int tile = blockIdx.x / (LQ_TILE / (16 * TB)), part = blockIdx.x % (LQ_TILE / (16 * TB));
-    if (tile >= g.tiles[0]) return;
-    id = g.tiles[2 + 2 * tile];
-    const int left = g.tiles[3 + 2 * tile] - part * (16 * TB);
-    if (left <= 0 || (int64_t)id >= g.adapters) return;
-    blocks = left > 16 ? TB : 1;
-    done = left >= 16 * TB ? ~0ull >> (64 - 16 * TB) : (1ull << left) - 1;
-#pragma unroll
-    for (int b = 0; b < TB; ++b) token[b] = g.order[tile * LQ_TILE + part * (16 * TB) + (done >> (16 * b + c) & 1 ? 16 * b + c : 0)];
-  } else {
-    const int64_t first = (int64_t)blockIdx.x * (16 * TB), mine = first + (lane < 16 * TB ? lane : 0);
-    live = lane < 16 * TB && mine < g.m;
-    id = live ? g.ids[mine] : -1;
-#pragma unroll
-    for (int b = 0; b < TB; ++b) token[b] = first + 16 * b + c < g.m ? first + 16 * b + c : g.m - 1;
-  }
+  const int64_t first = (int64_t)blockIdx.x * 16, mine = first + (lane < 16 ? lane : 0);
+  const bool live = lane < 16 && mine < g.m;
+  const int id = live ? g.ids[mine] : -1;
+  const int64_t token = first + c < g.m ? first + c : g.m - 1;
   const int64_t k_beg0 = (int64_t)blockIdx.y * g.k_per_split, k_end0 = k_beg0 + g.k_per_split < g.k ? k_beg0 + g.k_per_split : g.k;
   const int64_t per = ((k_end0 - k_beg0 + STEP * LQ_WAVES - 1) / (STEP * LQ_WAVES)) * STEP;
   const int64_t k_beg = k_beg0 + wave * per, k_end = k_beg + per < k_end0 ? k_beg + per : k_end0;
-  const T* x[TB];
+  const T* const x = (const T*)g.X + token * g.ldx;
+  f32x4 total[SB];
 #pragma unroll
-  for (int b = 0; b < TB; ++b) x[b] = (const T*)g.X + token[b] * g.ldx;
-  f32x4 total[TB][SB];
-#pragma unroll
-  for (int b = 0; b < TB; ++b)
-#pragma unroll
-    for (int s = 0; s < SB; ++s) total[b][s] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < SB; ++s) total[s] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
   unsigned char* const turn = smem + wave * (U * SB * 1024);
-  auto product = [&](int d, uint64_t same) {
+  uint64_t done = 0;                                 // tokens whose T is written
+  lq_adapters(g, id, live, blockIdx.z, [&](int d, uint64_t same) {
     done |= same;
     const T* const a = (const T*)g.A + (int64_t)d * g.k * g.r;
-    f32x4 acc[TB][SB];
+    f32x4 acc[SB];
 #pragma unroll
-    for (int b = 0; b < TB; ++b)
-#pragma unroll
-      for (int s = 0; s < SB; ++s) acc[b][s] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < SB; ++s) acc[s] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
     for (int64_t k0 = k_beg; k0 < k_end; k0 += STEP * U) {
-      frag st[U][TB], sm[U][SB];
+      frag st[U], sm[U][SB];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int64_t k = k0 + STEP * u + E * q, row = k0 + STEP * u + lane / PER;
+        const int64_t k = k0 + STEP * u + E * q;
+        st[u] = lq_load<T>(x + k, k_end - k);
 #pragma unroll
-        for (int b = 0; b < TB; ++b) st[u][b] = lq_load<T>(x[b] + k, b < blocks ? k_end - k : 0);
-#pragma unroll
-        for (int s = 0; s < SB; ++s) {
-          const int col = 16 * s + E * (lane % PER);
-          if (g.a_pieces) {
-            sm[u][s] = (frag){};
-            if (row < k_end && col < g.r) sm[u][s] = *(const frag*)(a + row * g.r + col);
-          } else {
-            sm[u][s] = lq_load<T>(a + row * g.r + col, row < k_end ? g.r - col : 0);
-          }
-        }
+        for (int s = 0; s < SB; ++s) sm[u][s] = lq_piece<T>(g, a, k0 + STEP * u + lane / PER, k_end, 16 * s + E * (lane % PER));
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -211,54 +209,91 @@ __global__ __launch_bounds__(64 * LQ_WAVES) void lora_down_kernel(LqArgs g) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int s = 0; s < SB; ++s) {
-          const unsigned char* at = turn + (u * SB + s) * 1024;
-          if constexpr (sizeof(T) == 2) {
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-            at += (8 * q + (c >> 2)) * 32 + (c & 3) * 8;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * 32));
-            sm[u][s] = __builtin_bit_cast(frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-          } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) sm[u][s][e] = *(const T*)(at + (E * q + e) * 64 + c * 4);
-          }
-        }
+        for (int s = 0; s < SB; ++s) sm[u][s] = lq_turned<T>(turn + (u * SB + s) * 1024, 16 * (int)sizeof(T), c, q);
       sb_wave_sync();
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int b = 0; b < TB; ++b)
-#pragma unroll
-          for (int s = 0; s < SB; ++s) acc[b][s] = ln_mfma(sm[u][s], st[u][b], acc[b][s]);
+        for (int s = 0; s < SB; ++s) acc[s] = ln_mfma(sm[u][s], st[u], acc[s]);
     }
+    const bool own = same >> c & 1;                  // a lane's column is token c
 #pragma unroll
-    for (int b = 0; b < TB; ++b) {                   // a lane's column is token c of the block
-      const bool own = same >> (16 * b + c) & 1;
+    for (int s = 0; s < SB; ++s)
 #pragma unroll
-      for (int s = 0; s < SB; ++s)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) total[b][s][u] = own ? acc[b][s][u] : total[b][s][u];
-    }
-  };
-  if constexpr (SORTED) product(id, done);
-  else lq_adapters(g, id, live, blockIdx.z, product);
+      for (int u = 0; u < 4; ++u) total[s][u] = own ? acc[s][u] : total[s][u];
+  });
   if (!done) return;                                 // (the same for all waves)
   __syncthreads();
   f32x4* const part = (f32x4*)smem;
 #pragma unroll
-  for (int b = 0; b < TB; ++b)
-#pragma unroll
-    for (int s = 0; s < SB; ++s) part[wave * QUADS + (b * SB + s) * 64 + lane] = total[b][s];
+  for (int s = 0; s < SB; ++s) part[wave * QUADS + s * 64 + lane] = total[s];
   __syncthreads();
   for (int i = threadIdx.x; i < QUADS; i += 64 * LQ_WAVES) {
-    const int b = i / (64 * SB), s = i / 64 % SB, l = i & 63;
     f32x4 v = part[i];
 #pragma unroll
     for (int w = 1; w < LQ_WAVES; ++w) v += part[w * QUADS + i];
-    if (done >> (16 * b + c) & 1)                    // (l is the lane)
-      *(f32x4*)(g.part + ((int64_t)blockIdx.y * g.m + (b ? token[TB - 1] : token[0])) * g.ldt + 16 * s + 4 * (l >> 4)) = v;
+    if (done >> c & 1) *(f32x4*)(g.part + ((int64_t)blockIdx.y * g.m + token) * g.ldt + 16 * (i / 64) + 4 * q) = v;
+  }
+}
+
+// Ordered tokens: a tile of 64, 16 to each wave; A passes through LDS in slabs that all waves read, the next one (and the next part of X) on
+// its way while one is multiplied.
+template <typename T, int SB>
+__global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_down_sorted_kernel(LqArgs g) {
+  constexpr int E = Ln<T>::E, STEP = Ln<T>::STEP, U = 4, SLAB = U * STEP, PITCH = 16 * SB * (int)sizeof(T) + (SB == 4 ? 16 : 0);
+  constexpr int PER = 16 * SB / E, TRIPS = SLAB * PER / (64 * LQ_UP_WAVES);      // pieces to a row, and of a slab to a thread
+  static_assert(SLAB * PER % (64 * LQ_UP_WAVES) == 0, "whole trips");
+  typedef typename Ln<T>::frag frag;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[2][SLAB * PITCH];
+  const int tile = blockIdx.x;
+  if (tile >= g.tiles[0]) return;
+  const int d = g.tiles[2 + 2 * tile], size = g.tiles[3 + 2 * tile];
+  if ((int64_t)d >= g.adapters) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, q = lane >> 4;
+  const int64_t k_beg = (int64_t)blockIdx.y * g.k_per_split, k_end = k_beg + g.k_per_split < g.k ? k_beg + g.k_per_split : g.k;
+  const bool work = 16 * wave < size, live = 16 * wave + c < size;
+  const int64_t token = g.order[tile * LQ_TILE + (live ? 16 * wave + c : 0)];
+  const T* const x = (const T*)g.X + token * g.ldx;
+  const T* const a = (const T*)g.A + (int64_t)d * g.k * g.r;
+  frag xs[U], as[TRIPS];
+  auto load = [&](int64_t k0) {
+#pragma unroll
+    for (int i = 0; i < TRIPS; ++i) {
+      const int at = threadIdx.x + i * (64 * LQ_UP_WAVES);
+      as[i] = lq_piece<T>(g, a, k0 + at / PER, k_end, E * (at % PER));
+    }
+    if (work) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) xs[u] = lq_load<T>(x + k0 + STEP * u + E * q, k_end - (k0 + STEP * u + E * q));
+    }
+  };
+  f32x4 acc[SB];
+#pragma unroll
+  for (int s = 0; s < SB; ++s) acc[s] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+  load(k_beg);
+  int turn = 0;
+  for (int64_t k0 = k_beg; k0 < k_end; k0 += SLAB, turn ^= 1) {
+    frag now[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) now[u] = xs[u];
+#pragma unroll
+    for (int i = 0; i < TRIPS; ++i) {
+      const int at = threadIdx.x + i * (64 * LQ_UP_WAVES);
+      *(frag*)(smem[turn] + at / PER * PITCH + at % PER * 16) = as[i];
+    }
+    if (k0 + SLAB < k_end) load(k0 + SLAB);
+    sb_barrier_lds();                                // (two slabs: who writes one has passed the barrier behind its last reading)
+    if (work) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int s = 0; s < SB; ++s) acc[s] = ln_mfma(lq_turned<T>(smem[turn] + STEP * u * PITCH + 16 * s * (int)sizeof(T), PITCH, c, q), now[u], acc[s]);
+    }
+  }
+  if (live) {
+#pragma unroll
+    for (int s = 0; s < SB; ++s) *(f32x4*)(g.part + ((int64_t)blockIdx.y * g.m + token) * g.ldt + 16 * s + 4 * q) = acc[s];
   }
 }
 
@@ -308,8 +343,8 @@ struct LqOut {
   typedef O vec __attribute__((ext_vector_type(E)));
   typedef vec any __attribute__((aligned(sizeof(O))));
 };
-// RS: steps of the rank.  TB: blocks of 16 tokens per wave.
-template <typename T, typename O, int TB, int RS>
+// Few tokens: tiles of 16 in the order they come; a wave has 16 E columns.  RS: steps of the rank.
+template <typename T, typename O, int RS>
 __global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_up_kernel(LqArgs g) {
   constexpr int E = Ln<T>::E, STEP = Ln<T>::STEP;
   typedef typename Ln<T>::frag frag;
@@ -318,144 +353,153 @@ __global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_up_kernel(LqArgs g) {
   const int c = lane & 15, q = lane >> 4;
   const int64_t col = ((int64_t)blockIdx.y * LQ_UP_WAVES + wave) * (16 * E) + E * c;       // of this lane's E columns
   if (col - E * c >= g.n) return;
-  const int64_t first = (int64_t)blockIdx.x * (16 * TB);
-  const int64_t mine = first + (lane < 16 * TB ? lane : 0);
-  const bool live = lane < 16 * TB && mine < g.m;
+  const int64_t first = (int64_t)blockIdx.x * 16;
+  const int64_t mine = first + (lane < 16 ? lane : 0);
+  const bool live = lane < 16 && mine < g.m;
   const int id = live ? g.ids[mine] : -1;
-  const float scale = live && id >= 0 && id < g.adapters ? (g.scales ? g.scales[id] : 1.0f) : 0.0f;
+  const int64_t token = first + c < g.m ? first + c : g.m - 1;
   const int here = g.n - col < E ? (int)(g.n - col < 0 ? 0 : g.n - col) : E;                // columns that exist
-  auto put = [&](int64_t token, const float (&v)[E]) {
-    const O* const rp = (const O*)g.R + token * g.ldr + col;
-    O* const yp = (O*)g.Y + token * g.ldy + col;
+  // R and Y of the lane's columns, in turn: read early, written when the product is there
+  auto get = [&](int64_t row, float (&v)[E]) {
+    const O* const rp = (const O*)g.R + row * g.ldr + col;
+    if (g.R && here == E) {
+      const typename LqOut<O, E>::vec y = *(const out_any*)rp;
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = (float)y[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = g.R && e < here ? (float)rp[e] : 0.0f;
+    }
+  };
+  auto put = [&](int64_t row, const float (&v)[E]) {
+    O* const yp = (O*)g.Y + row * g.ldy + col;
     if (here == E) {
       typename LqOut<O, E>::vec y;
-      if (g.R) {
-        y = *(const out_any*)rp;
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = (O)((float)y[e] + v[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = (O)v[e];
-      }
+      for (int e = 0; e < E; ++e) y[e] = (O)v[e];
       *(out_any*)yp = y;
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (e < here) yp[e] = (O)((g.R ? (float)rp[e] : 0.0f) + v[e]);
+        if (e < here) yp[e] = (O)v[e];
     }
   };
   lq_adapters(g, id, live, blockIdx.z, [&](int d, uint64_t same) {
-    // the lane's E x E blocks of B, turned: f[s][j] has column E c + j, rows STEP s + E q ..
-    frag f[RS][E];
-    const T* const b0 = (const T*)g.B + (int64_t)d * g.r * g.n + col;
+    const unsigned rows = (unsigned)same;
+    const float by = g.scales ? g.scales[d] : 1.0f;
+    float res[4][E];
 #pragma unroll
-    for (int s = 0; s < RS; ++s) {
-      frag v[E];
+    for (int i = 0; i < 4; ++i)
+      if (rows >> (4 * q + i) & 1) get(first + 4 * q + i, res[i]);
+    f32x4 acc[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) acc[j] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    const T* const b0 = (const T*)g.B + (int64_t)d * g.r * g.n + col;
+    frag v[RS][E];                                   // the lane's E x E blocks of B
+#pragma unroll
+    for (int s = 0; s < RS; ++s)
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         const int row = STEP * s + E * q + i;
         if (g.b_pieces) {
-          v[i] = (frag){};
-          if (row < g.r && here == E) v[i] = *(const frag*)(b0 + (int64_t)row * g.n);
+          v[s][i] = (frag){};
+          if (row < g.r && here == E) v[s][i] = *(const frag*)(b0 + (int64_t)row * g.n);
         } else {
-          v[i] = lq_load<T>(b0 + (int64_t)row * g.n, row < g.r ? here : 0);
+          v[s][i] = lq_load<T>(b0 + (int64_t)row * g.n, row < g.r ? here : 0);
         }
       }
 #pragma unroll
-      for (int j = 0; j < E; ++j) {
+    for (int s = 0; s < RS; ++s) {
+      float t[E] = {};
+      const int k = STEP * s + E * q;
+      if ((rows >> c & 1) && k < g.r) lq_t<E>(g, token, k, by, t);            // (rows of other adapters may not be written at all)
+      frag hi, lo;
+      lq_parts<T>(t, hi, lo);
+#pragma unroll
+      for (int j = 0; j < E; ++j) {                  // turned: column E c + j, rows STEP s + E q ..
+        frag f;
         if constexpr (sizeof(T) == 2) {
           typedef unsigned int words __attribute__((ext_vector_type(4)));
           words w;
 #pragma unroll
           for (int p = 0; p < 4; ++p)
-            w[p] = __builtin_amdgcn_perm(__builtin_bit_cast(words, v[2 * p + 1])[j / 2], __builtin_bit_cast(words, v[2 * p])[j / 2],
+            w[p] = __builtin_amdgcn_perm(__builtin_bit_cast(words, v[s][2 * p + 1])[j / 2], __builtin_bit_cast(words, v[s][2 * p])[j / 2],
                                          j & 1 ? 0x07060302u : 0x05040100u);
-          f[s][j] = __builtin_bit_cast(frag, w);
+          f = __builtin_bit_cast(frag, w);
         } else {
 #pragma unroll
-          for (int e = 0; e < E; ++e) f[s][j][e] = v[e][j];
+          for (int e = 0; e < E; ++e) f[e] = v[s][e][j];
         }
+        acc[j] = ln_mfma(hi, f, acc[j]);
+        if constexpr (sizeof(T) == 2) acc[j] = ln_mfma(lo, f, acc[j]);
       }
     }
 #pragma unroll
-    for (int b = 0; b < TB; ++b) {
-      const unsigned rows = (unsigned)(same >> (16 * b)) & 0xffffu;
-      if (!rows) continue;
-      const int64_t token = first + 16 * b + c < g.m ? first + 16 * b + c : g.m - 1;
-      const float by = __shfl(scale, 16 * b + c);
-      f32x4 acc[E];
+    for (int i = 0; i < 4; ++i)
+      if (rows >> (4 * q + i) & 1) {
+        float y[E];
 #pragma unroll
-      for (int j = 0; j < E; ++j) acc[j] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int s = 0; s < RS; ++s) {
-        float t[E] = {};
-        const int k = STEP * s + E * q;
-        if ((rows >> c & 1) && k < g.r) lq_t<E>(g, token, k, by, t);            // (rows of other adapters may not be written at all)
-        frag hi, lo;
-        lq_parts<T>(t, hi, lo);
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-          acc[j] = ln_mfma(hi, f[s][j], acc[j]);
-          if constexpr (sizeof(T) == 2) acc[j] = ln_mfma(lo, f[s][j], acc[j]);
-        }
+        for (int j = 0; j < E; ++j) y[j] = res[i][j] + acc[j][i];
+        put(first + 4 * q + i, y);
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (here && (rows >> (4 * q + i) & 1)) {
-          float v[E];
-#pragma unroll
-          for (int j = 0; j < E; ++j) v[j] = acc[j][i];
-          put(first + 16 * b + 4 * q + i, v);
-        }
-    }
   });
   if (blockIdx.z) return;
   // tokens without an adapter, and with one that is not there (asked of all lanes, also those without columns: they hold tokens)
   const uint64_t past = __ballot(live && (int64_t)id >= g.adapters), none = __ballot(live && id < 0);
-  if (!here) return;
   for (uint64_t left = g.in_place ? past : past | none; left; left &= left - 1) {
     const int t = __builtin_ctzll(left);
     if ((t & 3) != q) continue;                      // (rows in turn: the lanes of a quarter hold all of the wave's columns)
     float v[E];
+    get(first + t, v);
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = past >> t & 1 ? __builtin_nanf("") : 0.0f;
+    for (int e = 0; e < E; ++e) v[e] = past >> t & 1 ? __builtin_nanf("") : v[e];
     put(first + t, v);
   }
 }
 
-// Ordered tokens: a tile of 64, 16 to each wave, and 16 E columns, whose part of B passes through LDS.  B gives the rows of the product, in an
-// order that leaves a lane with E consecutive columns of its token: the transposing reads take chunks of four columns 2 E bytes apart.
+// Ordered tokens: a tile of 64, 16 to each wave, and `trips` times 16 E columns.  T is read once; the part of B for 16 E columns passes through LDS,
+// the next one (and R) on its way meanwhile.  B gives the rows of the product, in an order that leaves a lane with E consecutive columns of its
+// token: the transposing reads take chunks of four columns 2 E bytes apart.
 template <typename T, typename O, int RS>
 __global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_up_sorted_kernel(LqArgs g) {
-  constexpr int E = Ln<T>::E, STEP = Ln<T>::STEP, PITCH = 256 + 64, J = 4;
+  constexpr int E = Ln<T>::E, STEP = Ln<T>::STEP, PITCH = 256 + 64, J = 4, PIECES = RS * STEP / 16;      // (16 rows of 16 pieces at a time)
   typedef typename Ln<T>::frag frag;
   typedef typename LqOut<O, E>::any out_any;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[RS * STEP * PITCH];
-  const int cols = (int)((g.n + 16 * E - 1) / (16 * E)), tile = blockIdx.x / cols;       // (the columns of a tile one after the other)
+  typedef typename LqOut<O, E>::vec out_vec;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[2][RS * STEP * PITCH];
+  const int tile = blockIdx.x / g.groups;            // (the columns of a tile one after the other)
   if (tile >= g.tiles[0]) return;
   const int d = g.tiles[2 + 2 * tile], size = g.tiles[3 + 2 * tile];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
-  const int64_t first = (int64_t)(blockIdx.x - tile * cols) * (16 * E);
-  const bool there = (int64_t)d < g.adapters;
-  if (there) {
-    const T* const b = (const T*)g.B + (int64_t)d * g.r * g.n;
-    constexpr int TRIPS = RS * STEP / 16;            // 16 rows of 16 pieces at a time
-    frag v[TRIPS];
-    const int64_t col = first + E * (threadIdx.x & 15);
-#pragma unroll
-    for (int i = 0; i < TRIPS; ++i) {
-      const int row = 16 * i + (threadIdx.x >> 4);
-      v[i] = (frag){};
-      if (row < g.r && col < g.n) v[i] = g.b_pieces ? *(const frag*)(b + (int64_t)row * g.n + col) : lq_load<T>(b + (int64_t)row * g.n + col, g.n - col);
-    }
-#pragma unroll
-    for (int i = 0; i < TRIPS; ++i) *(frag*)(smem + (16 * i + (threadIdx.x >> 4)) * PITCH + 16 * (threadIdx.x & 15)) = v[i];
-  }
-  const bool live = 16 * wave + c < size;
+  const int64_t first = (int64_t)(blockIdx.x - tile * g.groups) * g.trips * (16 * E);
+  const int64_t end = first + (int64_t)g.trips * (16 * E) < g.n ? first + (int64_t)g.trips * (16 * E) : g.n;
+  const bool there = (int64_t)d < g.adapters, work = 16 * wave < size, live = 16 * wave + c < size;
   const int64_t token = g.order[tile * LQ_TILE + (live ? 16 * wave + c : 0)];
+  const T* const b = (const T*)g.B + (int64_t)(there ? d : 0) * g.r * g.n;
+  const O* const rp = (const O*)g.R + token * g.ldr;
+  O* const yp = (O*)g.Y + token * g.ldy;
+  frag v[PIECES];
+  out_vec res[J];
+  auto load = [&](int64_t at) {
+    const int64_t col = at + E * (threadIdx.x & 15);
+    if (there) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const int row = 16 * i + (threadIdx.x >> 4);
+        v[i] = (frag){};
+        if (row < g.r && col < g.n) v[i] = g.b_pieces ? *(const frag*)(b + (int64_t)row * g.n + col) : lq_load<T>(b + (int64_t)row * g.n + col, g.n - col);
+      }
+    }
+    if (g.R && live) {
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (at + 4 * E * j + E * q + E <= g.n) res[j] = *(const out_any*)(rp + at + 4 * E * j + E * q);
+    }
+  };
+  load(first);
   frag hi[RS], lo[RS];
-  if (there) {
+  if (there && work) {
     const float by = g.scales ? g.scales[d] : 1.0f;
 #pragma unroll
     for (int s = 0; s < RS; ++s) {
@@ -465,58 +509,59 @@ __global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_up_sorted_kernel(LqArgs
       lq_parts<T>(t, hi[s], lo[s]);
     }
   }
-  const O* const rp = (const O*)g.R + token * g.ldr;
-  O* const yp = (O*)g.Y + token * g.ldy;
-  typename LqOut<O, E>::vec res[J];
+  int turn = 0;
+  for (int64_t at = first; at < end; at += 16 * E, turn ^= 1) {
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int64_t col = first + 4 * E * j + E * q;
-    if (g.R && live && col + E <= g.n) res[j] = *(const out_any*)(rp + col);
-  }
-  __syncthreads();
-  if (16 * wave >= size) return;
+    for (int i = 0; i < PIECES; ++i) *(frag*)(smem[turn] + (16 * i + (threadIdx.x >> 4)) * PITCH + 16 * (threadIdx.x & 15)) = v[i];
+    out_vec now[J];
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    f32x4 acc[E / 4];
+    for (int j = 0; j < J; ++j) now[j] = res[j];
+    if (at + 16 * E < end) load(at + 16 * E);
+    sb_barrier_lds();                                // (two parts: who writes one has passed the barrier behind its last reading)
+    if (!work) continue;
 #pragma unroll
-    for (int h = 0; h < E / 4; ++h) acc[h] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
-    if (there) {
+    for (int j = 0; j < J; ++j) {
+      f32x4 acc[E / 4];
 #pragma unroll
-      for (int s = 0; s < RS; ++s)
+      for (int h = 0; h < E / 4; ++h) acc[h] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+      if (there) {
 #pragma unroll
-        for (int h = 0; h < E / 4; ++h) {
-          frag f;
-          if constexpr (sizeof(T) == 2) {
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-            const unsigned char* at = smem + (STEP * s + 8 * q + (c >> 2)) * PITCH + 64 * j + 16 * (c & 3) + 8 * h;
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * PITCH));
-            f = __builtin_bit_cast(frag, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-          } else {
+        for (int s = 0; s < RS; ++s)
 #pragma unroll
-            for (int e = 0; e < E; ++e) f[e] = *(const T*)(smem + (STEP * s + E * q + e) * PITCH + 64 * j + 4 * c);
+          for (int h = 0; h < E / 4; ++h) {
+            frag f;
+            if constexpr (sizeof(T) == 2) {
+              typedef short s16x4 __attribute__((ext_vector_type(4)));
+              typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+              const unsigned char* from = smem[turn] + (STEP * s + 8 * q + (c >> 2)) * PITCH + 64 * j + 16 * (c & 3) + 8 * h;
+              const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)from);
+              const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + 4 * PITCH));
+              f = __builtin_bit_cast(frag, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+            } else {
+#pragma unroll
+              for (int e = 0; e < E; ++e) f[e] = *(const T*)(smem[turn] + (STEP * s + E * q + e) * PITCH + 64 * j + 4 * c);
+            }
+            acc[h] = ln_mfma(f, hi[s], acc[h]);
+            if constexpr (sizeof(T) == 2) acc[h] = ln_mfma(f, lo[s], acc[h]);
           }
-          acc[h] = ln_mfma(f, hi[s], acc[h]);
-          if constexpr (sizeof(T) == 2) acc[h] = ln_mfma(f, lo[s], acc[h]);
-        }
-    } else if ((int64_t)d > g.adapters) {
+      } else if ((int64_t)d > g.adapters) {
 #pragma unroll
-      for (int h = 0; h < E / 4; ++h)
+        for (int h = 0; h < E / 4; ++h)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[h][e] = __builtin_nanf("");
-    }
-    const int64_t col = first + 4 * E * j + E * q;
-    if (!live || col >= g.n) continue;
-    if (col + E <= g.n) {
-      typename LqOut<O, E>::vec y;
+          for (int e = 0; e < 4; ++e) acc[h][e] = __builtin_nanf("");
+      }
+      const int64_t col = at + 4 * E * j + E * q;
+      if (!live || col >= g.n) continue;
+      if (col + E <= g.n) {
+        out_vec y;
 #pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = (O)((g.R ? (float)res[j][e] : 0.0f) + acc[e / 4][e % 4]);
-      *(out_any*)(yp + col) = y;
-    } else {
+        for (int e = 0; e < E; ++e) y[e] = (O)((g.R ? (float)now[j][e] : 0.0f) + acc[e / 4][e % 4]);
+        *(out_any*)(yp + col) = y;
+      } else {
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (col + e < g.n) yp[col + e] = (O)((g.R ? (float)rp[col + e] : 0.0f) + acc[e / 4][e % 4]);
+        for (int e = 0; e < E; ++e)
+          if (col + e < g.n) yp[col + e] = (O)((g.R ? (float)rp[col + e] : 0.0f) + acc[e / 4][e % 4]);
+      }
     }
   }
 }
@@ -525,25 +570,25 @@ struct LqPlan {
   bool sorted;
   int64_t tiles;         // at most
   size_t part_bytes, tile_bytes, bytes;
-  int tb, splits, shares, up_tb, up_shares, ldt;
-  int64_t k_per_split;
+  int splits, shares, up_shares, ldt, trips;
+  int64_t k_per_split, groups;
 };
 static LqPlan lora_requests_plan(int64_t m, int64_t k, int64_t n, int r, int64_t adapters, bool bf16) {
   LqPlan p;
-  const int e = bf16 ? 8 : 4, step = 4 * e * LQ_WAVES;
+  const int e = bf16 ? 8 : 4;
   p.sorted = m > 64 && adapters <= LQ_SORTED;
-  p.tiles = p.sorted ? ceil_div64(m, LQ_TILE) + std::min<int64_t>(adapters + 2, m) : 0;
   p.ldt = r <= 16 ? 16 : (r <= 32 ? 32 : 64);
-  p.tb = p.sorted || ceil_div64(m, 32) >= 256 ? 2 : 1;
-  const int64_t tiles = ceil_div64(m, 16 * p.tb), most = p.sorted ? 1 : std::min<int64_t>(16 * p.tb, adapters);
-  p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, most));
+  const int64_t cols = ceil_div64(n, 16 * e), most = std::min<int64_t>(16, adapters);
+  // K splits: 512 workgroups, of a slab (all waves together a step) at least
+  const int64_t tiles = ceil_div64(m, p.sorted ? LQ_TILE : 16), step = (p.sorted ? 16 : 4 * LQ_WAVES) * e;
+  p.shares = p.sorted ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, most));
   const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / (tiles * p.shares), ceil_div64(k, step)), 16));
   p.k_per_split = ceil_div64(ceil_div64(k, splits), step) * step;
   p.splits = (int)ceil_div64(k, p.k_per_split);
-  const int64_t cols = ceil_div64(n, 16 * e);
-  p.up_tb = cols * ceil_div64(m, 64) >= 2048 ? 4 : 1;
-  const int64_t up_tiles = ceil_div64(m, 16 * p.up_tb);
-  p.up_shares = (int)std::max<int64_t>(1, std::min<int64_t>(2048 / (cols * up_tiles), std::min<int64_t>(16 * p.up_tb, adapters)));
+  p.up_shares = (int)std::max<int64_t>(1, std::min<int64_t>(2048 / (cols * tiles), most));
+  p.trips = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(tiles * cols / 2048, 4), cols));
+  p.groups = ceil_div64(cols, p.trips);
+  p.tiles = p.sorted ? tiles + std::min<int64_t>(adapters + 2, m) : 0;
   p.part_bytes = (size_t)p.splits * m * p.ldt * 4;
   p.tile_bytes = p.sorted ? align_up(8 + (size_t)p.tiles * 8, 16) : 0;
   p.bytes = p.part_bytes + p.tile_bytes + (size_t)p.tiles * LQ_TILE * 4;
@@ -551,53 +596,44 @@ static LqPlan lora_requests_plan(int64_t m, int64_t k, int64_t n, int r, int64_t
 }
 // Fewer than 2^32 threads to a launch, and than 65536 rows of workgroups.
 static bool lora_requests_launches(const LqPlan& p, int64_t m, int64_t n, bool bf16) {
-  const int64_t wide = bf16 ? 128 : 64, limit = (1ll << 32) / 512;
-  if (p.sorted) {
-    const int64_t cols = ceil_div64(n, wide);
-    return 2 * p.tiles * p.splits < limit && p.tiles * cols < 2 * limit && p.tiles < (1ll << 31) / LQ_TILE;
-  }
-  const int64_t cols = ceil_div64(n, wide * LQ_UP_WAVES);
-  return ceil_div64(m, 16 * p.tb) * p.splits * p.shares < limit && cols < 65536 && ceil_div64(m, 16 * p.up_tb) * cols * p.up_shares < 2 * limit;
+  const int64_t limit = (1ll << 32) / 512;
+  if (p.sorted) return p.tiles * p.splits < 2 * limit && p.tiles * p.groups < 2 * limit && p.tiles < (1ll << 31) / LQ_TILE;
+  const int64_t cols = ceil_div64(n, (bf16 ? 128 : 64) * LQ_UP_WAVES), tiles = ceil_div64(m, 16);
+  return tiles * p.splits * p.shares < limit && cols < 65536 && tiles * cols * p.up_shares < 2 * limit;
 }
 
-template <typename T, typename O, int TB>
-static int launch_lora_up(hipStream_t s, const LqArgs& g, dim3 grid) {
-  const dim3 block(64 * LQ_UP_WAVES);
-  const int steps = (g.r + Ln<T>::STEP - 1) / Ln<T>::STEP;
-  if (steps == 1) LORACT_LAUNCH("lora_requests_up", s, (lora_up_kernel<T, O, TB, 1>), grid, block, 0, g);
-  else if (steps == 2) LORACT_LAUNCH("lora_requests_up", s, (lora_up_kernel<T, O, TB, 2>), grid, block, 0, g);
-  else if constexpr (sizeof(T) == 4) LORACT_LAUNCH("lora_requests_up", s, (lora_up_kernel<T, O, TB, 4>), grid, block, 0, g);
-  return LORACT_OK;
-}
-template <typename T, int TB, bool SORTED>
-static int launch_lora_down(hipStream_t s, const LqArgs& g, dim3 grid) {
-  const dim3 block(64 * LQ_WAVES);
-  if (g.ldt == 16) LORACT_LAUNCH("lora_requests_down", s, (lora_down_kernel<T, TB, 1, SORTED>), grid, block, 0, g);
-  else if (g.ldt == 32) LORACT_LAUNCH("lora_requests_down", s, (lora_down_kernel<T, TB, 2, SORTED>), grid, block, 0, g);
-  else LORACT_LAUNCH("lora_requests_down", s, (lora_down_kernel<T, TB, 4, SORTED>), grid, block, 0, g);
-  return LORACT_OK;
-}
 template <typename T, typename O>
 static int launch_lora_requests(hipStream_t s, LqArgs g, const LqPlan& p) {
-  g.ldt = p.ldt; g.splits = p.splits; g.k_per_split = p.k_per_split;
-  g.shares = p.shares;
+  g.ldt = p.ldt; g.splits = p.splits; g.k_per_split = p.k_per_split; g.shares = p.shares; g.trips = p.trips; g.groups = (int)p.groups;
+  const int steps = (g.r + Ln<T>::STEP - 1) / Ln<T>::STEP;
+  const dim3 up_block(64 * LQ_UP_WAVES);
+#define LQ_DOWN(KERNEL, GRID, BLOCK)                                                                 \
+  do {                                                                                               \
+    if (g.ldt == 16) LORACT_LAUNCH("lora_requests_down", s, (KERNEL<T, 1>), GRID, BLOCK, 0, g);       \
+    else if (g.ldt == 32) LORACT_LAUNCH("lora_requests_down", s, (KERNEL<T, 2>), GRID, BLOCK, 0, g);  \
+    else LORACT_LAUNCH("lora_requests_down", s, (KERNEL<T, 4>), GRID, BLOCK, 0, g);                   \
+  } while (0)
+#define LQ_UP(KERNEL, GRID)                                                                                                     \
+  do {                                                                                                                          \
+    if (steps == 1) LORACT_LAUNCH("lora_requests_up", s, (KERNEL<T, O, 1>), GRID, up_block, 0, g);                               \
+    else if (steps == 2) LORACT_LAUNCH("lora_requests_up", s, (KERNEL<T, O, 2>), GRID, up_block, 0, g);                          \
+    else if constexpr (sizeof(T) == 4) LORACT_LAUNCH("lora_requests_up", s, (KERNEL<T, O, 4>), GRID, up_block, 0, g);            \
+  } while (0)
   if (p.sorted) {
     g.tiles = (int*)((char*)g.part + p.part_bytes);
     g.order = (int*)((char*)g.tiles + p.tile_bytes);
     LORACT_LAUNCH("lora_requests_sort", s, lora_sort_kernel, dim3(1), dim3(1024), 0, g);
-    LORACT_TRY((launch_lora_down<T, 2, true>(s, g, dim3((unsigned)(2 * p.tiles), (unsigned)p.splits))));
-    const dim3 grid((unsigned)(p.tiles * ceil_div64(g.n, 16 * Ln<T>::E))), block(64 * LQ_UP_WAVES);
-    const int steps = (g.r + Ln<T>::STEP - 1) / Ln<T>::STEP;
-    if (steps == 1) LORACT_LAUNCH("lora_requests_up", s, (lora_up_sorted_kernel<T, O, 1>), grid, block, 0, g);
-    else if (steps == 2) LORACT_LAUNCH("lora_requests_up", s, (lora_up_sorted_kernel<T, O, 2>), grid, block, 0, g);
-    else if constexpr (sizeof(T) == 4) LORACT_LAUNCH("lora_requests_up", s, (lora_up_sorted_kernel<T, O, 4>), grid, block, 0, g);
+    const dim3 down((unsigned)p.tiles, (unsigned)p.splits), up((unsigned)(p.tiles * p.groups));
+    LQ_DOWN(lora_down_sorted_kernel, down, up_block);
+    LQ_UP(lora_up_sorted_kernel, up);
     return LORACT_OK;
   }
-  const dim3 down((unsigned)ceil_div64(g.m, 16 * p.tb), (unsigned)p.splits, (unsigned)p.shares);
-  if (p.tb == 2) LORACT_TRY((launch_lora_down<T, 2, false>(s, g, down)));
-  else LORACT_TRY((launch_lora_down<T, 1, false>(s, g, down)));
+  const dim3 down((unsigned)ceil_div64(g.m, 16), (unsigned)p.splits, (unsigned)p.shares);
+  LQ_DOWN(lora_down_kernel, down, dim3(64 * LQ_WAVES));
   g.shares = p.up_shares;
-  const dim3 up((unsigned)ceil_div64(g.m, 16 * p.up_tb), (unsigned)ceil_div64(g.n, 16 * Ln<T>::E * LQ_UP_WAVES), (unsigned)p.up_shares);
-  if (p.up_tb == 4) return launch_lora_up<T, O, 4>(s, g, up);
-  return launch_lora_up<T, O, 1>(s, g, up);
+  const dim3 up((unsigned)ceil_div64(g.m, 16), (unsigned)ceil_div64(g.n, 16 * Ln<T>::E * LQ_UP_WAVES), (unsigned)p.up_shares);
+  LQ_UP(lora_up_kernel, up);
+#undef LQ_DOWN
+#undef LQ_UP
+  return LORACT_OK;
 }
