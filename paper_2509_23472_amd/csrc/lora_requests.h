@@ -48,9 +48,10 @@ struct LqArgs {
 
 // Orders the tokens by adapter.  Groups: the adapters, tokens without one (none where Y is R), tokens whose adapter is not there.
 __global__ __launch_bounds__(1024) void lora_sort_kernel(LqArgs g) {
-  __shared__ int count[LQ_SORTED + 2];
+  constexpr int HELD = 8;                            // groups of a thread's first tokens that stay in registers
+  __shared__ int next[LQ_SORTED + 2], start[LQ_SORTED + 2];      // tokens counted, or placed; first tile
   __shared__ int sums[16];
-  const int tid = threadIdx.x, lane = tid & 63, groups = (int)g.adapters + 2;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, groups = (int)g.adapters + 2;
   auto group = [&](int64_t i) {
     if (i >= g.m) return -1;
     const int id = g.ids[i];
@@ -61,53 +62,80 @@ __global__ __launch_bounds__(1024) void lora_sort_kernel(LqArgs g) {
     const int d = __builtin_amdgcn_readfirstlane(mine);
     if (__all(mine == d)) {
       int at = 0;
-      if (lane == 0 && d >= 0) at = atomicAdd(&count[d], 64);
+      if (lane == 0 && d >= 0) at = atomicAdd(&next[d], 64);
       return __builtin_amdgcn_readfirstlane(at) + lane;
     }
-    return mine >= 0 ? atomicAdd(&count[mine], 1) : 0;
+    return mine >= 0 ? atomicAdd(&next[mine], 1) : 0;
   };
-  for (int i = tid; i < groups; i += 1024) count[i] = 0;
+  int held[HELD];
+#pragma unroll
+  for (int u = 0; u < HELD; ++u) held[u] = group(tid + 1024 * u);
+  for (int i = tid; i < groups; i += 1024) next[i] = 0;
   __syncthreads();
-  for (int64_t i0 = tid; i0 - tid < g.m; i0 += 4096) {         // (every lane comes as often)
-    int mine[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) mine[u] = group(i0 + 1024 * u);
+  for (int u = 0; u < HELD; ++u)
+    if (1024 * u < g.m) place(held[u]);
+  for (int64_t i = tid + 1024 * HELD; i - tid < g.m; i += 4096) {       // (every lane comes as often)
+    int more[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) place(mine[u]);
+    for (int u = 0; u < 4; ++u) more[u] = group(i + 1024 * u);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) place(more[u]);
   }
   __syncthreads();
   // first tile of every group: a thread has consecutive groups
-  const int per = (groups + 1023) / 1024, from = tid * per, to = from + per < groups ? from + per : groups;
+  const int per = (groups + 1023) / 1024, from = tid * per < groups ? tid * per : groups, to = from + per < groups ? from + per : groups;
   int mine = 0;
-  for (int i = from; i < to; ++i) mine += (count[i] + LQ_TILE - 1) / LQ_TILE;
+  for (int i = from; i < to; ++i) mine += (next[i] + LQ_TILE - 1) / LQ_TILE;
   int up_to = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const int other = __shfl_up(up_to, d);
     if (lane >= d) up_to += other;
   }
-  if (lane == 63) sums[tid >> 6] = up_to;
+  if (lane == 63) sums[wave] = up_to;
   __syncthreads();
-  int tile = up_to - mine;
-  for (int w = 0; w < (tid >> 6); ++w) tile += sums[w];
-  if (tid == 1023) g.tiles[0] = tile + mine;
+  int tile = up_to - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    const int s = sums[w];
+    tile += w < wave ? s : 0;
+    total += s;
+  }
   for (int i = from; i < to; ++i) {
-    const int n = count[i];
-    count[i] = tile * LQ_TILE;
-    for (int at = 0; at < n; at += LQ_TILE, ++tile) {
-      g.tiles[2 + 2 * tile] = i;
-      g.tiles[3 + 2 * tile] = n - at < LQ_TILE ? n - at : LQ_TILE;
-    }
+    start[i] = tile;
+    tile += (next[i] + LQ_TILE - 1) / LQ_TILE;
   }
   __syncthreads();
-  for (int64_t i0 = tid; i0 - tid < g.m; i0 += 4096) {
-    int mine4[4];
+  if (tid == 0) g.tiles[0] = total;
+  for (int t = tid; t < total; t += 1024) {          // its group: the last that begins at it or before
+    int lo = 0, hi = groups;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (start[mid] <= t) lo = mid;
+      else hi = mid;
+    }
+    const int left = next[lo] - (t - start[lo]) * LQ_TILE;
+    g.tiles[2 + 2 * t] = lo;
+    g.tiles[3 + 2 * t] = left < LQ_TILE ? left : LQ_TILE;
+  }
+  __syncthreads();
+  for (int i = tid; i < groups; i += 1024) next[i] = start[i] * LQ_TILE;
+  __syncthreads();
 #pragma unroll
-    for (int u = 0; u < 4; ++u) mine4[u] = group(i0 + 1024 * u);
+  for (int u = 0; u < HELD; ++u)
+    if (1024 * u < g.m) {
+      const int at = place(held[u]);
+      if (held[u] >= 0) g.order[at] = tid + 1024 * u;
+    }
+  for (int64_t i = tid + 1024 * HELD; i - tid < g.m; i += 4096) {
+    int more[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) more[u] = group(i + 1024 * u);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int at = place(mine4[u]);
-      if (mine4[u] >= 0) g.order[at] = (int)(i0 + 1024 * u);
+      const int at = place(more[u]);
+      if (more[u] >= 0) g.order[at] = (int)(i + 1024 * u);
     }
   }
 }
@@ -236,31 +264,37 @@ __global__ __launch_bounds__(64 * LQ_WAVES) void lora_down_kernel(LqArgs g) {
   }
 }
 
-// Ordered tokens: a tile of 64, 16 to each wave; A passes through LDS in slabs that all waves read, the next one (and the next part of X) on
-// its way while one is multiplied.
+// Ordered tokens: a tile of 64; four groups of waves share K, in each 16 tokens to a wave.  A passes through LDS in slabs that the waves of a group
+// read, the next one (and the next part of X) on its way while one is multiplied.  The groups' sums are added in LDS: parts of T that only the next
+// launch adds cost it a reading of each per 512 columns (8192 tokens, 11008 columns, rank 64: 97 us with one part, 124 with four).
+#define LQ_K_GROUPS 4
 template <typename T, int SB>
-__global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_down_sorted_kernel(LqArgs g) {
+__global__ __launch_bounds__(256 * LQ_K_GROUPS) void lora_down_sorted_kernel(LqArgs g) {
   constexpr int E = Ln<T>::E, STEP = Ln<T>::STEP, U = 4, SLAB = U * STEP, PITCH = 16 * SB * (int)sizeof(T) + (SB == 4 ? 16 : 0);
-  constexpr int PER = 16 * SB / E, TRIPS = SLAB * PER / (64 * LQ_UP_WAVES);      // pieces to a row, and of a slab to a thread
-  static_assert(SLAB * PER % (64 * LQ_UP_WAVES) == 0, "whole trips");
+  constexpr int PER = 16 * SB / E, TRIPS = SLAB * PER / 256;                     // pieces to a row, and of a slab to a thread
+  constexpr int SLABS = LQ_K_GROUPS * 2 * SLAB * PITCH, PARTS = (LQ_K_GROUPS - 1) * 4 * SB * 1024;
+  static_assert(SLAB * PER % 256 == 0, "whole trips");
   typedef typename Ln<T>::frag frag;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[2][SLAB * PITCH];
+  __shared__ __attribute__((aligned(16))) unsigned char smem[SLABS > PARTS ? SLABS : PARTS];
   const int tile = blockIdx.x;
   if (tile >= g.tiles[0]) return;
   const int d = g.tiles[2 + 2 * tile], size = g.tiles[3 + 2 * tile];
   if ((int64_t)d >= g.adapters) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane & 15, q = lane >> 4;
-  const int64_t k_beg = (int64_t)blockIdx.y * g.k_per_split, k_end = k_beg + g.k_per_split < g.k ? k_beg + g.k_per_split : g.k;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  const int tid = threadIdx.x & 255, c = lane & 15, q = lane >> 4;
+  const int64_t k_beg0 = (int64_t)blockIdx.y * g.k_per_split, k_end0 = k_beg0 + g.k_per_split < g.k ? k_beg0 + g.k_per_split : g.k;
+  const int64_t per = (g.k_per_split + LQ_K_GROUPS * SLAB - 1) / (LQ_K_GROUPS * SLAB) * SLAB;      // (as many slabs for every group)
+  const int64_t k_beg = k_beg0 + group * per, k_end = k_beg + per < k_end0 ? k_beg + per : k_end0;
   const bool work = 16 * wave < size, live = 16 * wave + c < size;
   const int64_t token = g.order[tile * LQ_TILE + (live ? 16 * wave + c : 0)];
   const T* const x = (const T*)g.X + token * g.ldx;
   const T* const a = (const T*)g.A + (int64_t)d * g.k * g.r;
+  unsigned char* const slabs = smem + group * (2 * SLAB * PITCH);
   frag xs[U], as[TRIPS];
   auto load = [&](int64_t k0) {
 #pragma unroll
     for (int i = 0; i < TRIPS; ++i) {
-      const int at = threadIdx.x + i * (64 * LQ_UP_WAVES);
+      const int at = tid + i * 256;
       as[i] = lq_piece<T>(g, a, k0 + at / PER, k_end, E * (at % PER));
     }
     if (work) {
@@ -273,27 +307,38 @@ __global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_down_sorted_kernel(LqAr
   for (int s = 0; s < SB; ++s) acc[s] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
   load(k_beg);
   int turn = 0;
-  for (int64_t k0 = k_beg; k0 < k_end; k0 += SLAB, turn ^= 1) {
+  for (int64_t at_k = 0; at_k < per; at_k += SLAB, turn ^= 1) {
+    unsigned char* const slab = slabs + turn * (SLAB * PITCH);
     frag now[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) now[u] = xs[u];
 #pragma unroll
     for (int i = 0; i < TRIPS; ++i) {
-      const int at = threadIdx.x + i * (64 * LQ_UP_WAVES);
-      *(frag*)(smem[turn] + at / PER * PITCH + at % PER * 16) = as[i];
+      const int at = tid + i * 256;
+      *(frag*)(slab + at / PER * PITCH + at % PER * 16) = as[i];
     }
-    if (k0 + SLAB < k_end) load(k0 + SLAB);
+    if (at_k + SLAB < per) load(k_beg + at_k + SLAB);
     sb_barrier_lds();                                // (two slabs: who writes one has passed the barrier behind its last reading)
     if (work) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int s = 0; s < SB; ++s) acc[s] = ln_mfma(lq_turned<T>(smem[turn] + STEP * u * PITCH + 16 * s * (int)sizeof(T), PITCH, c, q), now[u], acc[s]);
+        for (int s = 0; s < SB; ++s) acc[s] = ln_mfma(lq_turned<T>(slab + STEP * u * PITCH + 16 * s * (int)sizeof(T), PITCH, c, q), now[u], acc[s]);
     }
   }
-  if (live) {
+  __syncthreads();
+  f32x4* const part = (f32x4*)smem;
+  if (group) {
 #pragma unroll
-    for (int s = 0; s < SB; ++s) *(f32x4*)(g.part + ((int64_t)blockIdx.y * g.m + token) * g.ldt + 16 * s + 4 * q) = acc[s];
+    for (int s = 0; s < SB; ++s) part[((group - 1) * 4 + wave) * (SB * 64) + s * 64 + lane] = acc[s];
+  }
+  __syncthreads();
+  if (group || !live) return;
+#pragma unroll
+  for (int s = 0; s < SB; ++s) {
+#pragma unroll
+    for (int h = 1; h < LQ_K_GROUPS; ++h) acc[s] += part[((h - 1) * 4 + wave) * (SB * 64) + s * 64 + lane];
+    *(f32x4*)(g.part + ((int64_t)blockIdx.y * g.m + token) * g.ldt + 16 * s + 4 * q) = acc[s];
   }
 }
 
@@ -579,10 +624,10 @@ static LqPlan lora_requests_plan(int64_t m, int64_t k, int64_t n, int r, int64_t
   p.sorted = m > 64 && adapters <= LQ_SORTED;
   p.ldt = r <= 16 ? 16 : (r <= 32 ? 32 : 64);
   const int64_t cols = ceil_div64(n, 16 * e), most = std::min<int64_t>(16, adapters);
-  // K splits: 512 workgroups, of a slab (all waves together a step) at least
-  const int64_t tiles = ceil_div64(m, p.sorted ? LQ_TILE : 16), step = (p.sorted ? 16 : 4 * LQ_WAVES) * e;
+  // K splits: 512 workgroups (256 of ordered tokens), of a slab (a step) for each group (wave) at least
+  const int64_t tiles = ceil_div64(m, p.sorted ? LQ_TILE : 16), step = (p.sorted ? 16 * LQ_K_GROUPS : 4 * LQ_WAVES) * e;
   p.shares = p.sorted ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, most));
-  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / (tiles * p.shares), ceil_div64(k, step)), 16));
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((p.sorted ? 256 : 512) / (tiles * p.shares), ceil_div64(k, step)), 16));
   p.k_per_split = ceil_div64(ceil_div64(k, splits), step) * step;
   p.splits = (int)ceil_div64(k, p.k_per_split);
   p.up_shares = (int)std::max<int64_t>(1, std::min<int64_t>(2048 / (cols * tiles), most));
@@ -597,7 +642,7 @@ static LqPlan lora_requests_plan(int64_t m, int64_t k, int64_t n, int r, int64_t
 // Fewer than 2^32 threads to a launch, and than 65536 rows of workgroups.
 static bool lora_requests_launches(const LqPlan& p, int64_t m, int64_t n, bool bf16) {
   const int64_t limit = (1ll << 32) / 512;
-  if (p.sorted) return p.tiles * p.splits < 2 * limit && p.tiles * p.groups < 2 * limit && p.tiles < (1ll << 31) / LQ_TILE;
+  if (p.sorted) return p.tiles * p.splits < limit / LQ_K_GROUPS * 2 && p.tiles * p.groups < 2 * limit && p.tiles < (1ll << 31) / LQ_TILE;
   const int64_t cols = ceil_div64(n, (bf16 ? 128 : 64) * LQ_UP_WAVES), tiles = ceil_div64(m, 16);
   return tiles * p.splits * p.shares < limit && cols < 65536 && tiles * cols * p.up_shares < 2 * limit;
 }
@@ -624,7 +669,7 @@ static int launch_lora_requests(hipStream_t s, LqArgs g, const LqPlan& p) {
     g.order = (int*)((char*)g.tiles + p.tile_bytes);
     LORACT_LAUNCH("lora_requests_sort", s, lora_sort_kernel, dim3(1), dim3(1024), 0, g);
     const dim3 down((unsigned)p.tiles, (unsigned)p.splits), up((unsigned)(p.tiles * p.groups));
-    LQ_DOWN(lora_down_sorted_kernel, down, up_block);
+    LQ_DOWN(lora_down_sorted_kernel, down, dim3(256 * LQ_K_GROUPS));
     LQ_UP(lora_up_sorted_kernel, up);
     return LORACT_OK;
   }
