@@ -26,11 +26,13 @@
 
 #define LP_THREADS 256
 #define LP_CANDIDATES 1024
+#define LP_HELD 4
 #define LP_SPLITS 64
 
 struct LpArgs {
   const void* x;
   int64_t ld, m, n;
+  int64_t row0;          // of a launch
   const void* targets;   // int32 or int64, or null
   int target_64;
   float inv_t, c;        // 1 / T, 1 / (T ln 2)
@@ -53,23 +55,19 @@ struct LpSum {
 __device__ inline LpSum lp_none() { return {-FLT_MAX, 0.0f, 0.0f}; }
 #define LP_LN2 0.693147181f
 __device__ inline float lp_cut(float u) { return fmaxf(u, -300.0f); }
-// (Each operation is rounded by itself: a fused one would take its two sides differently, and the lanes of a butterfly would differ.)
 __device__ inline LpSum lp_moved(const LpSum& a, float m, float c) {
-#pragma clang fp contract(off)
   const float d = lp_cut((a.m - m) * c), f = __builtin_amdgcn_exp2f(d);
   return {m, a.s * f, (a.w + d * a.s) * f};
 }
-__device__ inline LpSum lp_merge(const LpSum& a, const LpSum& b, float c) {
-#pragma clang fp contract(off)
-  const float m = fmaxf(a.m, b.m);
-  const LpSum x = lp_moved(a, m, c), y = lp_moved(b, m, c);
-  return {m, x.s + y.s, x.w + y.w};
-}
 __device__ inline LpSum lp_wave_merge(LpSum a, float c) {
+  float m = a.m;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+  a = lp_moved(a, m, c);
 #pragma unroll
   for (int d = 32; d; d >>= 1) {
-    const LpSum b = {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.w, d)};
-    a = lp_merge(a, b, c);
+    a.s += __shfl_xor(a.s, d);
+    a.w += __shfl_xor(a.w, d);
   }
   return a;
 }
@@ -95,9 +93,9 @@ __device__ inline void lp_finish(const LpArgs& g, int64_t row, const LpSum& a, f
 }
 
 // Order of elements: larger values first, then lower indices; what is no number counts as -inf, and both zeros as one.
-__device__ inline uint64_t lp_key(float x, int64_t col) {
+__device__ inline uint64_t lp_key(float x, int col) {
   const unsigned b = x != x ? 0xff800000u : __float_as_uint(x + 0.0f);
-  return (uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (uint32_t)~(uint32_t)col;
+  return (uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | ~(uint32_t)col;
 }
 __device__ inline float lp_value(uint64_t key) {
   const unsigned b = (unsigned)(key >> 32);
@@ -117,53 +115,75 @@ __device__ inline int64_t lp_head(const T* at, int64_t n) {
   const int64_t head = (int64_t)((16 - ((uintptr_t)at & 15)) & 15) / (int64_t)sizeof(T);
   return head < n ? head : n;
 }
-// Calls f(values, column, how many) for the elements [c0, c1) of a row: whole pieces, then for thread i < 2 E one of the few around them.
-template <typename T, int U, typename F>
-__device__ inline void lp_each(const T* row, int64_t c0, int64_t c1, F f) {
+// Where the elements [c0, c1) of a row lie for a thread: whole pieces, then for thread i < 2 E one of the few around them (lone, -1: none).
+// (Columns are 32 bits: a row has 2^30 at most.)
+struct LpRun {
+  int first, pieces, lone;
+};
+template <typename T>
+__device__ inline LpRun lp_run(const T* row, int c0, int c1) {
   constexpr int E = LpPiece<T>::E;
-  const int64_t head = lp_head(row + c0, c1 - c0), first = c0 + head, pieces = (c1 - first) / E;
-  for (int64_t v = threadIdx.x; v < pieces; v += LP_THREADS * U) {
-    typename LpPiece<T>::vec raw[U];
+  const int head = (int)lp_head(row + c0, c1 - c0), first = c0 + head, pieces = (c1 - first) / E, tail = c1 - first - pieces * E;
+  const int i = threadIdx.x;
+  return {first, pieces, i < head ? c0 + i : (i >= E && i < E + tail ? first + pieces * E + i - E : -1)};
+}
+template <typename T, int U, int THREADS>
+__device__ inline void lp_fetch(const T* row, const LpRun& r, int v, typename LpPiece<T>::vec (&raw)[U]) {
+  const T* const first = row + r.first;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t at = v + u * LP_THREADS;
-      raw[u] = *(const typename LpPiece<T>::vec*)(row + first + (at < pieces ? at : v) * E);
-    }
+  for (int u = 0; u < U; ++u)
+    if (v + u * THREADS < r.pieces) raw[u] = *(const typename LpPiece<T>::vec*)(first + (unsigned)(v + u * THREADS) * LpPiece<T>::E);
+}
+// Calls f(values, column, how many) for pieces that are there.
+template <typename T, int U, int THREADS, typename F>
+__device__ inline void lp_visit(const LpRun& r, int v, const typename LpPiece<T>::vec (&raw)[U], F f) {
+  constexpr int E = LpPiece<T>::E;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float x[E];
+  for (int u = 0; u < U; ++u) {
+    if (v + u * THREADS >= r.pieces) continue;
+    float x[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = (float)raw[u][e];
-      if (v + u * LP_THREADS < pieces) f(x, first + (v + u * LP_THREADS) * E, E);
-    }
+    for (int e = 0; e < E; ++e) x[e] = (float)raw[u][e];
+    f(x, r.first + (v + u * THREADS) * E, E);
   }
-  const int64_t tail = c1 - first - pieces * E, i = threadIdx.x;
-  const int64_t col = i < head ? c0 + i : (i >= E && i < E + tail ? first + pieces * E + i - E : -1);
-  if (col < 0) return;
+}
+template <typename T, typename F>
+__device__ inline void lp_alone(const LpRun& r, float value, F f) {
+  constexpr int E = LpPiece<T>::E;
+  if (r.lone < 0) return;
   float x[E];
-  x[0] = (float)row[col];
+  x[0] = value;
 #pragma unroll
   for (int e = 1; e < E; ++e) x[e] = -__builtin_inff();
-  f(x, col, 1);
+  f(x, r.lone, 1);
 }
-
+// Calls f for all of a run, U pieces in flight.
+template <typename T, int U, int THREADS, typename F>
+__device__ inline void lp_each(const T* row, int c0, int c1, F f) {
+  const LpRun r = lp_run(row, c0, c1);
+  for (int v = threadIdx.x; v < r.pieces; v += THREADS * U) {
+    typename LpPiece<T>::vec raw[U];
+    lp_fetch<T, U, THREADS>(row, r, v, raw);
+    lp_visit<T, U, THREADS>(r, v, raw, f);
+  }
+  lp_alone<T>(r, r.lone < 0 ? 0.0f : (float)row[r.lone], f);
+}
 // Fills the elements [c0, c1) of a row.
 template <typename T>
-__device__ inline void lp_fill(T* row, int64_t c0, int64_t c1, T value) {
+__device__ inline void lp_fill(T* row, int c0, int c1, T value) {
   constexpr int E = LpPiece<T>::E;
-  const int64_t head = lp_head(row + c0, c1 - c0), first = c0 + head, pieces = (c1 - first) / E, tail = c1 - first - pieces * E;
+  const LpRun r = lp_run(row, c0, c1);
   typename LpPiece<T>::vec all;
 #pragma unroll
   for (int e = 0; e < E; ++e) all[e] = value;
-  for (int64_t v = threadIdx.x; v < pieces; v += LP_THREADS) *(typename LpPiece<T>::vec*)(row + first + v * E) = all;
-  if (threadIdx.x < head) row[c0 + threadIdx.x] = value;
-  if (threadIdx.x < tail) row[first + pieces * E + threadIdx.x] = value;
+  for (int v = threadIdx.x; v < r.pieces; v += LP_THREADS) *(typename LpPiece<T>::vec*)(row + r.first + (unsigned)v * E) = all;
+  if (r.lone >= 0) row[r.lone] = value;
 }
 
 // Ranks the `count` candidates in LDS (all different, count at most LP_CANDIDATES): rank r < k goes to out(r, key).
-template <typename F>
+template <int THREADS, typename F>
 __device__ inline void lp_rank(const uint64_t* cand, int count, int k, F out) {
-  for (int i = threadIdx.x; i < count; i += LP_THREADS) {
+  for (int i = threadIdx.x; i < count; i += THREADS) {
     const uint64_t mine = cand[i];
     int above = 0;
 #pragma unroll 16
@@ -172,120 +192,145 @@ __device__ inline void lp_rank(const uint64_t* cand, int count, int k, F out) {
   }
 }
 
-template <typename T, bool TOP>
-__global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LpArgs g) {
-  constexpr int E = LpPiece<T>::E, WAVES = LP_THREADS / 64;
+// HELD: a workgroup's columns stay in registers (LP_HELD pieces of a thread) between the passes.
+template <typename T, int THREADS, bool TOP, bool HELD>
+__global__ __launch_bounds__(THREADS) void logprob_kernel(LpArgs g) {
+  constexpr int E = LpPiece<T>::E, WAVES = THREADS / 64;
   __shared__ LpSum sums[WAVES];
-  __shared__ uint64_t best_of[TOP ? LP_THREADS : 1], cand[TOP ? LP_CANDIDATES : 1], bound;
+  __shared__ uint64_t best_of[TOP ? THREADS : 1], cand[TOP ? LP_CANDIDATES : 1], bound;
   __shared__ int found;
   const int tid = threadIdx.x, split = blockIdx.y;
-  const int64_t c0 = split * g.chunk, c1 = c0 + g.chunk < g.n ? c0 + g.chunk : g.n;
-  for (int64_t row = blockIdx.x; row < g.m; row += gridDim.x) {
-    const T* const x = (const T*)g.x + row * g.ld;
-    LpSum a = lp_none();
-    float best = -__builtin_inff();
-    int64_t best_col = -1;
-    lp_each<T, 4>(x, c0, c1, [&](const float (&v)[E], int64_t col, int count) {
+  const int n = (int)g.n, chunk = (int)g.chunk, c0 = split * chunk, c1 = n - c0 < chunk ? n : c0 + chunk;
+  const int64_t row = g.row0 + blockIdx.x;
+  const T* const x = (const T*)g.x + row * g.ld;
+  LpRun run;
+  typename LpPiece<T>::vec raw[HELD ? LP_HELD : 1];
+  float alone = 0.0f;
+  if constexpr (HELD) {
+    run = lp_run(x, c0, c1);
+    lp_fetch<T, LP_HELD, THREADS>(x, run, tid, raw);
+    if (run.lone >= 0) alone = (float)x[run.lone];
+  }
+  auto each = [&](auto f) {
+    if constexpr (HELD) {
+      lp_visit<T, LP_HELD, THREADS>(run, tid, raw, f);
+      lp_alone<T>(run, alone, f);
+    } else {
+      lp_each<T, 4, THREADS>(x, c0, c1, f);
+    }
+  };
+  LpSum a = lp_none();
+  float best = -__builtin_inff();
+  int best_col = -1;
+  each([&](const float (&v)[E], int col, int count) {
+    float top = v[0];
+#pragma unroll
+    for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
+    if (top > a.m) a = lp_moved(a, top, g.c);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (e >= count) break;
+      const float u = (v[e] - a.m) * g.c, p = __builtin_amdgcn_exp2f(u);
+      a.s += p;
+      a.w = fmaf(lp_cut(u), p, a.w);
+    }
+    if (TOP && (best_col < 0 || top > best)) {
+      best = top > best ? top : best;
+      int at = 0;
+#pragma unroll
+      for (int e = E - 1; e >= 0; --e)
+        if (v[e] == best) at = e;
+      best_col = col + (best == -__builtin_inff() ? 0 : at);
+    }
+  });
+  a = lp_wave_merge(a, g.c);
+  if ((tid & 63) == 0) sums[tid >> 6] = a;
+  if (TOP) best_of[tid] = best_col < 0 ? 0 : lp_key(best, best_col);
+  if (TOP && tid == 0) { bound = 0; found = 0; }
+  __syncthreads();
+  a = (tid & 63) < WAVES ? sums[tid & 63] : lp_none();
+  a = lp_wave_merge(a, g.c);
+  const float log_s = lp_log_sum(a.s);
+  if (tid == 0) {
+    if (g.splits == 1) lp_finish<T>(g, row, a, log_s);
+    else *(f32x4*)(g.part + (row * g.splits + split) * 4) = (f32x4){a.m, a.s, a.w, 0.0f};
+  }
+  if constexpr (TOP) {
+    // The bound, found by one wave, or four: of the maxima of 256 groups of threads, or of 64 where that will do.
+    const int groups = g.top <= 32 ? 64 : 256;
+    uint64_t mine = best_of[tid];
+    int above = 0;
+    if (tid < groups) {
+      for (int i = tid + groups; i < THREADS; i += groups) mine = best_of[i] > mine ? best_of[i] : mine;
+      cand[tid] = mine;
+    }
+    if (groups > 64) __syncthreads();
+    else sb_wave_sync();
+    if (tid < groups) {
+#pragma unroll 16
+      for (int i = 0; i < groups; ++i) above += cand[i] > mine;
+      if (above == g.top - 1 && mine) bound = mine;        // (all different but for groups without elements)
+    }
+    __syncthreads();
+    const uint64_t least = bound;
+    const float least_value = least ? lp_value(least) : -__builtin_inff();
+    each([&](const float (&v)[E], int col, int count) {
       float top = v[0];
 #pragma unroll
       for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
-      if (top > a.m) a = lp_moved(a, top, g.c);
+      if (top < least_value) return;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         if (e >= count) break;
-        const float u = (v[e] - a.m) * g.c, p = __builtin_amdgcn_exp2f(u);
-        a.s += p;
-        a.w = fmaf(lp_cut(u), p, a.w);
-      }
-      if (TOP && (best_col < 0 || top > best)) {
-        best = top > best ? top : best;
-        int at = 0;
-#pragma unroll
-        for (int e = E - 1; e >= 0; --e)
-          if (v[e] == best) at = e;
-        best_col = col + (best == -__builtin_inff() ? 0 : at);
+        if (v[e] < least_value) continue;          // (passed by most waves as a whole)
+        const uint64_t key = lp_key(v[e], col + e);
+        if (key >= least) {
+          const int at = atomicAdd(&found, 1);
+          if (at < LP_CANDIDATES) cand[at] = key;
+        }
       }
     });
-    a = lp_wave_merge(a, g.c);
-    if ((tid & 63) == 0) sums[tid >> 6] = a;
-    if (TOP) best_of[tid] = best_col < 0 ? 0 : lp_key(best, best_col);
-    if (TOP && tid == 0) { bound = 0; found = 0; }
     __syncthreads();
-    a = sums[0];
+    const int count = found;
+    auto put = [&](int r, uint64_t key) {
+      if (g.splits > 1) {
+        g.part_top[(row * g.splits + split) * g.top + r] = key;
+      } else {
+        g.top_ids[row * g.top + r] = lp_index(key);
+        g.top_logp[row * g.top + r] = lp_log(g, lp_value(key), a, log_s);
+      }
+    };
+    if (count <= LP_CANDIDATES) {
+      lp_rank<THREADS>(cand, count, g.top, put);
+      if (g.splits > 1)
+        for (int r = count + tid; r < g.top; r += THREADS) put(r, 0);
+    } else {                                       // one by one, each below the one before
+      uint64_t last = ~0ull;
+      for (int r = 0; r < g.top; ++r) {
+        uint64_t next = 0;
+        lp_each<T, 1, THREADS>(x, c0, c1, [&](const float (&v)[E], int col, int cnt) {
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) a = lp_merge(a, sums[w], g.c);
-    const float log_s = lp_log_sum(a.s);
-    if (tid == 0) {
-      if (g.splits == 1) lp_finish<T>(g, row, a, log_s);
-      else *(f32x4*)(g.part + (row * g.splits + split) * 4) = (f32x4){a.m, a.s, a.w, 0.0f};
-    }
-    if constexpr (TOP) {
-      const uint64_t mine = best_of[tid];
-      int above = 0;
-#pragma unroll 16
-      for (int i = 0; i < LP_THREADS; ++i) above += best_of[i] > mine;
-      if (above == g.top - 1 && mine) bound = mine;        // (all different but for threads without elements)
-      __syncthreads();
-      const uint64_t least = bound;
-      const float least_value = least ? lp_value(least) : -__builtin_inff();
-      lp_each<T, 4>(x, c0, c1, [&](const float (&v)[E], int64_t col, int count) {
-        float top = v[0];
-#pragma unroll
-        for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
-        if (top < least_value) return;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          if (e >= count) break;
-          const uint64_t key = lp_key(v[e], col + e);
-          if (key >= least) {
-            const int at = atomicAdd(&found, 1);
-            if (at < LP_CANDIDATES) cand[at] = key;
+          for (int e = 0; e < E; ++e) {
+            if (e >= cnt) break;
+            const uint64_t key = lp_key(v[e], col + e);
+            if (key < last && key > next) next = key;
           }
-        }
-      });
-      __syncthreads();
-      const int count = found;
-      auto put = [&](int r, uint64_t key) {
-        if (g.splits > 1) {
-          g.part_top[(row * g.splits + split) * g.top + r] = key;
-        } else {
-          g.top_ids[row * g.top + r] = lp_index(key);
-          g.top_logp[row * g.top + r] = lp_log(g, lp_value(key), a, log_s);
-        }
-      };
-      if (count <= LP_CANDIDATES) {
-        lp_rank(cand, count, g.top, put);
-        if (g.splits > 1)
-          for (int r = count + tid; r < g.top; r += LP_THREADS) put(r, 0);
-      } else {                                       // one by one, each below the one before
-        uint64_t last = ~0ull;
-        for (int r = 0; r < g.top; ++r) {
-          uint64_t next = 0;
-          lp_each<T, 4>(x, c0, c1, [&](const float (&v)[E], int64_t col, int cnt) {
+        });
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-              if (e >= cnt) break;
-              const uint64_t key = lp_key(v[e], col + e);
-              if (key < last && key > next) next = key;
-            }
-          });
-#pragma unroll
-          for (int d = 32; d; d >>= 1) {
-            const uint64_t other = __shfl_xor((unsigned long long)next, d);
-            next = other > next ? other : next;
-          }
-          __syncthreads();
-          if ((tid & 63) == 0) best_of[tid >> 6] = next;
-          __syncthreads();
-          last = best_of[0];
-#pragma unroll
-          for (int w = 1; w < WAVES; ++w) last = best_of[w] > last ? best_of[w] : last;
-          if (tid == 0) put(r, last);
+        for (int d = 32; d; d >>= 1) {
+          const uint64_t other = __shfl_xor((unsigned long long)next, d);
+          next = other > next ? other : next;
         }
+        __syncthreads();
+        if ((tid & 63) == 0) best_of[tid >> 6] = next;
+        __syncthreads();
+        last = best_of[0];
+        for (int w = 1; w < WAVES; ++w) last = best_of[w] > last ? best_of[w] : last;
+        if (tid == 0) put(r, last);
       }
     }
-    __syncthreads();
   }
+  __syncthreads();
 }
 
 // Joins the parts of split rows: their sums in a fixed tree, and the ranks of the candidates among those that are not below a bound of the k-th
@@ -295,42 +340,41 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LpArgs g) {
   extern __shared__ uint64_t cand[];                 // splits x top
   __shared__ int found;
   const int tid = threadIdx.x, lane = tid & 63, total = g.splits * g.top;
-  for (int64_t row = blockIdx.x; row < g.m; row += gridDim.x) {
-    const uint64_t* const lists = g.part_top + row * total;
-    LpSum a = lp_none();
-    uint64_t last = 0, early = ~0ull;
-    if (lane < g.splits) {
-      const f32x4 p = *(const f32x4*)(g.part + (row * g.splits + lane) * 4);
-      if (g.top) {
-        last = lists[lane * g.top + g.top - 1];
-        early = lists[lane * g.top + (g.top - 1) / g.splits];
-      }
-      a = {p[0], p[1], p[2]};
-    }
-    a = lp_wave_merge(a, g.c);
-    const float log_s = lp_log_sum(a.s);
-    if (tid == 0) lp_finish<T>(g, row, a, log_s);
+  const int64_t row = g.row0 + blockIdx.x;
+  const uint64_t* const lists = g.part_top + row * total;
+  LpSum a = lp_none();
+  uint64_t last = 0, early = ~0ull;
+  if (lane < g.splits) {
+    const f32x4 p = *(const f32x4*)(g.part + (row * g.splits + lane) * 4);
     if (g.top) {
-#pragma unroll
-      for (int d = 32; d; d >>= 1) {
-        const uint64_t l = __shfl_xor((unsigned long long)last, d), e = __shfl_xor((unsigned long long)early, d);
-        last = l > last ? l : last;
-        early = e < early ? e : early;
-      }
-      const uint64_t least = last > early ? last : early;
-      if (tid == 0) found = 0;
-      __syncthreads();
-      for (int i = tid; i < total; i += LP_THREADS) {
-        const uint64_t key = lists[i];
-        if (key && key >= least) cand[atomicAdd(&found, 1)] = key;
-      }
-      __syncthreads();
-      lp_rank(cand, found, g.top, [&](int r, uint64_t key) {
-        g.top_ids[row * g.top + r] = lp_index(key);
-        g.top_logp[row * g.top + r] = lp_log(g, lp_value(key), a, log_s);
-      });
-      __syncthreads();
+      last = lists[lane * g.top + g.top - 1];
+      early = lists[lane * g.top + (g.top - 1) / g.splits];
     }
+    a = {p[0], p[1], p[2]};
+  }
+  a = lp_wave_merge(a, g.c);
+  const float log_s = lp_log_sum(a.s);
+  if (tid == 0) lp_finish<T>(g, row, a, log_s);
+  if (g.top) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+      const uint64_t l = __shfl_xor((unsigned long long)last, d), e = __shfl_xor((unsigned long long)early, d);
+      last = l > last ? l : last;
+      early = e < early ? e : early;
+    }
+    const uint64_t least = last > early ? last : early;
+    if (tid == 0) found = 0;
+    __syncthreads();
+    for (int i = tid; i < total; i += LP_THREADS) {
+      const uint64_t key = lists[i];
+      if (key && key >= least) cand[atomicAdd(&found, 1)] = key;
+    }
+    __syncthreads();
+    lp_rank<LP_THREADS>(cand, found, g.top, [&](int r, uint64_t key) {
+      g.top_ids[row * g.top + r] = lp_index(key);
+      g.top_logp[row * g.top + r] = lp_log(g, lp_value(key), a, log_s);
+    });
+    __syncthreads();
   }
 }
 
@@ -361,37 +405,36 @@ __device__ inline float lp_slope(const LpRow& r, float u, float p) { return ENTR
 template <typename T, bool ENTROPY>
 __global__ __launch_bounds__(LP_THREADS) void logprob_backward_kernel(LpArgs g) {
   constexpr int E = LpPiece<T>::E;
-  const int64_t c0 = blockIdx.y * g.chunk, c1 = c0 + g.chunk < g.n ? c0 + g.chunk : g.n;
-  for (int64_t row = blockIdx.x; row < g.m; row += gridDim.x) {
-    const float m = g.stats[row], log_s = g.stats[g.m + row];
-    const LpRow r = lp_row(g, row, m, m == -__builtin_inff() ? 0.0f : exp2f(log_s), log_s, g.stats[2 * g.m + row]);
-    const T* const x = (const T*)g.x + row * g.ld;
-    T* const y = (T*)g.grad + row * g.ldg;
-    if (r.zero || r.bad) {
-      const T fill = (T)(r.bad ? __builtin_nanf("") : 0.0f);
-      lp_fill(y, c0, c1, fill);
-      continue;
-    }
-    lp_each<T, 4>(x, c0, c1, [&](const float (&v)[E], int64_t col, int count) {
-      typename LpPiece<T>::vec out;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if (e >= count) break;
-        const float u = (v[e] - r.m) * g.c;
-        out[e] = (T)lp_slope<ENTROPY>(r, u, __builtin_amdgcn_exp2f(u));
-      }
-      if (r.target >= col && r.target < col + count) {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (col + e == r.target) {
-            const float u = (v[e] - r.m) * g.c;
-            out[e] = (T)(r.g + lp_slope<ENTROPY>(r, u, __builtin_amdgcn_exp2f(u)));
-          }
-      }
-      if (count == E) *(typename LpPiece<T>::any*)(y + col) = out;
-      else y[col] = out[0];
-    });
+  const int n = (int)g.n, chunk = (int)g.chunk, c0 = (int)blockIdx.y * chunk, c1 = n - c0 < chunk ? n : c0 + chunk;
+  const int64_t row = g.row0 + blockIdx.x;
+  const float m = g.stats[row], log_s = g.stats[g.m + row];
+  const LpRow r = lp_row(g, row, m, m == -__builtin_inff() ? 0.0f : exp2f(log_s), log_s, g.stats[2 * g.m + row]);
+  const T* const x = (const T*)g.x + row * g.ld;
+  T* const y = (T*)g.grad + row * g.ldg;
+  if (r.zero || r.bad) {
+    const T fill = (T)(r.bad ? __builtin_nanf("") : 0.0f);
+    lp_fill(y, c0, c1, fill);
+    return;
   }
+  lp_each<T, 4, LP_THREADS>(x, c0, c1, [&](const float (&v)[E], int col, int count) {
+    typename LpPiece<T>::vec out;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (e >= count) break;
+      const float u = (v[e] - r.m) * g.c;
+      out[e] = (T)lp_slope<ENTROPY>(r, u, __builtin_amdgcn_exp2f(u));
+    }
+    if (r.target >= col && r.target < col + count) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (col + e == r.target) {
+          const float u = (v[e] - r.m) * g.c;
+          out[e] = (T)(r.g + lp_slope<ENTROPY>(r, u, __builtin_amdgcn_exp2f(u)));
+        }
+    }
+    if (count == E) *(typename LpPiece<T>::any*)(y + col) = out;
+    else y[col] = out[0];
+  });
 }
 
 // Both in one call: a row stays in the registers of a workgroup between the sums and the gradient.  V pieces per thread.  The exponentials are formed
@@ -402,132 +445,145 @@ __global__ __launch_bounds__(THREADS, V < 8 || THREADS * V == 8192 ? 8 : (V == 8
   __shared__ float tops[WAVES];
   __shared__ float sums[2][WAVES];
   const int tid = threadIdx.x;
-  for (int64_t row = blockIdx.x; row < g.m; row += gridDim.x) {
-    const T* const x = (const T*)g.x + row * g.ld;
-    const int n = (int)g.n, head = (int)lp_head(x, g.n), pieces = (n - head) / E, tail = n - head - pieces * E;      // (rows in registers are short)
-    const T* const body = x + head;
-    typename LpPiece<T>::vec raw[V];
+  const int64_t row = g.row0 + blockIdx.x;
+  const T* const x = (const T*)g.x + row * g.ld;
+  const int n = (int)g.n, head = (int)lp_head(x, g.n), pieces = (n - head) / E, tail = n - head - pieces * E;      // (rows in registers are short)
+  const T* const body = x + head;
+  typename LpPiece<T>::vec raw[V];
 #pragma unroll
-    for (int u = 0; u < V; ++u) {
-      const int at = tid + u * THREADS;
-      if (at < pieces) raw[u] = *(const typename LpPiece<T>::vec*)(body + (unsigned)at * E);
+  for (int u = 0; u < V; ++u) {
+    const int at = tid + u * THREADS;
+    if (at < pieces) raw[u] = *(const typename LpPiece<T>::vec*)(body + (unsigned)at * E);
+  }
+  const int lone = tid < head ? tid : (tid >= E && tid < E + tail ? head + pieces * E + tid - E : -1);
+  const float alone = lone >= 0 ? (float)x[lone] : -__builtin_inff();
+  float top = alone;
+#pragma unroll
+  for (int u = 0; u < V; ++u)
+    if (tid + u * THREADS < pieces) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) top = fmaxf(top, (float)raw[u][e]);
     }
-    const int lone = tid < head ? tid : (tid >= E && tid < E + tail ? head + pieces * E + tid - E : -1);
-    const float alone = lone >= 0 ? (float)x[lone] : -__builtin_inff();
-    float top = alone;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if ((tid & 63) == 0) tops[tid >> 6] = top;
+  __syncthreads();
+  top = tops[0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) top = fmaxf(top, tops[w]);
+  LpSum a = {fmaxf(top, -FLT_MAX), 0.0f, 0.0f};
+  auto add = [&](float v) {
+    const float u = (v - a.m) * g.c, p = __builtin_amdgcn_exp2f(u);
+    a.s += p;
+    a.w = fmaf(lp_cut(u), p, a.w);
+  };
+  if (lone >= 0) add(alone);
+#pragma unroll
+  for (int u = 0; u < V; ++u)
+    if (tid + u * THREADS < pieces) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) add((float)raw[u][e]);
+    }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    a.s += __shfl_xor(a.s, d);
+    a.w += __shfl_xor(a.w, d);
+  }
+  if ((tid & 63) == 0) { sums[0][tid >> 6] = a.s; sums[1][tid >> 6] = a.w; }
+  __syncthreads();
+  a.s = sums[0][0];
+  a.w = sums[1][0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) { a.s += sums[0][w]; a.w += sums[1][w]; }
+  const float log_s = lp_log_sum(a.s);
+  const LpRow r = lp_row(g, row, a.m, a.s, log_s, lp_entropy(a, log_s));
+  if (tid == 0) lp_finish<T>(g, row, a, log_s);
+  const float asked = r.g != 0.0f && !r.bad && r.target >= 0 ? (float)x[r.target] : 0.0f;
+  __syncthreads();                                 // (the target's logit is read before the gradient may take its place)
+  T* const y = (T*)g.grad + row * g.ldg;
+  if (r.zero || r.bad) {
+    const T fill = (T)(r.bad ? __builtin_nanf("") : 0.0f);
+    if (lone >= 0) y[lone] = fill;
 #pragma unroll
     for (int u = 0; u < V; ++u)
       if (tid + u * THREADS < pieces) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) top = fmaxf(top, (float)raw[u][e]);
-      }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if ((tid & 63) == 0) tops[tid >> 6] = top;
-    __syncthreads();
-    top = tops[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, tops[w]);
-    LpSum a = {fmaxf(top, -FLT_MAX), 0.0f, 0.0f};
-    auto add = [&](float v) {
-      const float u = (v - a.m) * g.c, p = __builtin_amdgcn_exp2f(u);
-      a.s += p;
-      a.w = fmaf(lp_cut(u), p, a.w);
-    };
-    if (lone >= 0) add(alone);
-#pragma unroll
-    for (int u = 0; u < V; ++u)
-      if (tid + u * THREADS < pieces) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) add((float)raw[u][e]);
-      }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-      a.s += __shfl_xor(a.s, d);
-      a.w += __shfl_xor(a.w, d);
-    }
-    if ((tid & 63) == 0) { sums[0][tid >> 6] = a.s; sums[1][tid >> 6] = a.w; }
-    __syncthreads();
-    a.s = sums[0][0];
-    a.w = sums[1][0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) { a.s += sums[0][w]; a.w += sums[1][w]; }
-    const float log_s = lp_log_sum(a.s);
-    const LpRow r = lp_row(g, row, a.m, a.s, log_s, lp_entropy(a, log_s));
-    if (tid == 0) lp_finish<T>(g, row, a, log_s);
-    const float asked = r.g != 0.0f && !r.bad && r.target >= 0 ? (float)x[r.target] : 0.0f;
-    __syncthreads();                                 // (the target's logit is read before the gradient may take its place)
-    T* const y = (T*)g.grad + row * g.ldg;
-    if (r.zero || r.bad) {
-      const T fill = (T)(r.bad ? __builtin_nanf("") : 0.0f);
-      if (lone >= 0) y[lone] = fill;
-#pragma unroll
-      for (int u = 0; u < V; ++u)
-        if (tid + u * THREADS < pieces) {
-          typename LpPiece<T>::vec out;
-#pragma unroll
-          for (int e = 0; e < E; ++e) out[e] = fill;
-          *(typename LpPiece<T>::any*)(y + head + (unsigned)(tid + u * THREADS) * E) = out;
-        }
-      continue;
-    }
-    const int hit = r.g != 0.0f && r.target >= 0 ? (int)r.target : -1;
-    auto slope = [&](float v) {
-      const float u = (v - r.m) * g.c;
-      return lp_slope<ENTROPY>(r, u, __builtin_amdgcn_exp2f(u));
-    };
-    if (lone >= 0) y[lone] = (T)(slope(alone) + (lone == hit ? r.g : 0.0f));
-#pragma unroll
-    for (int u = 0; u < V; ++u) {
-      const int at = tid + u * THREADS;
-      if (at < pieces) {
-        const int col = head + at * E;
         typename LpPiece<T>::vec out;
 #pragma unroll
-        for (int e = 0; e < E; ++e) out[e] = (T)slope((float)raw[u][e]);
-        if (hit >= col && hit < col + E) {
-          const T own = (T)(r.g + slope(asked));
-#pragma unroll
-          for (int e = 0; e < E; ++e) out[e] = col + e == hit ? own : out[e];
-        }
-        *(typename LpPiece<T>::any*)(y + head + (unsigned)at * E) = out;
+        for (int e = 0; e < E; ++e) out[e] = fill;
+        *(typename LpPiece<T>::any*)(y + head + (unsigned)(tid + u * THREADS) * E) = out;
       }
+    return;
+  }
+  const int hit = r.g != 0.0f && r.target >= 0 ? (int)r.target : -1;
+  auto slope = [&](float v) {
+    const float u = (v - r.m) * g.c;
+    return lp_slope<ENTROPY>(r, u, __builtin_amdgcn_exp2f(u));
+  };
+  if (lone >= 0) y[lone] = (T)(slope(alone) + (lone == hit ? r.g : 0.0f));
+#pragma unroll
+  for (int u = 0; u < V; ++u) {
+    const int at = tid + u * THREADS;
+    if (at < pieces) {
+      const int col = head + at * E;
+      typename LpPiece<T>::vec out;
+#pragma unroll
+      for (int e = 0; e < E; ++e) out[e] = (T)slope((float)raw[u][e]);
+      if (hit >= col && hit < col + E) {
+        const T own = (T)(r.g + slope(asked));
+#pragma unroll
+        for (int e = 0; e < E; ++e) out[e] = col + e == hit ? own : out[e];
+      }
+      *(typename LpPiece<T>::any*)(y + head + (unsigned)at * E) = out;
     }
   }
 }
 
-// Splits of a row between workgroups: as many as make 1024 of them, of at least 4096 columns.
-static int lp_splits(int64_t m, int64_t n) {
-  const int64_t want = std::max<int64_t>(1, 1024 / m);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, n / 4096), LP_SPLITS));
+// Workgroups of 1024 threads where they are enough for the card and 256 threads are not; with fewer rows these are split between workgroups of 256,
+// as many as make 1024 of them, of 512 pieces at least.
+static bool lp_wide(int64_t m, int64_t n, bool bf16) { return m >= 128 && m < 1024 && n >= (bf16 ? 8192 : 4096); }
+static int lp_splits(int64_t m, int64_t n, bool bf16) {
+  const int64_t want = m >= 128 ? 1 : 1024 / m;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, n / (bf16 ? 4096 : 2048)), LP_SPLITS));
 }
 static int64_t lp_chunk(int64_t n, int splits) { return (int64_t)align_up((size_t)ceil_div64(n, splits), 64); }
-static size_t lp_part_bytes(int64_t m, int64_t n, int top) {
-  const int s = lp_splits(m, n);
+static size_t lp_part_bytes(int64_t m, int64_t n, int top, bool bf16) {
+  const int s = lp_splits(m, n, bf16);
   return s > 1 ? (size_t)m * s * (16 + 8 * (size_t)top) : 0;
 }
 // Pieces that a workgroup of the one-call kernel can hold in registers; rows of more, and few rows, take two passes.
-static bool lp_held(int64_t m, int64_t n, bool bf16) { return lp_splits(m, n) == 1 && n / (bf16 ? 8 : 4) <= 16 * 1024; }
+static bool lp_held(int64_t m, int64_t n, bool bf16) { return lp_splits(m, n, bf16) == 1 && n / (bf16 ? 8 : 4) <= 16 * 1024; }
 
+#define LP_ROWS (1 << 20)                            // of a launch: fewer than 2^32 threads
 template <typename T>
 static int launch_logprobs(hipStream_t s, LpArgs g) {
-  g.splits = lp_splits(g.m, g.n);
+  g.splits = lp_splits(g.m, g.n, sizeof(T) == 2);
   g.chunk = lp_chunk(g.n, g.splits);
   g.splits = (int)ceil_div64(g.n, g.chunk);
-  const dim3 grid((unsigned)std::min<int64_t>(g.m, 1 << 20), (unsigned)g.splits), block(LP_THREADS);
-  if (g.top) LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, true>), grid, block, 0, g);
-  else LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, false>), grid, block, 0, g);
-  if (g.splits > 1)
-    LORACT_LAUNCH("token_logprobs_join", s, logprob_join_kernel<T>, dim3(grid.x), block, (unsigned)(g.splits * g.top * 8), g);
+  const int64_t pieces = g.chunk / LpPiece<T>::E;
+#define LP_FORWARD(THREADS)                                                                                                                    \
+  do {                                                                                                                                         \
+    const dim3 threads(THREADS);                                                                                                               \
+    if (!g.top) LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, THREADS, false, false>), grid, threads, 0, g);                             \
+    else if (pieces <= LP_HELD * THREADS) LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, THREADS, true, true>), grid, threads, 0, g);     \
+    else LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, THREADS, true, false>), grid, threads, 0, g);                                     \
+  } while (0)
+  for (g.row0 = 0; g.row0 < g.m; g.row0 += LP_ROWS) {
+    const dim3 grid((unsigned)std::min<int64_t>(g.m - g.row0, LP_ROWS), (unsigned)g.splits);
+    if (lp_wide(g.m, g.n, sizeof(T) == 2)) LP_FORWARD(1024);
+    else LP_FORWARD(LP_THREADS);
+    if (g.splits > 1) LORACT_LAUNCH("token_logprobs_join", s, logprob_join_kernel<T>, dim3(grid.x), dim3(LP_THREADS), (unsigned)(g.splits * g.top * 8), g);
+  }
+#undef LP_FORWARD
   return LORACT_OK;
 }
 template <typename T>
 static int launch_logprobs_backward(hipStream_t s, LpArgs g) {
-  const int64_t rows = std::min<int64_t>(g.m, 1 << 16);
   g.chunk = std::max<int64_t>(LP_THREADS * 4 * LpPiece<T>::E, lp_chunk(g.n, 64));
-  const dim3 grid((unsigned)rows, (unsigned)ceil_div64(g.n, g.chunk));
-  if (g.d_entropy) LORACT_LAUNCH("token_logprobs_backward", s, (logprob_backward_kernel<T, true>), grid, dim3(LP_THREADS), 0, g);
-  else LORACT_LAUNCH("token_logprobs_backward", s, (logprob_backward_kernel<T, false>), grid, dim3(LP_THREADS), 0, g);
+  for (g.row0 = 0; g.row0 < g.m; g.row0 += 1 << 17) {
+    const dim3 grid((unsigned)std::min<int64_t>(g.m - g.row0, 1 << 17), (unsigned)ceil_div64(g.n, g.chunk));
+    if (g.d_entropy) LORACT_LAUNCH("token_logprobs_backward", s, (logprob_backward_kernel<T, true>), grid, dim3(LP_THREADS), 0, g);
+    else LORACT_LAUNCH("token_logprobs_backward", s, (logprob_backward_kernel<T, false>), grid, dim3(LP_THREADS), 0, g);
+  }
   return LORACT_OK;
 }
 template <typename T>
@@ -537,17 +593,19 @@ static int launch_logprobs_grad(hipStream_t s, LpArgs g) {
     return launch_logprobs_backward<T>(s, g);
   }
   const int64_t pieces = g.n / LpPiece<T>::E;
-  const dim3 grid((unsigned)std::min<int64_t>(g.m, 1 << 20));
 #define LP_GRAD(THREADS, V)                                                                                                       \
   do {                                                                                                                             \
     if (g.d_entropy) LORACT_LAUNCH("token_logprobs_grad", s, (logprob_grad_kernel<T, THREADS, V, true>), grid, dim3(THREADS), 0, g); \
     else LORACT_LAUNCH("token_logprobs_grad", s, (logprob_grad_kernel<T, THREADS, V, false>), grid, dim3(THREADS), 0, g);          \
   } while (0)
-  if (pieces <= 256 * 2) LP_GRAD(256, 2);
-  else if (pieces <= 256 * 8) LP_GRAD(256, 8);
-  else if (pieces <= 512 * 8) LP_GRAD(512, 8);
-  else if (pieces <= 1024 * 8) LP_GRAD(1024, 8);
-  else LP_GRAD(1024, 16);
+  for (g.row0 = 0; g.row0 < g.m; g.row0 += LP_ROWS) {
+    const dim3 grid((unsigned)std::min<int64_t>(g.m - g.row0, LP_ROWS));
+    if (pieces <= 256 * 2) LP_GRAD(256, 2);
+    else if (pieces <= 256 * 8) LP_GRAD(256, 8);
+    else if (pieces <= 512 * 8) LP_GRAD(512, 8);
+    else if (pieces <= 1024 * 8) LP_GRAD(1024, 8);
+    else LP_GRAD(1024, 16);
+  }
 #undef LP_GRAD
   return LORACT_OK;
 }

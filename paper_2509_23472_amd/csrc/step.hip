@@ -144,7 +144,7 @@ extern "C" {
 int loract_token_logprobs_workspace_bytes(const loract_logprob_params* p, size_t* bytes) {
   if (!bytes) return LORACT_ERR_INVALID_ARG;
   LORACT_TRY(check_logprobs(p, true));
-  *bytes = align_up(lp_part_bytes(p->m, p->n, p->top), 256);
+  *bytes = align_up(lp_part_bytes(p->m, p->n, p->top, p->dtype == LORACT_BF16), 256);
   return LORACT_OK;
 }
 
@@ -153,7 +153,7 @@ int loract_token_logprobs(const void* x_dev, const void* targets_dev, const lora
   LORACT_TRY(check_logprobs(p, true));
   if (!x_dev || !stats_dev || (logp_dev && !targets_dev) || (p->top && (!top_logp_dev || !top_ids_dev))) return LORACT_ERR_INVALID_ARG;
   if (!logprobs_aligned(x_dev, targets_dev, p, {logp_dev, stats_dev, p->top ? top_logp_dev : nullptr, p->top ? top_ids_dev : nullptr})) return LORACT_ERR_INVALID_ARG;
-  const size_t need = lp_part_bytes(p->m, p->n, p->top);
+  const size_t need = lp_part_bytes(p->m, p->n, p->top, p->dtype == LORACT_BF16);
   if (need && (!ws_dev || ws_bytes < need)) return LORACT_ERR_WORKSPACE_TOO_SMALL;
   if (need && !at_multiple(ws_dev, 16)) return LORACT_ERR_INVALID_ARG;
   const int64_t size = p->dtype == LORACT_BF16 ? 2 : 4;
@@ -164,7 +164,7 @@ int loract_token_logprobs(const void* x_dev, const void* targets_dev, const lora
   LpArgs g = logprob_args(x_dev, targets_dev, p);
   g.logp = logp_dev; g.stats = stats_dev; g.top = p->top; g.top_logp = top_logp_dev; g.top_ids = top_ids_dev;
   g.part = (float*)ws_dev;
-  g.part_top = need ? (uint64_t*)((char*)ws_dev + (size_t)p->m * lp_splits(p->m, p->n) * 16) : nullptr;
+  g.part_top = need ? (uint64_t*)((char*)ws_dev + (size_t)p->m * lp_splits(p->m, p->n, p->dtype == LORACT_BF16) * 16) : nullptr;
   return size == 2 ? launch_logprobs<bf16_t>((hipStream_t)stream, g) : launch_logprobs<float>((hipStream_t)stream, g);
 }
 
@@ -190,7 +190,7 @@ int loract_token_logprobs_grad(const void* x_dev, const void* targets_dev, const
   if ((d_logp_dev || logp_dev) && !targets_dev) return LORACT_ERR_INVALID_ARG;
   const int64_t size = p->dtype == LORACT_BF16 ? 2 : 4;
   if (!logprobs_aligned(x_dev, targets_dev, p, {logp_dev, stats_dev, d_logp_dev, d_entropy_dev}) || !at_multiple(grad_dev, size)) return LORACT_ERR_INVALID_ARG;
-  const size_t need = lp_part_bytes(p->m, p->n, 0);
+  const size_t need = lp_part_bytes(p->m, p->n, 0, p->dtype == LORACT_BF16);
   if (need && (!ws_dev || ws_bytes < need)) return LORACT_ERR_WORKSPACE_TOO_SMALL;
   if (need && !at_multiple(ws_dev, 16)) return LORACT_ERR_INVALID_ARG;
   const LpOperands o = {extent_rows(x_dev, p->m, p->ld, p->n, size), extent_bytes(targets_dev, p->m * p->target_bits / 8), extent_bytes(d_logp_dev, p->m * 4),
