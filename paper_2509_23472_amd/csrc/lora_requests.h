@@ -4,9 +4,9 @@
 //          next launch adds as it reads them.
 //   up     Y = R + s T B.
 //
-// Up to 64 tokens: two launches.  Tokens in tiles, in order; a tile goes over the different adapters of its tokens (found by ballots) and takes
+// Few tokens and adapters: two launches.  Tokens in tiles, in order; a tile goes over the different adapters of its tokens (found by ballots) and takes
 // from each product what belongs to their tokens.  An adapter's infinities and NaN thus reach its own tokens only.
-// More tokens: a first launch orders them by adapter, in tiles of 64 that have one adapter each.  (In the order they come, a tile of single tokens of 22
+// Else a first launch orders them by adapter, in tiles of 64 that have one adapter each.  (In the order they come, a tile of single tokens of 22
 // requests walks over 22 adapters while others have one: 8192 tokens, the last hundred of them single ones, took 1040 us at rank 64 and 11008
 // columns, 330 without those.)  The places of an adapter's tokens among each other depend on an atomic counter, but no result depends on them.
 //
@@ -621,19 +621,22 @@ struct LqPlan {
 static LqPlan lora_requests_plan(int64_t m, int64_t k, int64_t n, int r, int64_t adapters, bool bf16) {
   LqPlan p;
   const int e = bf16 ? 8 : 4;
-  p.sorted = m > 64 && adapters <= LQ_SORTED;
+  // Ordering costs a launch (4 us), which the walk's serial turns cost too where there are many adapters: 64 tokens of as many, 4096 -> 4096 at rank 16
+  // (17 MB of A and B) 14 us in the order they come, 18 ordered; 4096 -> 11008 (31 MB) 27 both ways; at rank 64 (124 MB) 77 and 43.
+  const int64_t wide = 16 * e, cols = ceil_div64(n, wide), own = std::min(adapters, m);
+  p.sorted = adapters <= LQ_SORTED && (m > 64 || r > 32 || (double)own * r * (double)(k + n) * (16 / e) > (double)(32 << 20));
   p.ldt = r <= 16 ? 16 : (r <= 32 ? 32 : 64);
-  const int64_t cols = ceil_div64(n, 16 * e), most = std::min<int64_t>(16, adapters);
   // K splits: 512 workgroups (256 of ordered tokens), of a slab (a step) for each group (wave) at least
-  const int64_t tiles = ceil_div64(m, p.sorted ? LQ_TILE : 16), step = (p.sorted ? 16 * LQ_K_GROUPS : 4 * LQ_WAVES) * e;
+  const int64_t tiles = p.sorted ? std::max(ceil_div64(m, LQ_TILE), own) : ceil_div64(m, 16), step = (p.sorted ? 16 * LQ_K_GROUPS : 4 * LQ_WAVES) * e;
+  const int64_t most = std::min<int64_t>(16, adapters);
   p.shares = p.sorted ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, most));
   const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((p.sorted ? 256 : 512) / (tiles * p.shares), ceil_div64(k, step)), 16));
   p.k_per_split = ceil_div64(ceil_div64(k, splits), step) * step;
   p.splits = (int)ceil_div64(k, p.k_per_split);
   p.up_shares = (int)std::max<int64_t>(1, std::min<int64_t>(2048 / (cols * tiles), most));
-  p.trips = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(tiles * cols / 2048, 4), cols));
+  p.trips = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(tiles * cols / 1024, 4), cols));
   p.groups = ceil_div64(cols, p.trips);
-  p.tiles = p.sorted ? tiles + std::min<int64_t>(adapters + 2, m) : 0;
+  p.tiles = p.sorted ? ceil_div64(m, LQ_TILE) + std::min<int64_t>(adapters + 2, m) : 0;
   p.part_bytes = (size_t)p.splits * m * p.ldt * 4;
   p.tile_bytes = p.sorted ? align_up(8 + (size_t)p.tiles * 8, 16) : 0;
   p.bytes = p.part_bytes + p.tile_bytes + (size_t)p.tiles * LQ_TILE * 4;
