@@ -280,3 +280,17 @@ def test_another_stream():
         got = L.loract_token_logprobs(x, t, top=5)
     torch.cuda.current_stream().wait_stream(side)
     assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+@pytest.mark.parametrize("m,n", [(7, 20000), (600, 5000), (700, 140001)])
+def test_entropy_without_targets(m, n):
+    x, _, gen = _logits(m, n, BF, 15)
+    d = torch.randn(m, generator=gen, device="cuda")
+    f = L.loract_token_logprobs(x, top=3)
+    assert f.logp is None and torch.equal(f.top_ids[:5], ref.top(x[:5], 3))
+    few = slice(0, 9)
+    _check_grad(L.loract_token_logprobs_backward(x, None, f.stats, None, d)[few], x[few], None, None, d[few])
+    logp, entropy, grad = L.loract_token_logprobs_grad(x, None, None, d)
+    assert logp is None
+    _check_grad(grad[few], x[few], None, None, d[few])
+    _close(entropy[few], ref.logprobs(x[few], None)[2], 4 * _bound(x[few], 1.0) * ref.logprobs(x[few], None)[2].clamp(min=1), "entropy")
