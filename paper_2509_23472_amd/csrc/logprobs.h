@@ -439,7 +439,8 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_backward_kernel(LpArgs g) 
 
 // Both in one call: a row stays in the registers of a workgroup between the sums and the gradient.  V pieces per thread.  The exponentials are formed
 // again for the gradient: kept, they take twice the row's registers, and no second workgroup of the CU could work while one waits for memory.
-template <typename T, int THREADS, int V, bool ENTROPY>
+// REST: what lies behind V pieces per thread (65536 float32, 131072 bf16) is summed beside a running maximum and read again for the gradient.
+template <typename T, int THREADS, int V, bool ENTROPY, bool REST = false>
 __global__ __launch_bounds__(THREADS, V < 8 || THREADS * V == 8192 ? 8 : (V == 8 ? 7 : 4)) void logprob_grad_kernel(LpArgs g) {
   constexpr int E = LpPiece<T>::E, WAVES = THREADS / 64;
   __shared__ float tops[WAVES];
@@ -447,7 +448,7 @@ __global__ __launch_bounds__(THREADS, V < 8 || THREADS * V == 8192 ? 8 : (V == 8
   const int tid = threadIdx.x;
   const int64_t row = g.row0 + blockIdx.x;
   const T* const x = (const T*)g.x + row * g.ld;
-  const int n = (int)g.n, head = (int)lp_head(x, g.n), pieces = (n - head) / E, tail = n - head - pieces * E;      // (rows in registers are short)
+  const int n = (int)g.n, head = (int)lp_head(x, g.n), pieces = (n - head) / E, tail = n - head - pieces * E;
   const T* const body = x + head;
   typename LpPiece<T>::vec raw[V];
 #pragma unroll
@@ -457,7 +458,31 @@ __global__ __launch_bounds__(THREADS, V < 8 || THREADS * V == 8192 ? 8 : (V == 8
   }
   const int lone = tid < head ? tid : (tid >= E && tid < E + tail ? head + pieces * E + tid - E : -1);
   const float alone = lone >= 0 ? (float)x[lone] : -__builtin_inff();
-  float top = alone;
+  // f(values, piece) for the pieces that are not held
+  auto rest = [&](auto f) {
+    for (int at = tid + V * THREADS; at < pieces; at += 2 * THREADS) {
+      typename LpPiece<T>::vec two[2];
+      two[0] = *(const typename LpPiece<T>::vec*)(body + (unsigned)at * E);
+      if (at + THREADS < pieces) two[1] = *(const typename LpPiece<T>::vec*)(body + (unsigned)(at + THREADS) * E);
+      f(two[0], at);
+      if (at + THREADS < pieces) f(two[1], at + THREADS);
+    }
+  };
+  LpSum more = lp_none();
+  if constexpr (REST)
+    rest([&](const typename LpPiece<T>::vec& v, int) {
+      float t = (float)v[0];
+#pragma unroll
+      for (int e = 1; e < E; ++e) t = fmaxf(t, (float)v[e]);
+      if (t > more.m) more = lp_moved(more, t, g.c);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float u = ((float)v[e] - more.m) * g.c, p = __builtin_amdgcn_exp2f(u);
+        more.s += p;
+        more.w = fmaf(lp_cut(u), p, more.w);
+      }
+    });
+  float top = REST ? fmaxf(alone, more.m) : alone;
 #pragma unroll
   for (int u = 0; u < V; ++u)
     if (tid + u * THREADS < pieces) {
@@ -472,6 +497,7 @@ __global__ __launch_bounds__(THREADS, V < 8 || THREADS * V == 8192 ? 8 : (V == 8
 #pragma unroll
   for (int w = 1; w < WAVES; ++w) top = fmaxf(top, tops[w]);
   LpSum a = {fmaxf(top, -FLT_MAX), 0.0f, 0.0f};
+  if constexpr (REST) a = lp_moved(more, a.m, g.c);
   auto add = [&](float v) {
     const float u = (v - a.m) * g.c, p = __builtin_amdgcn_exp2f(u);
     a.s += p;
@@ -512,6 +538,12 @@ __global__ __launch_bounds__(THREADS, V < 8 || THREADS * V == 8192 ? 8 : (V == 8
         for (int e = 0; e < E; ++e) out[e] = fill;
         *(typename LpPiece<T>::any*)(y + head + (unsigned)(tid + u * THREADS) * E) = out;
       }
+    if constexpr (REST) {
+      typename LpPiece<T>::vec out;
+#pragma unroll
+      for (int e = 0; e < E; ++e) out[e] = fill;
+      for (int at = tid + V * THREADS; at < pieces; at += THREADS) *(typename LpPiece<T>::any*)(y + head + (unsigned)at * E) = out;
+    }
     return;
   }
   const int hit = r.g != 0.0f && r.target >= 0 ? (int)r.target : -1;
@@ -520,22 +552,22 @@ __global__ __launch_bounds__(THREADS, V < 8 || THREADS * V == 8192 ? 8 : (V == 8
     return lp_slope<ENTROPY>(r, u, __builtin_amdgcn_exp2f(u));
   };
   if (lone >= 0) y[lone] = (T)(slope(alone) + (lone == hit ? r.g : 0.0f));
+  auto put = [&](const typename LpPiece<T>::vec& v, int at) {
+    const int col = head + at * E;
+    typename LpPiece<T>::vec out;
 #pragma unroll
-  for (int u = 0; u < V; ++u) {
-    const int at = tid + u * THREADS;
-    if (at < pieces) {
-      const int col = head + at * E;
-      typename LpPiece<T>::vec out;
+    for (int e = 0; e < E; ++e) out[e] = (T)slope((float)v[e]);
+    if (hit >= col && hit < col + E) {
+      const T own = (T)(r.g + slope(asked));
 #pragma unroll
-      for (int e = 0; e < E; ++e) out[e] = (T)slope((float)raw[u][e]);
-      if (hit >= col && hit < col + E) {
-        const T own = (T)(r.g + slope(asked));
-#pragma unroll
-        for (int e = 0; e < E; ++e) out[e] = col + e == hit ? own : out[e];
-      }
-      *(typename LpPiece<T>::any*)(y + head + (unsigned)at * E) = out;
+      for (int e = 0; e < E; ++e) out[e] = col + e == hit ? own : out[e];
     }
-  }
+    *(typename LpPiece<T>::any*)(y + head + (unsigned)at * E) = out;
+  };
+#pragma unroll
+  for (int u = 0; u < V; ++u)
+    if (tid + u * THREADS < pieces) put(raw[u], tid + u * THREADS);
+  if constexpr (REST) rest(put);
 }
 
 // Workgroups of 1024 threads where they are enough for the card and 256 threads are not; with fewer rows these are split between workgroups of 256,
@@ -550,8 +582,9 @@ static size_t lp_part_bytes(int64_t m, int64_t n, int top, bool bf16) {
   const int s = lp_splits(m, n, bf16);
   return s > 1 ? (size_t)m * s * (16 + 8 * (size_t)top) : 0;
 }
-// Pieces that a workgroup of the one-call kernel can hold in registers; rows of more, and few rows, take two passes.
-static bool lp_held(int64_t m, int64_t n, bool bf16) { return lp_splits(m, n, bf16) == 1 && n / (bf16 ? 8 : 4) <= 16 * 1024; }
+// A workgroup per row holds what it can of it in registers; few rows are split between workgroups, in two passes, and so are rows of which less than half
+// could be held.
+static bool lp_held(int64_t m, int64_t n, bool bf16) { return lp_splits(m, n, bf16) == 1 && n / (bf16 ? 8 : 4) <= 32 * 1024; }
 
 #define LP_ROWS (1 << 20)                            // of a launch: fewer than 2^32 threads
 template <typename T>
@@ -593,18 +626,19 @@ static int launch_logprobs_grad(hipStream_t s, LpArgs g) {
     return launch_logprobs_backward<T>(s, g);
   }
   const int64_t pieces = g.n / LpPiece<T>::E;
-#define LP_GRAD(THREADS, V)                                                                                                       \
-  do {                                                                                                                             \
-    if (g.d_entropy) LORACT_LAUNCH("token_logprobs_grad", s, (logprob_grad_kernel<T, THREADS, V, true>), grid, dim3(THREADS), 0, g); \
-    else LORACT_LAUNCH("token_logprobs_grad", s, (logprob_grad_kernel<T, THREADS, V, false>), grid, dim3(THREADS), 0, g);          \
+#define LP_GRAD(THREADS, V, REST)                                                                                                        \
+  do {                                                                                                                                    \
+    if (g.d_entropy) LORACT_LAUNCH("token_logprobs_grad", s, (logprob_grad_kernel<T, THREADS, V, true, REST>), grid, dim3(THREADS), 0, g);  \
+    else LORACT_LAUNCH("token_logprobs_grad", s, (logprob_grad_kernel<T, THREADS, V, false, REST>), grid, dim3(THREADS), 0, g);           \
   } while (0)
   for (g.row0 = 0; g.row0 < g.m; g.row0 += LP_ROWS) {
     const dim3 grid((unsigned)std::min<int64_t>(g.m - g.row0, LP_ROWS));
-    if (pieces <= 256 * 2) LP_GRAD(256, 2);
-    else if (pieces <= 256 * 8) LP_GRAD(256, 8);
-    else if (pieces <= 512 * 8) LP_GRAD(512, 8);
-    else if (pieces <= 1024 * 8) LP_GRAD(1024, 8);
-    else LP_GRAD(1024, 16);
+    if (pieces <= 256 * 2) LP_GRAD(256, 2, false);
+    else if (pieces <= 256 * 8) LP_GRAD(256, 8, false);
+    else if (pieces <= 512 * 8) LP_GRAD(512, 8, false);
+    else if (pieces <= 1024 * 8) LP_GRAD(1024, 8, false);
+    else if (pieces <= 1024 * 16) LP_GRAD(1024, 16, false);
+    else LP_GRAD(1024, 16, true);
   }
 #undef LP_GRAD
   return LORACT_OK;

@@ -88,7 +88,7 @@ def test_forward_and_gradients(m, n, dtype):
         _close(entropy, ref.logprobs(x, t)[2], 4 * b * ref.logprobs(x, t)[2].clamp(min=1), "entropy")
 
 
-@pytest.mark.parametrize("m,n,dtype", [(600, 17000, BF), (520, 33000, F32), (513, 70001, F32), (515, 140000, BF), (1030, 32000, BF), (600, 4100, F32)])
+@pytest.mark.parametrize("m,n,dtype", [(600, 17000, BF), (520, 33000, F32), (513, 70001, F32), (515, 140000, BF), (400, 131001, F32), (130, 300000, BF), (130, 131100, F32), (1030, 32000, BF), (600, 4100, F32)])
 def test_rows_in_registers_and_rows_that_are_too_long(m, n, dtype):
     x, t, gen = _logits(m, n, dtype, 5)
     d_logp = torch.randn(m, generator=gen, device="cuda")
@@ -152,7 +152,7 @@ def test_clumped_maxima_exceed_the_candidates(m, dtype, trip):
 
 def test_masked_rows_and_lowest_values():
     for dtype in (BF, F32):
-        for m, n in ((6, 300), (6, 40000), (600, 4099)):
+        for m, n in ((6, 300), (6, 40000), (600, 4099), (150, 140003)):
             x, t, gen = _logits(m, n, dtype, 8)
             x[0] = -INF                                    # nothing is left
             x[1] = torch.finfo(dtype).min                  # the type's lowest value everywhere: as good as equal
@@ -179,7 +179,7 @@ def test_masked_rows_and_lowest_values():
 
 
 def test_what_is_no_number_and_targets_out_of_range():
-    for m, n in ((5, 700), (5, 20000), (600, 5000)):
+    for m, n in ((5, 700), (5, 20000), (600, 5000), (150, 80000)):
         x, t, _ = _logits(m, n, F32, 9)
         clean = L.loract_token_logprobs(x, t, top=3)
         x[0, 5] = float("nan")
@@ -199,7 +199,7 @@ def test_what_is_no_number_and_targets_out_of_range():
         assert (L.loract_token_logprobs_backward(x, t, f.stats, one) == 0).all() and (L.loract_token_logprobs_grad(x, t, one)[2] == 0).all()
 
 
-@pytest.mark.parametrize("m,n,dtype", [(600, 5000, BF), (3, 20001, BF), (700, 3001, F32)])
+@pytest.mark.parametrize("m,n,dtype", [(600, 5000, BF), (3, 20001, BF), (700, 3001, F32), (200, 80003, F32)])
 def test_in_place_and_strided(m, n, dtype):
     x, t, gen = _logits(m, n, dtype, 10, pad=5)
     d = torch.randn(m, generator=gen, device="cuda")
