@@ -604,8 +604,9 @@ class AdamwState:
     def __init__(self, sizes: Sequence[int], bits: int, device: torch.device):
         if bits not in (8, 32):
             raise ValueError("states are held in 32 or 8 bits")
-        self.sizes, self.bits = list(sizes), bits
-        padded = sum(-(-n // ADAMW_BLOCK) * ADAMW_BLOCK for n in self.sizes)
+        self.sizes, self.bits = tuple(sizes), bits
+        self._sizes, self._size_words = list(sizes), struct.pack("%dq" % len(self.sizes), *self.sizes)
+        self._padded = padded = sum(-(-n // ADAMW_BLOCK) * ADAMW_BLOCK for n in self.sizes)
         dtype = torch.float32 if bits == 32 else torch.uint8
         self.m, self.v = (torch.zeros(padded, dtype=dtype, device=device) for _ in range(2))
         self.exps = None
@@ -628,9 +629,10 @@ def _tensor_list(ts: Sequence[torch.Tensor], sizes: list, dtype: torch.dtype, de
     T = torch.Tensor
     if len(ts) != len(sizes) or list(map(T.numel, ts)) != sizes:
         raise ValueError("%s must be the state's %d tensors, with its sizes" % (what, len(sizes)))
-    if set(map(_DTYPE_OF, ts)) != {dtype} or set(map(T.get_device, ts)) != {device} or device < 0 or not all(map(T.is_contiguous, ts)):
+    n = len(ts)
+    if list(map(_DTYPE_OF, ts)).count(dtype) != n or list(map(T.get_device, ts)).count(device) != n or device < 0 or not all(map(T.is_contiguous, ts)):
         raise ValueError("%s must be contiguous tensors of %s on one GPU with the others" % (what, dtype))
-    return struct.pack("%dQ" % len(ts), *map(T.data_ptr, ts))
+    return struct.pack("%dQ" % n, *map(T.data_ptr, ts))
 
 
 def _scalar(v, dtype: torch.dtype, device: int, what: str):
@@ -649,12 +651,13 @@ def loract_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], 
 
     `grads` are float32 or bfloat16.  `copies` of float32 parameters get them rounded to bfloat16.  step (from 1 on) and lr are numbers, or
     tensors of one element (int64, float32) that are read when the step runs, as `grad_scale` (float32, multiplies the gradients) always is:
-    a captured step takes what changes from replay to replay from these.  What is held in fewer than 32 bits is rounded at random by
+    a captured step takes what changes from replay to replay from these.  Each tensor is looked over by every call (half a microsecond);
+    parameters that lie in one buffer can be given as one tensor.  What is held in fewer than 32 bits is rounded at random by
     (seed, step), so that small changes are kept on average."""
     params, grads = list(params), list(grads)
     if not params or not grads:
         raise ValueError("no tensors")
-    sizes, dev, dt, gdt = state.sizes, params[0].get_device(), params[0].dtype, grads[0].dtype
+    sizes, dev, dt, gdt = state._sizes, params[0].get_device(), params[0].dtype, grads[0].dtype
     p_ptr = _tensor_list(params, sizes, dt, dev, "params")
     g_ptr = _tensor_list(grads, sizes, gdt, dev, "grads")
     c_ptr = None
@@ -662,7 +665,7 @@ def loract_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], 
         if dt is not torch.float32:
             raise ValueError("only float32 parameters have copies")
         c_ptr = _tensor_list(list(copies), sizes, torch.bfloat16, dev, "copies")
-    padded = sum((n + ADAMW_BLOCK - 1) // ADAMW_BLOCK for n in sizes) * ADAMW_BLOCK
+    padded = state._padded
     held = torch.float32 if state.bits == 32 else torch.float8_e4m3fn
     for t in (state.m, state.v):
         if t.shape != (padded,) or t.dtype is not held or not t.is_contiguous() or t.get_device() != dev:
@@ -678,7 +681,7 @@ def loract_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], 
             raise ValueError("grad_scale must be a tensor")
         scale_ptr = _scalar(grad_scale, torch.float32, dev, "grad_scale")[1]
     args = _ADAMW_PARAMS.pack(lr, betas[0], betas[1], eps, weight_decay, step, seed & _SEED, _dtype_code(dt), _dtype_code(gdt), state.bits)
-    code = _lib.load().loract_adamw(p_ptr, g_ptr, c_ptr, struct.pack("%dq" % len(sizes), *sizes), len(sizes), args, state.m.data_ptr(),
+    code = _lib.load().loract_adamw(p_ptr, g_ptr, c_ptr, state._size_words, len(sizes), args, state.m.data_ptr(),
                                     state.v.data_ptr(), _ptr(state.exps), lr_ptr, step_ptr, scale_ptr, _stream_on(dev))
     if code:
         raise LoractError(code, "loract_adamw")

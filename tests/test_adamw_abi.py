@@ -119,3 +119,63 @@ def test_the_binding_refuses(bad, monkeypatch):
     with pytest.raises((ValueError, TypeError)):
         L.loract_adamw(t.p, t.g, t.state, **t.kw)
     assert len(reached) == 1
+
+
+SPANS = r"""
+#include "%s/paper_2509_23472_amd/csrc/spans.h"
+#include <cstdio>
+#include <random>
+#include <vector>
+// Every place of a gradient among the written intervals, in ascending, descending and mixed order, against all pairs.
+int main() {
+  std::mt19937 rng(5);
+  auto pick = [&](int n) { return (int)(rng() %% (unsigned)n); };
+  int met = 0, apart = 0;
+  for (int round = 0; round < 3000; ++round) {
+    const int n = 1 + pick(40), order = pick(3);
+    std::vector<int> at(n);
+    for (int i = 0; i < n; ++i) at[i] = i;
+    if (order == 1) std::reverse(at.begin(), at.end());
+    if (order == 2) std::shuffle(at.begin(), at.end(), rng);
+    std::vector<void*> p(n), copy(n);
+    std::vector<const void*> g(n);
+    std::vector<int64_t> size(n);
+    const uintptr_t p0 = 1 << 20, c0 = 1 << 24;
+    for (int i = 0; i < n; ++i) {
+      size[i] = pick(8) ? 1 + pick(30) : 0;
+      p[i] = (void*)(p0 + at[i] * 400);
+      copy[i] = pick(3) ? (void*)(c0 + at[i] * 400) : nullptr;
+      g[i] = (const void*)((pick(2) ? p0 : c0) + at[i] * 400 + 200);
+    }
+    if (pick(2)) g[pick(n)] = (const void*)((pick(2) ? p0 : c0) + pick(n) * 400 + 4 * pick(100));
+    if (pick(8) == 0) p[pick(n)] = p[pick(n)];               // (a tensor that is in the list twice)
+    Span state[3] = {{1 << 28, (1 << 28) + 1000}, {1 << 29, (1 << 29) + 1000}, {7, 7}}, scalars[3] = {{0, 0}, {0, 0}, {0, 0}};
+    if (pick(20) == 0) scalars[1] = {(uintptr_t)(1 << 29) + 996, (uintptr_t)(1 << 29) + 1004};
+    if (pick(20) == 0) state[0] = {p0 + 100, p0 + 104};
+    std::vector<Span> out, in;
+    for (const Span& s : state) if (s.hi > s.lo) out.push_back(s);
+    for (const Span& s : scalars) if (s.hi > s.lo) in.push_back(s);
+    for (int i = 0; i < n; ++i) {
+      if (!size[i]) continue;
+      out.push_back({(uintptr_t)p[i], (uintptr_t)p[i] + size[i] * 4});
+      if (copy[i]) out.push_back({(uintptr_t)copy[i], (uintptr_t)copy[i] + size[i] * 2});
+      in.push_back({(uintptr_t)g[i], (uintptr_t)g[i] + size[i] * 4});
+    }
+    bool want = false;
+    for (size_t i = 0; i < out.size(); ++i) {
+      for (size_t j = 0; j < i; ++j) want |= out[i].lo < out[j].hi && out[j].lo < out[i].hi;
+      for (const Span& s : in) want |= out[i].lo < s.hi && s.lo < out[i].hi;
+    }
+    if (adamw_meets(p.data(), g.data(), copy.data(), size.data(), n, 4, 4, state, scalars) != (int)want) return 1;
+    (want ? met : apart)++;
+  }
+  return met > 300 && apart > 300 ? 0 : 2;
+}
+"""
+
+
+def test_shared_memory_among_many_tensors_in_any_order(tmp_path):
+    src, exe = tmp_path / "spans.cpp", tmp_path / "spans"
+    src.write_text(SPANS % ROOT)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", str(src), "-o", str(exe)], check=True)
+    assert subprocess.run([str(exe)]).returncode == 0
