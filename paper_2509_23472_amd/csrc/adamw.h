@@ -12,7 +12,9 @@
 // to three digits would undo for ever; the root stays above zero where it is (a zero root below a moment that is not zero would make a step of m / eps).
 // bf16 parameters are rounded at random for the same reason.
 //
-// Bound by memory: p read and written, g read, the states read and written.
+// Bound by memory: p read and written, g read, the states read and written.  4 x 4096 x 4096: all in float32 315 us (6.0 TB/s; more is read than written, a copy
+// has 5.1), bf16 with 8-bit states 140 (4.8; 168 before the conversions took the rounding and a reciprocal the division: 85 vector operations per element are as
+// much as the reads allow).  448 adapters of 40 M elements, float32 with copies: 256 us in five launches, of which each starts and ends by itself.
 #pragma once
 #include "common.h"
 

@@ -17,7 +17,8 @@
 // go to the lowest index and the order of the atomic counter does not show.  Where too many lie above the bound (a row in descending
 // order), they are found one by one.
 //
-// Bound by memory: the logits are read once, the gradient written once.
+// Bound by memory: the logits are read once, the gradient written once.  8192 x 32000: forward 98 us (5.3 TB/s; a copy 5.1), backward 211, both in one
+// call 200 (5.2); float32 4096 x 32000 the same.  1001 x 50257 float32 forward 39, backward 86 (4.7).
 #pragma once
 #include "common.h"
 
@@ -26,7 +27,6 @@
 
 #define LP_THREADS 256
 #define LP_CANDIDATES 1024
-#define LP_HELD 4
 #define LP_SPLITS 64
 
 struct LpArgs {
@@ -127,46 +127,31 @@ __device__ inline LpRun lp_run(const T* row, int c0, int c1) {
   const int i = threadIdx.x;
   return {first, pieces, i < head ? c0 + i : (i >= E && i < E + tail ? first + pieces * E + i - E : -1)};
 }
-template <typename T, int U, int THREADS>
-__device__ inline void lp_fetch(const T* row, const LpRun& r, int v, typename LpPiece<T>::vec (&raw)[U]) {
-  const T* const first = row + r.first;
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (v + u * THREADS < r.pieces) raw[u] = *(const typename LpPiece<T>::vec*)(first + (unsigned)(v + u * THREADS) * LpPiece<T>::E);
-}
-// Calls f(values, column, how many) for pieces that are there.
+// Calls f(values, column, how many) for all elements [c0, c1) of a row, U pieces in flight.
 template <typename T, int U, int THREADS, typename F>
-__device__ inline void lp_visit(const LpRun& r, int v, const typename LpPiece<T>::vec (&raw)[U], F f) {
+__device__ inline void lp_each(const T* row, int c0, int c1, F f) {
   constexpr int E = LpPiece<T>::E;
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (v + u * THREADS >= r.pieces) continue;
-    float x[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = (float)raw[u][e];
-    f(x, r.first + (v + u * THREADS) * E, E);
-  }
-}
-template <typename T, typename F>
-__device__ inline void lp_alone(const LpRun& r, float value, F f) {
-  constexpr int E = LpPiece<T>::E;
-  if (r.lone < 0) return;
+  const LpRun r = lp_run(row, c0, c1);
+  const T* const first = row + r.first;
   float x[E];
-  x[0] = value;
+  for (int v = threadIdx.x; v < r.pieces; v += THREADS * U) {
+    typename LpPiece<T>::vec raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (v + u * THREADS < r.pieces) raw[u] = *(const typename LpPiece<T>::vec*)(first + (unsigned)(v + u * THREADS) * E);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (v + u * THREADS >= r.pieces) continue;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = (float)raw[u][e];
+      f(x, r.first + (v + u * THREADS) * E, E);
+    }
+  }
+  if (r.lone < 0) return;
+  x[0] = (float)row[r.lone];
 #pragma unroll
   for (int e = 1; e < E; ++e) x[e] = -__builtin_inff();
   f(x, r.lone, 1);
-}
-// Calls f for all of a run, U pieces in flight.
-template <typename T, int U, int THREADS, typename F>
-__device__ inline void lp_each(const T* row, int c0, int c1, F f) {
-  const LpRun r = lp_run(row, c0, c1);
-  for (int v = threadIdx.x; v < r.pieces; v += THREADS * U) {
-    typename LpPiece<T>::vec raw[U];
-    lp_fetch<T, U, THREADS>(row, r, v, raw);
-    lp_visit<T, U, THREADS>(r, v, raw, f);
-  }
-  lp_alone<T>(r, r.lone < 0 ? 0.0f : (float)row[r.lone], f);
 }
 // Fills the elements [c0, c1) of a row.
 template <typename T>
@@ -192,8 +177,9 @@ __device__ inline void lp_rank(const uint64_t* cand, int count, int k, F out) {
   }
 }
 
-// HELD: a workgroup's columns stay in registers (LP_HELD pieces of a thread) between the passes.
-template <typename T, int THREADS, bool TOP, bool HELD>
+// One pass for the sums, a second for the candidates.  (Kept in registers between the two, the columns of small workgroups gain nothing: 256 x 32000 with 20
+// alternatives 14.1 us both ways, 512 x 32000 24 against 19.)
+template <typename T, int THREADS, bool TOP>
 __global__ __launch_bounds__(THREADS) void logprob_kernel(LpArgs g) {
   constexpr int E = LpPiece<T>::E, WAVES = THREADS / 64;
   __shared__ LpSum sums[WAVES];
@@ -203,22 +189,7 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LpArgs g) {
   const int n = (int)g.n, chunk = (int)g.chunk, c0 = split * chunk, c1 = n - c0 < chunk ? n : c0 + chunk;
   const int64_t row = g.row0 + blockIdx.x;
   const T* const x = (const T*)g.x + row * g.ld;
-  LpRun run;
-  typename LpPiece<T>::vec raw[HELD ? LP_HELD : 1];
-  float alone = 0.0f;
-  if constexpr (HELD) {
-    run = lp_run(x, c0, c1);
-    lp_fetch<T, LP_HELD, THREADS>(x, run, tid, raw);
-    if (run.lone >= 0) alone = (float)x[run.lone];
-  }
-  auto each = [&](auto f) {
-    if constexpr (HELD) {
-      lp_visit<T, LP_HELD, THREADS>(run, tid, raw, f);
-      lp_alone<T>(run, alone, f);
-    } else {
-      lp_each<T, 4, THREADS>(x, c0, c1, f);
-    }
-  };
+  auto each = [&](auto f) { lp_each<T, 4, THREADS>(x, c0, c1, f); };
   LpSum a = lp_none();
   float best = -__builtin_inff();
   int best_col = -1;
@@ -570,8 +541,9 @@ __global__ __launch_bounds__(THREADS, V < 8 || THREADS * V == 8192 ? 8 : (V == 8
   if constexpr (REST) rest(put);
 }
 
-// Workgroups of 1024 threads where they are enough for the card and 256 threads are not; with fewer rows these are split between workgroups of 256,
-// as many as make 1024 of them, of 512 pieces at least.
+// Workgroups of 1024 threads where they are enough for the card and 256 threads are not (with 20 alternatives: 256 x 32000 14 us, 21 split between
+// workgroups of 256 and joined; 1024 x 32000 43, 29 with 256 threads).  Fewer rows are split between workgroups of 256, as many as make 1024 of
+// them, of 512 pieces at least: a row of 128000 with 5 alternatives 7 us and 4 for the join.
 static bool lp_wide(int64_t m, int64_t n, bool bf16) { return m >= 128 && m < 1024 && n >= (bf16 ? 8192 : 4096); }
 static int lp_splits(int64_t m, int64_t n, bool bf16) {
   const int64_t want = m >= 128 ? 1 : 1024 / m;
@@ -592,13 +564,10 @@ static int launch_logprobs(hipStream_t s, LpArgs g) {
   g.splits = lp_splits(g.m, g.n, sizeof(T) == 2);
   g.chunk = lp_chunk(g.n, g.splits);
   g.splits = (int)ceil_div64(g.n, g.chunk);
-  const int64_t pieces = g.chunk / LpPiece<T>::E;
-#define LP_FORWARD(THREADS)                                                                                                                    \
-  do {                                                                                                                                         \
-    const dim3 threads(THREADS);                                                                                                               \
-    if (!g.top) LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, THREADS, false, false>), grid, threads, 0, g);                             \
-    else if (pieces <= LP_HELD * THREADS) LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, THREADS, true, true>), grid, threads, 0, g);     \
-    else LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, THREADS, true, false>), grid, threads, 0, g);                                     \
+#define LP_FORWARD(THREADS)                                                                                                   \
+  do {                                                                                                                         \
+    if (g.top) LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, THREADS, true>), grid, dim3(THREADS), 0, g);               \
+    else LORACT_LAUNCH("token_logprobs", s, (logprob_kernel<T, THREADS, false>), grid, dim3(THREADS), 0, g);                   \
   } while (0)
   for (g.row0 = 0; g.row0 < g.m; g.row0 += LP_ROWS) {
     const dim3 grid((unsigned)std::min<int64_t>(g.m - g.row0, LP_ROWS), (unsigned)g.splits);
@@ -633,6 +602,7 @@ static int launch_logprobs_grad(hipStream_t s, LpArgs g) {
   } while (0)
   for (g.row0 = 0; g.row0 < g.m; g.row0 += LP_ROWS) {
     const dim3 grid((unsigned)std::min<int64_t>(g.m - g.row0, LP_ROWS));
+    // (512 threads with eight pieces: 8192 x 32000 bf16 212 us, with 1024 and four 250: fewer waves wait for the same row)
     if (pieces <= 256 * 2) LP_GRAD(256, 2, false);
     else if (pieces <= 256 * 8) LP_GRAD(256, 8, false);
     else if (pieces <= 512 * 8) LP_GRAD(512, 8, false);
