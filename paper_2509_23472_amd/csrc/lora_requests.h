@@ -14,8 +14,8 @@
 // would weigh as much as the output's own.
 //
 // Bound by memory: single tokens by A and B, prompts by X, R and Y.  Few tokens with an adapter each: the walk is shared out over workgroups too.
-// 8192 tokens of 24 adapters, 4096 -> 11008, rank 64: ordering 10 us, down 43 (rank 16: 24), up 101 (87, 4.1 TB/s); one token, rank 16, 4.6 and 7.8, where
-// each launch is a chain of three reads.
+// 8192 tokens of 24 adapters, 4096 -> 11008, rank 64: ordering 10 us, down 43 (rank 16: 24), up 101 (87, 4.1 TB/s); one token, rank 16, 4.5 and 7, where each launch
+// is a chain of three reads.
 #pragma once
 #include "common.h"
 #include "frag.h"
@@ -629,11 +629,12 @@ static LqPlan lora_requests_plan(int64_t m, int64_t k, int64_t n, int r, int64_t
   p.sorted = adapters <= LQ_SORTED && (m > 64 || r > 32 || (double)own * r * (double)(k + n) * (16 / e) > (double)(32 << 20));
   p.ldt = r <= 16 ? 16 : (r <= 32 ? 32 : 64);
   // K splits: 256 workgroups, of a slab (a step) for each group (wave) at least.  More parts of T cost the second launch more than they give the first: 64
-  // tokens of as many adapters, 4096 -> 4096 at rank 16, 13.4 us with 256, 14.7 with 512, 20 with 1024.
+  // tokens of as many adapters, 4096 -> 4096 at rank 16, 13.4 us with 256, 14.7 with 512, 20 with 1024.  Eight parts at most, which that launch has in
+  // flight: one token 4096 -> 11008 9.6 us in a graph, 10.8 with sixteen parts, 9.2 with four; at rank 64, ordered, 14.5, 14.5 and 15.9.
   const int64_t tiles = p.sorted ? std::max(ceil_div64(m, LQ_TILE), own) : ceil_div64(m, 16), step = (p.sorted ? 16 * LQ_K_GROUPS : 4 * LQ_WAVES) * e;
   const int64_t most = std::min<int64_t>(16, adapters);
   p.shares = p.sorted ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, most));
-  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(256 / (tiles * p.shares), ceil_div64(k, step)), 16));
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(256 / (tiles * p.shares), ceil_div64(k, step)), 8));
   p.k_per_split = ceil_div64(ceil_div64(k, splits), step) * step;
   p.splits = (int)ceil_div64(k, p.k_per_split);
   // Second launch: in the order they come, 2048 waves (64 tokens as above 14.7 us, with 1024 of them 16.7, with 4096 14.7); ordered, up to four times

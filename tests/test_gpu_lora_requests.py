@@ -40,7 +40,7 @@ def _check(got, x, a, b, ids, scales, res):
 SHAPES = [(1, 4096, 11008, 16, 8, "single"), (1, 1, 1, 1, 1, "single"), (2, 7, 5, 3, 2, "single"), (64, 4096, 4096, 16, 64, "single"), (17, 100, 130, 8, 5, "mixed"),
           (100, 257, 129, 33, 30, "mixed"), (33, 64, 1000, 64, 3, "mixed"), (300, 1030, 770, 12, 5, "runs"), (1000, 512, 640, 48, 16, "runs"), (8200, 264, 136, 64, 7, "runs"),
           (8200, 255, 1031, 5, 40, "mixed"), (5, 2050, 2048, 32, 100, "single"), (4100, 96, 11008, 17, 3, "runs"),
-          (300, 24, 40, 4, 9000, "mixed"), (500, 24, 40, 4, 8192, "mixed"), (64, 200, 136, 16, 7, "runs"), (65, 200, 136, 16, 7, "runs"), (20000, 40, 72, 8, 3, "mixed"),
+          (300, 24, 40, 4, 9000, "mixed"), (20, 40, 72, 64, 9000, "mixed"), (40, 300, 41, 33, 8200, "single"), (500, 24, 40, 4, 8192, "mixed"), (64, 200, 136, 16, 7, "runs"), (65, 200, 136, 16, 7, "runs"), (20000, 40, 72, 8, 3, "mixed"),
           (1, 4096, 4096, 64, 8, "single"), (60, 1400, 5000, 64, 60, "single"), (33, 4096, 11008, 64, 70, "mixed"), (8200, 64, 11003, 5, 6, "mixed"), (8200, 1000, 11008, 64, 5, "runs")]
 
 
