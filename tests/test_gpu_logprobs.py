@@ -294,3 +294,18 @@ def test_entropy_without_targets(m, n):
     assert logp is None
     _check_grad(grad[few], x[few], None, None, d[few])
     _close(entropy[few], ref.logprobs(x[few], None)[2], 4 * _bound(x[few], 1.0) * ref.logprobs(x[few], None)[2].clamp(min=1), "entropy")
+
+
+@pytest.mark.parametrize("n,dtype", [(3, F32), (9, BF)])
+def test_more_rows_than_a_launch_has(n, dtype):
+    m = (1 << 20) + 77
+    x, t, gen = _logits(m, n, dtype, 16)
+    d = torch.randn(m, generator=gen, device="cuda")
+    f = L.loract_token_logprobs(x, t, top=2)
+    log_p, _, entropy, logp = ref.logprobs(x, t)
+    b = _bound(x, 1.0)
+    _close(f.logp, logp, b + 40 * U, "logp")
+    _close(f.entropy, entropy, 4 * b * entropy.clamp(min=1), "entropy")
+    assert torch.equal(f.top_ids[-100:], ref.top(x[-100:], 2))
+    _check_grad(L.loract_token_logprobs_backward(x, t, f.stats, d), x, t, d, None)
+    _check_grad(L.loract_token_logprobs_grad(x, t, d)[2], x, t, d, None)
