@@ -352,7 +352,9 @@ typedef struct {
 /*
  * One step of AdamW over `count` tensors at once; every operation in float32 and in this order:
  *   g = grad_scale g,  m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) (g g),  r' = sqrt(v')
- *   p' = (1 - lr weight_decay) p - (lr / (1 - beta1^t)) (m' / (r' / sqrt(1 - beta2^t) + eps))
+ *   p' = (1 - lr weight_decay) p - (lr / (1 - beta1^t)) (m' / (r' (1 / sqrt(1 - beta2^t)) + eps))
+ * the factors of t and of the rates rounded once from 64 bits, the last quotient formed with the hardware's reciprocal (an ulp; the states do
+ * not depend on it).
  * p, g, copy, n    arrays of `count` in host memory, read before the call returns: the tensors' device pointers (contiguous; p of
  *                  p_dtype, updated in place; g of g_dtype) and their sizes (0: a tensor without elements).  copy, or any entry of it, may be
  *                  NULL: else p' rounded to bf16 is written there too (float32 parameters only).

@@ -4,7 +4,7 @@
 //   rate = lr / (1 - b1^t),  inv = 1 / sqrt(1 - b2^t)
 //
 // Every operation is rounded by itself, in this order (no fused multiply-adds): the codes of the 8-bit states are then a function
-// of the definition alone, whoever computes them.
+// of the definition alone, whoever computes them.  Only the quotient, which no state depends on, takes the hardware's reciprocal (an ulp).
 //
 // States in 8 bits.  Of 256 elements m and r = sqrt(v) are held as e4m3 numbers times a power of two each.  A power of two costs no digit of a
 // floating-point code, only range (17 binades below the largest element), and scaling by it is exact.  The root, not v, because its range is
