@@ -439,7 +439,7 @@ typedef struct {
  *            is not there (adapters or more) gives a row of NaN.
  * scales_dev adapters floats, or NULL (ones).   R_dev m x n_out, or NULL (zeros).
  * Y_dev      out, m x n_out; may be R with the same ld: then rows without an adapter are left as they are.
- * Sums are float32, X A is not rounded to less than 16 bits between the products.  What an adapter or a token holds reaches the tokens with that
+ * Sums are float32, and X A keeps all 24 digits between the products.  What an adapter or a token holds reaches the tokens with that
  * adapter and that token alone, be it infinite.  adapters, n_in up to 2^30; m up to 2^27, n_out up to 2^24, and less together where a launch could not
  * hold them (LORACT_ERR_UNSUPPORTED, from the workspace query too).
  */

@@ -10,8 +10,9 @@
 // requests walks over 22 adapters while others have one: 8192 tokens, the last hundred of them single ones, took 1040 us at rank 64 and 11008
 // columns, 330 without those.)  The places of an adapter's tokens among each other depend on an atomic counter, but no result depends on them.
 //
-// bf16 T enters the second product as the sum of two bf16 numbers: 16 bits of it for one more matrix instruction, where one rounding
-// would weigh as much as the output's own.
+// T of bf16 operands enters the second product as the sum of three bf16 numbers, which hold all of its 24 digits: float32 results are off by 1.0e-7 to 1.3e-7 of
+// the norm, as those of float32 operands are (with two numbers, 16 digits, by 2.5e-6, and the second launch takes 1 to 2 % less: 102 against 104 us at 8192 tokens of 24
+// adapters, 4096 -> 11008, rank 64).
 //
 // Bound by memory: single tokens by A and B, prompts by X, R and Y.  Few tokens with an adapter each: the walk is shared out over workgroups too.
 // 8192 tokens of 24 adapters, 4096 -> 11008, rank 64: ordering 10 us, down 43 (rank 16: 24), up 101 (87, 4.1 TB/s); one token, rank 16, 4.5 and 7, where each launch
@@ -372,17 +373,29 @@ __device__ inline void lq_t(const LqArgs& g, int64_t token, int k, float by, flo
 #pragma unroll
   for (int e = 0; e < E; ++e) t[e] = k + e < g.r ? t[e] * by : 0.0f;
 }
-// The operand of that: hi, and for bf16 what it leaves.
+// The operand of that: T itself, or three bf16 numbers whose sum is T.  Each takes eight of the 24 digits, cut off towards zero, so that what it leaves is exact.
+template <typename T>
+struct LqParts {
+  static constexpr int N = sizeof(T) == 2 ? 3 : 1;
+  typename Ln<T>::frag part[N];
+};
 template <typename T, int E>
-__device__ inline void lq_parts(const float (&t)[E], typename Ln<T>::frag& hi, typename Ln<T>::frag& lo) {
+__device__ inline LqParts<T> lq_parts(const float (&t)[E]) {
+  constexpr int N = LqParts<T>::N;
+  LqParts<T> f;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    hi[e] = (T)t[e];
-    if constexpr (sizeof(T) == 2) {
-      const float rest = t[e] - (float)hi[e];
-      lo[e] = (T)(fabsf(rest) < __builtin_inff() ? rest : 0.0f);
+    float left = t[e];
+#pragma unroll
+    for (int p = 0; p < N - 1; ++p) {
+      const unsigned cut = __float_as_uint(left) & 0xffff0000u;
+      f.part[p][e] = (T)__uint_as_float(cut);
+      const float rest = left - __uint_as_float(cut);
+      left = fabsf(rest) < __builtin_inff() ? rest : 0.0f;
     }
+    f.part[N - 1][e] = (T)left;
   }
+  return f;
 }
 
 template <typename O, int E>
@@ -460,8 +473,7 @@ __global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_up_kernel(LqArgs g) {
       float t[E] = {};
       const int k = STEP * s + E * q;
       if ((rows >> c & 1) && k < g.r) lq_t<E>(g, token, k, by, t);            // (rows of other adapters may not be written at all)
-      frag hi, lo;
-      lq_parts<T>(t, hi, lo);
+      const LqParts<T> ts = lq_parts<T>(t);
 #pragma unroll
       for (int j = 0; j < E; ++j) {                  // turned: column E c + j, rows STEP s + E q ..
         frag f;
@@ -477,8 +489,8 @@ __global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_up_kernel(LqArgs g) {
 #pragma unroll
           for (int e = 0; e < E; ++e) f[e] = v[s][e][j];
         }
-        acc[j] = ln_mfma(hi, f, acc[j]);
-        if constexpr (sizeof(T) == 2) acc[j] = ln_mfma(lo, f, acc[j]);
+#pragma unroll
+        for (int p = 0; p < LqParts<T>::N; ++p) acc[j] = ln_mfma(ts.part[p], f, acc[j]);
       }
     }
 #pragma unroll
@@ -545,7 +557,7 @@ __global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_up_sorted_kernel(LqArgs
     }
   };
   load(first);
-  frag hi[RS], lo[RS];
+  LqParts<T> ts[RS];
   if (there && work) {
     const float by = g.scales ? g.scales[d] : 1.0f;
 #pragma unroll
@@ -553,7 +565,7 @@ __global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_up_sorted_kernel(LqArgs
       float t[E] = {};
       const int k = STEP * s + E * q;
       if (live && k < g.r) lq_t<E>(g, token, k, by, t);
-      lq_parts<T>(t, hi[s], lo[s]);
+      ts[s] = lq_parts<T>(t);
     }
   }
   int turn = 0;
@@ -588,8 +600,8 @@ __global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_up_sorted_kernel(LqArgs
 #pragma unroll
               for (int e = 0; e < E; ++e) f[e] = *(const T*)(smem[turn] + (STEP * s + E * q + e) * PITCH + 64 * j + 4 * c);
             }
-            acc[h] = ln_mfma(f, hi[s], acc[h]);
-            if constexpr (sizeof(T) == 2) acc[h] = ln_mfma(f, lo[s], acc[h]);
+#pragma unroll
+            for (int p = 0; p < LqParts<T>::N; ++p) acc[h] = ln_mfma(f, ts[s].part[p], acc[h]);
           }
       } else if ((int64_t)d > g.adapters) {
 #pragma unroll
