@@ -440,7 +440,7 @@ typedef struct {
  * scales_dev adapters floats, or NULL (ones).   R_dev m x n_out, or NULL (zeros).
  * Y_dev      out, m x n_out; may be R with the same ld: then rows without an adapter are left as they are.
  * Sums are float32, and X A keeps all 24 digits between the products.  What an adapter or a token holds reaches the tokens with that
- * adapter and that token alone, be it infinite.  adapters, n_in up to 2^30; m up to 2^27, n_out up to 2^24, and less together where a launch could not
+ * adapter and that token alone, be it infinite: an infinite element of B gives infinity by the sign of X A (of a magnitude of 2^-100 or more; 0 gives NaN).  adapters, n_in up to 2^30; m up to 2^27, n_out up to 2^24, and less together where a launch could not
  * hold them (LORACT_ERR_UNSUPPORTED, from the workspace query too).
  */
 int loract_lora_requests_workspace_bytes(const loract_requests_params* p, size_t* bytes);

@@ -373,7 +373,9 @@ __device__ inline void lq_t(const LqArgs& g, int64_t token, int k, float by, flo
 #pragma unroll
   for (int e = 0; e < E; ++e) t[e] = k + e < g.r ? t[e] * by : 0.0f;
 }
-// The operand of that: T itself, or three bf16 numbers whose sum is T.  Each takes eight of the 24 digits, cut off towards zero, so that what it leaves is exact.
+// The operand of that: T itself, or three bf16 numbers whose sum is T.  Each takes eight of the 24 digits, and what it leaves is exact.  A number that eight digits
+// hold gives its predecessor towards zero, so that something is left: all three have T's sign, and an infinite element of B meets no zero and no
+// opposite sign (T inf is T's infinity whatever its digits, as of float32 operands; an infinite T has the largest number twice, then infinity).
 template <typename T>
 struct LqParts {
   static constexpr int N = sizeof(T) == 2 ? 3 : 1;
@@ -388,10 +390,9 @@ __device__ inline LqParts<T> lq_parts(const float (&t)[E]) {
     float left = t[e];
 #pragma unroll
     for (int p = 0; p < N - 1; ++p) {
-      const unsigned cut = __float_as_uint(left) & 0xffff0000u;
-      f.part[p][e] = (T)__uint_as_float(cut);
-      const float rest = left - __uint_as_float(cut);
-      left = fabsf(rest) < __builtin_inff() ? rest : 0.0f;
+      const float cut = __uint_as_float((__float_as_uint(left) - (left != 0.0f)) & 0xffff0000u);
+      f.part[p][e] = (T)cut;
+      left -= cut;
     }
     f.part[N - 1][e] = (T)left;
   }

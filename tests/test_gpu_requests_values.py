@@ -1,9 +1,10 @@
-"""Adapters of many requests, both routes (in the order the tokens come, and ordered by adapter first): the digits of X A."""
+"""Adapters of many requests, both routes (in the order the tokens come, and ordered by adapter first): the digits of X A, infinite elements
+of B."""
 import pytest
 import torch
 
 import paper_2509_23472_amd as L
-from test_gpu_lora_requests import BF, F32, _ids
+from test_gpu_lora_requests import BF, F32, INF, _check, _ids, _make
 
 pytestmark = pytest.mark.gpu
 # (tokens, rank, adapters): few tokens of a small rank in the order they come; more of them, a larger rank, or much of A and B ordered
@@ -29,3 +30,31 @@ def test_float32_results_keep_24_digits_of_xa(m, r, count):
     want = 0.5 * t[:, None] * torch.exp2(hot % 5.0).double()[ids.clamp(min=0).long()]
     want[ids < 0] = 0
     assert torch.equal(got.double(), want), (got.double() - want).abs().max()
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF, BF), (F32, F32), (BF, F32)])
+@pytest.mark.parametrize("m,r,count", ROUTES)
+def test_infinite_elements_of_b(m, r, count, dtype, out_dtype):
+    """t inf = +-inf by the sign of t, whatever t's digits: numbers of bf16 (X of one element that is not zero, A of powers of two), and any others."""
+    x, a, b, scales, res, gen = _make(m, 130, 72, r, count, dtype, m + 1, out_dtype)
+    x[::2] = 0
+    x[::2, 5] = torch.randn(len(x[::2]), generator=gen, device="cuda").to(dtype)
+    a[:, 5] = torch.exp2(torch.randint(-3, 4, (count, r), generator=gen, device="cuda").float()).to(dtype)
+    scales.fill_(0.5)
+    b[:, r // 2, 7], b[:, 0, 30], b[:, r - 1, 71] = INF, -INF, INF
+    ids = _ids("mixed", m, count, gen)
+    ids[0] = 0
+    got = L.loract_lora_requests(x, a, b, ids, scales, residual=res, out_dtype=out_dtype)
+    live, far = ids >= 0, torch.tensor([7, 30, 71], device="cuda")
+    near = torch.ones(72, dtype=torch.bool, device="cuda")
+    near[far] = False
+    _check(got[:, near], x, a, b[:, :, near], ids, scales, res[:, near])
+    # b's other elements of these columns are finite: the signs are those of X A at the infinite one, which is no zero and far from it
+    for j, k, sign in ((7, r // 2, 1), (30, 0, -1), (71, r - 1, 1)):
+        t = (x.double() * a[ids.clamp(min=0).long(), :, k].double()).sum(1) * sign
+        sure = live & (t.abs() > 1e-6)
+        assert sure.sum() >= live.sum() - 1 and torch.equal(got[sure, j].double(), t[sure].sign() * INF), j
+    assert torch.equal(got[~live], res[~live])
+    x[:] = 0                                                     # 0 inf is no number
+    got = L.loract_lora_requests(x, a, b, ids, scales, residual=res, out_dtype=out_dtype)
+    assert torch.isnan(got[live][:, far]).all() and torch.equal(got[live][:, near], res[live][:, near]) and torch.equal(got[~live], res[~live])
