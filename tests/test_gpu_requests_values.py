@@ -1,10 +1,10 @@
 """Adapters of many requests, both routes (in the order the tokens come, and ordered by adapter first): the digits of X A, infinite elements
-of B."""
+of B, tokens whose adapter is not in the pool, what is not finite."""
 import pytest
 import torch
 
 import paper_2509_23472_amd as L
-from test_gpu_lora_requests import BF, F32, INF, _check, _ids, _make
+from test_gpu_lora_requests import BF, F32, INF, NAN, _check, _ids, _make
 
 pytestmark = pytest.mark.gpu
 # (tokens, rank, adapters): few tokens of a small rank in the order they come; more of them, a larger rank, or much of A and B ordered
@@ -58,3 +58,42 @@ def test_infinite_elements_of_b(m, r, count, dtype, out_dtype):
     x[:] = 0                                                     # 0 inf is no number
     got = L.loract_lora_requests(x, a, b, ids, scales, residual=res, out_dtype=out_dtype)
     assert torch.isnan(got[live][:, far]).all() and torch.equal(got[live][:, near], res[live][:, near]) and torch.equal(got[~live], res[~live])
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF, BF), (F32, F32), (BF, F32)])
+@pytest.mark.parametrize("how", ["residual", "in place", "no residual"])
+@pytest.mark.parametrize("m,r,count", ROUTES[1:])
+def test_ids_past_the_pool(m, r, count, how, dtype, out_dtype):
+    x, a, b, scales, res, gen = _make(m, 64, 200, r, count, dtype, 6, out_dtype)
+    ids = _ids("mixed", m, count, gen)
+    past = torch.tensor([4, 11, m // 2, m - 1], device="cuda")
+    ids[past] = torch.tensor([count, 2 ** 31 - 1, 77, count], dtype=torch.int32, device="cuda")
+    ids[[0, m - 2]] = -1
+    if how == "in place":
+        got = L.loract_lora_requests(x, a, b, ids, scales, residual=(out := res.clone()), out=out, out_dtype=out_dtype)
+        assert got is out
+    else:
+        got = L.loract_lora_requests(x, a, b, ids, scales, residual=res if how == "residual" else None, out_dtype=out_dtype)
+    assert torch.isnan(got[past]).all()
+    assert torch.equal(got[ids < 0], res[ids < 0] if how != "no residual" else torch.zeros_like(res[ids < 0]))
+    _check(got, x, a, b, ids, scales, res if how != "no residual" else None)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("m,r", [(300, 16), (50, 64), (777, 33)])
+def test_what_is_not_finite_stays_with_its_own_where_tokens_are_ordered(m, r, dtype):
+    """Several tokens of every adapter share its tile with the token that holds NaN."""
+    x, a, b, scales, res, gen = _make(m, 200, 136, r, 8, dtype, 7)
+    ids = (torch.arange(m, device="cuda") % 8).int()
+    clean = L.loract_lora_requests(x, a, b, ids, scales, residual=res)
+    _check(clean, x, a, b, ids, scales, res)
+    a[2, 5, 3], b[3, 1, 7], x[9, 0], scales[6], res[12, 4], x[21, 199] = NAN, INF, NAN, INF, NAN, INF
+    got = L.loract_lora_requests(x, a, b, ids, scales, residual=res)
+    token = torch.arange(m, device="cuda")
+    own = (token == 9) | (token == 12) | (token == 21)
+    untouched = ~((ids == 2) | (ids == 3) | (ids == 6) | own)
+    assert torch.equal(got[untouched], clean[untouched]) and untouched.sum() > m // 2
+    assert torch.isnan(got[ids == 2]).all() and torch.isnan(got[9]).all() and not torch.isfinite(got[ids == 6]).any() and not torch.isfinite(got[21]).any()
+    row = (ids == 3) & ~own
+    assert torch.isinf(got[row][:, 7]).all() and torch.equal(got[row][:, :7], clean[row][:, :7]) and torch.equal(got[row][:, 8:], clean[row][:, 8:])
+    assert torch.isnan(got[12, 4]) and torch.equal(got[12, :4], clean[12, :4]) and torch.equal(got[12, 5:], clean[12, 5:])
