@@ -1,7 +1,7 @@
 // Log probabilities of given tokens under logits (tokens x vocabulary), with the entropy and the largest alternatives, and their gradient.
 //
 //   c = 1 / (T ln 2),  M = max x,  u_j = (x_j - M) c,  S = sum 2^u_j,  W = sum u_j 2^u_j
-//   log p_j = ln 2 (u_j - log2 S),   H = ln 2 (log2 S - W / S)      (no cancellation: log2 S >= 0, W <= 0)
+//   log p_j = (x_j - M) / T - ln 2 log2 S,   H = ln 2 (log2 S - W / S)      (no cancellation: log2 S >= 0, W <= 0)
 //   dx_j = (1 / T) [ g (delta_jt - p_j) - h p_j (log p_j + H) ]
 //
 // Exponents are binary logarithms, so that an element costs a difference, a product and the exponential: a CU has 30 vector operations for each bf16
@@ -71,9 +71,10 @@ __device__ inline LpSum lp_wave_merge(LpSum a, float c) {
   }
   return a;
 }
-// Log probability of an element of logit x (what is below nothing, a row without a distribution, gives -inf).
+// Log probability of an element of logit x (what is below nothing, a row without a distribution, gives -inf).  By 1 / T, not by c, which takes the lowest
+// values of a type, finite masks, past float32's range: their log p is finite as they are.
 __device__ inline float lp_log(const LpArgs& g, float x, const LpSum& a, float log_s) {
-  return a.s == 0.0f ? -__builtin_inff() : ((x - a.m) * g.c - log_s) * LP_LN2;
+  return a.s == 0.0f ? -__builtin_inff() : fmaf(-LP_LN2, log_s, (x - a.m) * g.inv_t);
 }
 __device__ inline float lp_log_sum(float s) { return s == 0.0f ? 0.0f : log2f(s); }
 __device__ inline float lp_entropy(const LpSum& a, float log_s) { return a.s == 0.0f ? 0.0f : (log_s - a.w / a.s) * LP_LN2; }
