@@ -342,7 +342,7 @@ int loract_qknorm_rope_backward(const void* q_dev, const void* k_dev, const lora
 #define LORACT_ADAMW_BLOCK 256   /* elements of a state in 8 bits that share an exponent; tensors begin at multiples of it */
 
 typedef struct {
-  double lr, beta1, beta2, eps, weight_decay;   /* lr, eps, weight_decay >= 0; 0 <= beta < 1 */
+  double lr, beta1, beta2, eps, weight_decay;   /* lr, weight_decay >= 0; eps 0, or 2^-126 or more; 0 <= beta < 1 */
   int64_t step;          /* t, from 1 on */
   uint64_t seed;         /* of the random roundings */
   int32_t p_dtype, g_dtype;      /* loract_dtype of the parameters and of the gradients */

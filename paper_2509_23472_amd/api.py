@@ -649,7 +649,7 @@ def loract_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], 
                  copies: Optional[Sequence[torch.Tensor]] = None) -> None:
     """One step of AdamW on all of `params` (float32 or bfloat16, in place) and `state`.
 
-    `grads` are float32 or bfloat16.  `copies` of float32 parameters get them rounded to bfloat16.  step (from 1 on) and lr are numbers, or
+    `grads` are float32 or bfloat16.  `copies` of float32 parameters get them rounded to bfloat16.  eps is 0 or 2^-126 at least.  step (from 1 on) and lr are numbers, or
     tensors of one element (int64, float32) that are read when the step runs, as `grad_scale` (float32, multiplies the gradients) always is:
     a captured step takes what changes from replay to replay from these.  Each tensor is looked over by every call (half a microsecond);
     parameters that lie in one buffer can be given as one tensor.  What is held in fewer than 32 bits is rounded at random by

@@ -19,6 +19,8 @@ static int64_t adamw_padded(int64_t n) { return (int64_t)align_up((size_t)n, LOR
 
 static bool in_unit(double v) { return v >= 0.0 && v < 1.0; }
 static bool at_least_zero(double v) { return v >= 0.0 && v <= 1.7e308; }
+// (to the hardware's reciprocal a denominator below 2^-126 is zero: a parameter without a gradient would become 0 / 0)
+static bool eps_ok(double v) { return v == 0.0 || (v >= 0x1p-126 && v <= 1.7e308); }
 
 extern "C" {
 
@@ -27,7 +29,7 @@ int loract_adamw(void* const* p, const void* const* g, void* const* copy, const 
                  const int64_t* step_dev, const float* grad_scale_dev, void* stream) {
   if (!params || count < 0 || (count && (!p || !g || !n))) return LORACT_ERR_INVALID_ARG;
   if (!dtype_ok(params->p_dtype) || !dtype_ok(params->g_dtype) || (params->state_bits != 32 && params->state_bits != 8)) return LORACT_ERR_INVALID_ARG;
-  if (!in_unit(params->beta1) || !in_unit(params->beta2) || !at_least_zero(params->eps) || !at_least_zero(params->weight_decay)) return LORACT_ERR_INVALID_ARG;
+  if (!in_unit(params->beta1) || !in_unit(params->beta2) || !eps_ok(params->eps) || !at_least_zero(params->weight_decay)) return LORACT_ERR_INVALID_ARG;
   if ((!lr_dev && !at_least_zero(params->lr)) || (!step_dev && params->step < 1)) return LORACT_ERR_INVALID_ARG;
   if (count > (1 << 24)) return LORACT_ERR_UNSUPPORTED;
   const bool narrow = params->state_bits == 8, p_bf16 = params->p_dtype == LORACT_BF16, g_bf16 = params->g_dtype == LORACT_BF16;
