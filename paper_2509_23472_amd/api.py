@@ -653,7 +653,10 @@ def loract_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], 
     tensors of one element (int64, float32) that are read when the step runs, as `grad_scale` (float32, multiplies the gradients) always is:
     a captured step takes what changes from replay to replay from these.  Each tensor is looked over by every call (half a microsecond);
     parameters that lie in one buffer can be given as one tensor.  What is held in fewer than 32 bits is rounded at random by
-    (seed, step), so that small changes are kept on average."""
+    (seed, step), so that small changes are kept on average.
+
+    Like everything that this package writes, parameters and copies change without autograd's notice: a backward pass through a graph that
+    saved them before the step does not raise (torch.autograd.graph.increment_version(params) makes it)."""
     params, grads = list(params), list(grads)
     if not params or not grads:
         raise ValueError("no tensors")
