@@ -5,20 +5,21 @@
 //   dx_j = (1 / T) [ g (delta_jt - p_j) - h p_j (log p_j + H) ]
 //
 // Exponents are binary logarithms, so that an element costs a difference, a product and the exponential: a CU has 30 vector operations for each bf16
-// that it reads and writes at the rate of a copy, and an exponential is four of them.  c is rounded once for all elements (a relative error of 2^-25 of
-// the temperature), u twice.  The maximum is one of x itself: a row of the type's lowest value, which x c may not hold, is as good as equal.
+// that it reads and writes at the rate of a copy, and an exponential is four of them.  c is rounded once for all elements (a relative error of at most
+// 2^-24 of the temperature), u twice.  The maximum is one of x itself: a row of the type's lowest value, which x c may not hold, is as good as equal.
 // S and W are kept beside a running maximum in one pass: a new maximum M' takes S to S 2^((M - M') c), W to (W + (M - M') c S) 2^((M - M') c).
 // In W u is cut off at -300, where 2^u is 0: an infinite u times 0 never occurs; NaN stays in S.
 // The running maximum starts at the lowest finite number, so that a row of nothing but -inf ends with S = 0.
 //
-// The k largest: a workgroup first finds each thread's largest element; the k-th largest of those bounds the k-th largest element from below,
-// and few elements lie above it (k (1 + k / 512) of them in random order).  A second pass over the row, which is in L2, collects these in LDS, where they
+// The k largest: a workgroup first finds the largest element of each of 64 groups of its columns (k up to 32) or of 256; the k-th largest of those bounds the k-th
+// largest element from below, and few elements lie above it (in random order -G ln(1 - k / G) of them for G groups: 24 for k = 20, 74 for 64).  A second pass over the row, which is in L2, collects these in LDS, where they
 // are ranked by counting.  Elements are ordered by one 64-bit number, the value's order above the index's complement: no two are equal, so ties
 // go to the lowest index and the order of the atomic counter does not show.  Where too many lie above the bound (a row in descending
 // order), they are found one by one.
 //
 // Bound by memory: the logits are read once, the gradient written once.  8192 x 32000: forward 98 us (5.3 TB/s; a copy 5.1), backward 211, both in one
-// call 200 (5.2); float32 4096 x 32000 the same.  1001 x 50257 float32 forward 39, backward 86 (4.7).
+// call 200 (5.2); float32 4096 x 32000 the same.  1001 x 50257 float32 forward 39, backward 86 (4.7) each in a row; one after the other 55 and 69: the
+// gradient's last lines leave the caches during the next forward pass.
 #pragma once
 #include "common.h"
 
@@ -179,7 +180,7 @@ __device__ inline void lp_rank(const uint64_t* cand, int count, int k, F out) {
 }
 
 // One pass for the sums, a second for the candidates.  (Kept in registers between the two, the columns of small workgroups gain nothing: 256 x 32000 with 20
-// alternatives 14.1 us both ways, 512 x 32000 24 against 19.)
+// alternatives 14.1 us both ways, 512 x 32000 24 kept and 19 read again.)
 template <typename T, int THREADS, bool TOP>
 __global__ __launch_bounds__(THREADS) void logprob_kernel(LpArgs g) {
   constexpr int E = LpPiece<T>::E, WAVES = THREADS / 64;
@@ -412,6 +413,8 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_backward_kernel(LpArgs g) 
 // Both in one call: a row stays in the registers of a workgroup between the sums and the gradient.  V pieces per thread.  The exponentials are formed
 // again for the gradient: kept, they take twice the row's registers, and no second workgroup of the CU could work while one waits for memory.
 // REST: what lies behind V pieces per thread (65536 float32, 131072 bf16) is summed beside a running maximum and read again for the gradient.
+// (1024 threads with eight pieces have 64 registers each for two workgroups to a CU and keep two more words in scratch memory: 8192 x 50257 bf16 takes 324 us, at the
+// copy's rate 320.)
 template <typename T, int THREADS, int V, bool ENTROPY, bool REST = false>
 __global__ __launch_bounds__(THREADS, V < 8 || THREADS * V == 8192 ? 8 : (V == 8 ? 7 : 4)) void logprob_grad_kernel(LpArgs g) {
   constexpr int E = LpPiece<T>::E, WAVES = THREADS / 64;
@@ -542,9 +545,13 @@ __global__ __launch_bounds__(THREADS, V < 8 || THREADS * V == 8192 ? 8 : (V == 8
   if constexpr (REST) rest(put);
 }
 
-// Workgroups of 1024 threads where they are enough for the card and 256 threads are not (with 20 alternatives: 256 x 32000 14 us, 21 split between
-// workgroups of 256 and joined; 1024 x 32000 43, 29 with 256 threads).  Fewer rows are split between workgroups of 256, as many as make 1024 of
-// them, of 512 pieces at least: a row of 128000 with 5 alternatives 7 us and 4 for the join.
+// Workgroups of 1024 threads where they are enough for the card and 256 threads are not.  us with 1024 and with 256 threads, 32000 columns in bf16: 256 rows 9.0 and
+// 10.5 (20 alternatives: 15.2 and 18.6; 21 split between workgroups of 256 and joined), 512 rows 11.9 and 12.6 (18.8 and 21.7), 768 rows 16.0 and 15.1 (27.1 and 24.6), 1024 rows
+// 19.0 and 17.8 (31.2 and 28.5).  Longer rows gain from 1024 threads for longer: 50257 columns in float32 768 rows 31.1 and 32.3 (51.9 and 53.8), 1024 rows 39.5
+// and 40.5 (64.1 and 68.6).  One border for all of them costs 14 % at worst (2048 rows of 50257 in
+// float32 with alternatives 135, 119).  Fewer rows are split between workgroups of 256, as many as make 1024 of
+// them, of 512 pieces at least: a row of 128000 with 5 alternatives 7 us and 4 for the join.  (The gradient in the same call takes a third launch then: one row
+// of 32000 8.6 us, 64 rows 10.5, 127 rows 14.1; 128 rows, a workgroup each, 9.9.)
 static bool lp_wide(int64_t m, int64_t n, bool bf16) { return m >= 128 && m < 1024 && n >= (bf16 ? 8192 : 4096); }
 static int lp_splits(int64_t m, int64_t n, bool bf16) {
   const int64_t want = m >= 128 ? 1 : 1024 / m;
@@ -603,7 +610,8 @@ static int launch_logprobs_grad(hipStream_t s, LpArgs g) {
   } while (0)
   for (g.row0 = 0; g.row0 < g.m; g.row0 += LP_ROWS) {
     const dim3 grid((unsigned)std::min<int64_t>(g.m - g.row0, LP_ROWS));
-    // (512 threads with eight pieces: 8192 x 32000 bf16 212 us, with 1024 and four 250: fewer waves wait for the same row)
+    // (512 threads with eight pieces: 8192 x 32000 bf16 203 us, with 1024 and four 239, 16384 x 16400 201 and 253: fewer waves wait for the same row; 4096 x 16000
+    // float32 106 and 103)
     if (pieces <= 256 * 2) LP_GRAD(256, 2, false);
     else if (pieces <= 256 * 8) LP_GRAD(256, 8, false);
     else if (pieces <= 512 * 8) LP_GRAD(512, 8, false);

@@ -15,8 +15,8 @@
 // adapters, 4096 -> 11008, rank 64).
 //
 // Bound by memory: single tokens by A and B, prompts by X, R and Y.  Few tokens with an adapter each: the walk is shared out over workgroups too.
-// 8192 tokens of 24 adapters, 4096 -> 11008, rank 64: ordering 10 us, down 43 (rank 16: 24), up 101 (87, 4.1 TB/s); one token, rank 16, 4.5 and 7, where each launch
-// is a chain of three reads.
+// 8192 tokens of 24 adapters, 4096 -> 11008, rank 64: ordering 10 us, down 43 (rank 16: 24), up 102 (87, 4.1 TB/s; float32 results, whose R and Y are 721 MB, 226 together);
+// one token, rank 16, 4.6 and 6.8, where each launch is a chain of three reads.
 #pragma once
 #include "common.h"
 #include "frag.h"
@@ -404,7 +404,9 @@ struct LqOut {
   typedef O vec __attribute__((ext_vector_type(E)));
   typedef vec any __attribute__((aligned(sizeof(O))));
 };
-// Few tokens: tiles of 16 in the order they come; a wave has 16 E columns.  RS: steps of the rank.
+// Few tokens: tiles of 16 in the order they come; a wave has 16 E columns.  RS: steps of the rank.  (The conditions around its loads and stores are more than the scalar
+// registers hold: 157 of them pass through vector registers for bf16 and rank up to 32, 319 beyond, 35 to 180 for float32.  They are part of its 9 us at 64 tokens,
+// 4096 -> 4096, rank 16.)
 template <typename T, typename O, int RS>
 __global__ __launch_bounds__(64 * LQ_UP_WAVES) void lora_up_kernel(LqArgs g) {
   constexpr int E = Ln<T>::E, STEP = Ln<T>::STEP;
@@ -637,7 +639,10 @@ static LqPlan lora_requests_plan(int64_t m, int64_t k, int64_t n, int r, int64_t
   LqPlan p;
   const int e = bf16 ? 8 : 4;
   // Ordering costs a launch (4 us), which the walk's serial turns cost too where there are many adapters: 64 tokens of as many, 4096 -> 4096 at rank 16
-  // (17 MB of A and B) 14 us in the order they come, 18 ordered; 4096 -> 11008 (31 MB) 27 both ways; at rank 64 (124 MB) 77 and 43.
+  // (17 MB of A and B) 14 us in the order they come, 18 ordered; 4096 -> 11008 (31 MB) 27 both ways; at rank 64 (124 MB) 77 and 43.  More than 64 tokens are ordered
+  // because the identifiers, which are not known here, may be mixed: 4096 -> 4096, rank 16, 128 tokens of 24 adapters in any order 20 us in the order they come, 13.5 ordered (5
+  // adapters 14.1 and 12.6), 512 tokens 41 and 16, 1000 tokens 74 and 20.  Where they are not, that costs up to 4 us: 128 tokens of one adapter 10.3 and 13.4,
+  // 1000 tokens 17 and 18.5; float32 1030 -> 770 of one adapter 8.5 and 13, of 24 mixed ones 12.6 and 13.3, 1000 tokens 38 and 17.
   const int64_t wide = 16 * e, cols = ceil_div64(n, wide), own = std::min(adapters, m);
   p.sorted = adapters <= LQ_SORTED && (m > 64 || r > 32 || (double)own * r * (double)(k + n) * (16 / e) > (double)(32 << 20));
   p.ldt = r <= 16 ? 16 : (r <= 32 ? 32 : 64);
