@@ -11,7 +11,7 @@
 // columns, 330 without those.)  The places of an adapter's tokens among each other depend on an atomic counter, but no result depends on them.
 //
 // T of bf16 operands enters the second product as the sum of three bf16 numbers, which hold all of its 24 digits: float32 results are off by 1.0e-7 to 1.3e-7 of
-// the norm, as those of float32 operands are (with two numbers, 16 digits, by 2.5e-6, and the second launch takes 1 to 2 % less: 102 against 104 us at 8192 tokens of 24
+// the norm, as those of float32 operands are (with two numbers, 16 digits, by 2.5e-6, and the second launch takes 1 to 2 % less: 101 against 102 us at 8192 tokens of 24
 // adapters, 4096 -> 11008, rank 64).
 //
 // Bound by memory: single tokens by A and B, prompts by X, R and Y.  Few tokens with an adapter each: the walk is shared out over workgroups too.
